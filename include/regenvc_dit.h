@@ -112,6 +112,71 @@ regenvc_status regenvc_rms_norm_fwd(const void *x, int64_t ldx, void *y, int64_t
 regenvc_status regenvc_dit_modulation(const void *w_mod, const void *b_mod, const float *e, float *mod,
                                       int32_t rows, int32_t C, void *stream);
 
+/* A norm over a row's C channels: REGENVC_NORM_LAYER (t - mean) / sqrt(var +
+   eps), biased variance, or REGENVC_NORM_RMS t / sqrt(mean(t^2) + eps); times
+   w, plus b (bf16 [C], or NULL: 1 and 0; b with REGENVC_NORM_LAYER only). */
+#define REGENVC_NORM_NONE 0
+#define REGENVC_NORM_LAYER 1
+#define REGENVC_NORM_RMS 2
+typedef struct {
+    int32_t kind;
+    float eps; /* finite, >= 0 */
+    const void *w, *b;
+} regenvc_norm;
+
+/* The f32 vectors that scale a row: gate, and the modulation of the norm after
+   it (scale and shift together, instead of that norm's w and b; or NULL: gate 1).
+   Row r of the batch takes row r / group_rows of each, ld elements apart (a
+   multiple of 4): one set for all rows with group_rows >= rows (or 0), one
+   per latent frame, or one per token with 1. */
+typedef struct {
+    const float *gate, *scale, *shift;
+    int64_t ld;
+    int32_t group_rows;
+} regenvc_row_vectors;
+
+/* The seam between two branches of a block, in one pass: what a branch gave, y,
+   is normalized, gated and added to the residual stream, and the stream is
+   normalized for the next branch:
+     u     = N_post(y)                       (post kind NONE: u = y)
+     x_out = alpha x + gate u
+     h     = N_pre(x_out) (1 + scale) + shift    (or N_pre(x_out) w + b)
+   x, x_out: f32 [rows, C]; y, h: [rows, C] in dtype (bf16, rounded to nearest
+   even, or f32); row strides ld* multiples of 8.  x_out may be x itself (same
+   pointer and stride); outputs overlap nothing else.  C a multiple of 8, at
+   most 8192; pointers 16-byte aligned; alpha finite. */
+regenvc_status regenvc_residual_norm_fwd(const float *x, int64_t ldx, const void *y, int64_t ldy, regenvc_dtype dtype,
+                                         const regenvc_norm *post, const regenvc_norm *pre,
+                                         const regenvc_row_vectors *vectors, float alpha, float *x_out, int64_t ldxo,
+                                         void *h, int64_t ldh, int32_t rows, int32_t C, void *stream);
+
+/* The f32 gradients of the vectors: dgate, dscale, dshift [groups, C], groups =
+   ceil(rows / group_rows), dw, db (of pre) and dpost_w, dpost_b [C],
+   contiguous, written, not added to; any may be NULL (not computed), and those
+   of vectors that the forward call does not have must be. */
+typedef struct {
+    float *dgate, *dscale, *dshift, *dw, *db, *dpost_w, *dpost_b;
+} regenvc_norm_grads;
+
+/* Gradients of regenvc_residual_norm_fwd.  x_out: what it wrote; y and the
+   vectors: what it read (shift is not needed); gh: gradient of h in dtype; gx:
+   f32 gradient of x_out from the rest of the program, or NULL (0).
+     dx = gradient of x (f32; may be gx itself), dy = gradient of y (in dtype)
+   Statistics are formed again from the rows.  Sums over rows are added in a
+   fixed order.  workspace: 256-byte aligned, at least
+   regenvc_residual_norm_bwd_workspace bytes (NULL if that is 0). */
+regenvc_status regenvc_residual_norm_bwd(const float *x_out, int64_t ldx, const void *y, int64_t ldy,
+                                         regenvc_dtype dtype, const regenvc_norm *post, const regenvc_norm *pre,
+                                         const regenvc_row_vectors *vectors, float alpha, const void *gh, int64_t ldgh,
+                                         const float *gx, int64_t ldgx, float *dx, int64_t lddx, void *dy, int64_t lddy,
+                                         const regenvc_norm_grads *grads, int32_t rows, int32_t C, void *workspace,
+                                         int64_t workspace_bytes, void *stream);
+
+/* Workspace bytes of such a call with group_sums gradients of gate, scale and
+   shift and row_sums of w and b asked for, on n_cu compute units.  Host-only. */
+regenvc_status regenvc_residual_norm_bwd_workspace(int32_t rows, int32_t C, int32_t group_rows, int32_t group_sums,
+                                                   int32_t row_sums, int32_t n_cu, int64_t *bytes);
+
 /* The block's parameters (device pointers, bf16): linear weights [out, in],
    biases [out], normalization scales [C]. */
 typedef struct {

@@ -46,6 +46,36 @@ class DitParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in DIT_PARAM_NAMES]
 
 
+class MxCache(ctypes.Structure):
+    """regenvc_mx_cache: device pointers and sizes of an MXFP4 key/value cache."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")] + \
+               [(n, ctypes.c_int32) for n in ("B", "capacity", "heads", "D")]
+
+
+class MxAttnPlan(ctypes.Structure):
+    """regenvc_mx_attn_plan: the decomposition of an attention call over a cache."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("tile_rows", "row_tiles", "key_ranges")]
+
+
+class Norm(ctypes.Structure):
+    """regenvc_norm: a norm over a row, with its bf16 weights."""
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p)]
+
+
+class RowVectors(ctypes.Structure):
+    """regenvc_row_vectors: gate and modulation of the rows, one set per group."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "scale", "shift")] + \
+               [("ld", ctypes.c_int64), ("group_rows", ctypes.c_int32)]
+
+
+NORM_GRAD_NAMES = ("dgate", "dscale", "dshift", "dw", "db", "dpost_w", "dpost_b")
+
+
+class NormGrads(ctypes.Structure):
+    """regenvc_norm_grads: f32 gradients of a norm's vectors."""
+    _fields_ = [(n, ctypes.c_void_p) for n in NORM_GRAD_NAMES]
+
+
 class RegenvcError(RuntimeError):
     def __init__(self, status: int, fn: str, detail: str):
         self.status = status
@@ -55,6 +85,11 @@ class RegenvcError(RuntimeError):
 _PT = ctypes.POINTER(Tensor)
 _i32 = ctypes.c_int32
 _FP = ctypes.POINTER(ctypes.c_float)
+_p = ctypes.c_void_p
+_i64 = ctypes.c_int64
+_PI64 = ctypes.POINTER(ctypes.c_int64)
+_PC = ctypes.POINTER(MxCache)
+_PN = ctypes.POINTER(Norm)
 _SIGNATURES = {
     "regenvc_attn_fwd": [_PT, _PT, _PT, _PT, ctypes.c_int, ctypes.c_void_p,
                          _i32, _i32, _i32, _i32, _i32, ctypes.c_float, ctypes.c_void_p],
@@ -109,6 +144,24 @@ _SIGNATURES = {
                               ctypes.c_int64, ctypes.c_void_p],
     "regenvc_qk_norm_rope": [_PT, _PT, ctypes.c_void_p, ctypes.c_void_p, _PT, _PT, _i32, _i32, _i32, _i32,
                              _i32, _i32, _i32, _i32, ctypes.c_float, ctypes.c_float, ctypes.c_void_p],
+    "regenvc_residual_norm_fwd": [_p, _i64, _p, _i64, ctypes.c_int, _PN, _PN, ctypes.POINTER(RowVectors), ctypes.c_float,
+                                  _p, _i64, _p, _i64, _i32, _i32, _p],
+    "regenvc_residual_norm_bwd": [_p, _i64, _p, _i64, ctypes.c_int, _PN, _PN, ctypes.POINTER(RowVectors), ctypes.c_float,
+                                  _p, _i64, _p, _i64, _p, _i64, _p, _i64, ctypes.POINTER(NormGrads), _i32, _i32, _p,
+                                  _i64, _p],
+    "regenvc_residual_norm_bwd_workspace": [_i32, _i32, _i32, _i32, _i32, _i32, _PI64],
+    "regenvc_mx_bytes": [_i32, _i32, _PI64, _PI64],
+    "regenvc_mx_quantize": [_p, ctypes.c_int, _i64, _p, _p, _i32, _i32, _p],
+    "regenvc_mx_dequantize": [_p, _p, _p, ctypes.c_int, _i64, _i32, _i32, _p],
+    "regenvc_mx_linear_fwd": [_p, _i64, _p, _p, _p, _p, _p, _p, _p, _i64, _i32, _i32, _i32, _i32, _p, _i64, _p],
+    "regenvc_mx_linear_workspace": [_i32, _i32, _i32, _i32, _i32, _i32, _PI64, _PI64],
+    "regenvc_mx_linear_plan_query": [_i32, _i32, _i32, _i32, _i32, _i64, ctypes.POINTER(TilePlan)],
+    "regenvc_mx_cache_append": [_PC, _PT, _PT, _i32, _p, _p, _p],
+    "regenvc_mx_cache_values": [_PC, _p, _p, ctypes.c_int, _p],
+    "regenvc_mx_attn_cache_fwd": [_PT, _PC, _p, _i32, _PT, ctypes.c_int, _p, _i32, _i32, _i32, ctypes.c_float, _p, _i64,
+                                  _p],
+    "regenvc_mx_attn_cache_workspace": [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _PI64],
+    "regenvc_mx_attn_cache_plan_query": [_i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(MxAttnPlan)],
 }
 
 _lib = None
@@ -148,6 +201,50 @@ def stream_of(device) -> int:
     if raw is not None and device.index is not None:
         return raw(device.index)
     return torch.cuda.current_stream(device).cuda_stream
+
+
+class _Nothing:
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return False
+
+
+_NOTHING = _Nothing()
+
+
+def on_device(device):
+    """Context with a torch device current (nothing to do where it is already)."""
+    import torch
+    return _NOTHING if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def same_device(device, **tensors) -> None:
+    """Refuses tensors (None: not given) that lie elsewhere than on `device`."""
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def device_index(device) -> int:
+    """The index of a torch device (the current one's where it has none)."""
+    import torch
+    idx = torch.device(device).index
+    return torch.cuda.current_device() if idx is None else idx
+
+
+_N_CU = {}  # device index -> compute units
+
+
+def compute_units(device) -> int:
+    """Compute units of a torch device."""
+    import torch
+    idx = device_index(device)
+    n = _N_CU.get(idx)
+    if n is None:
+        n = _N_CU[idx] = torch.cuda.get_device_properties(idx).multi_processor_count
+    return n
 
 
 def split_workspace(need: int, device):

@@ -41,20 +41,7 @@ def _desc(t: torch.Tensor, name: str, dtype: torch.dtype) -> _lib.Tensor:
 _stream = _lib.stream_of
 
 
-class _Nothing:
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        return False
-
-
-_NOTHING = _Nothing()
-
-
-def _on(device: torch.device):
-    """Context with `device` current (nothing to do where it is already)."""
-    return _NOTHING if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+_on = _lib.on_device
 
 
 def _fptr(t: Optional[torch.Tensor], name: str, shape) -> Optional[int]:

@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_NAME = "libregenvc_attn.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 SOURCES = ["api.cpp", "attn_fwd.hip", "lse_merge.hip", "norm_rope.hip", "dit_api.cpp", "dit.hip", "vae_api.cpp",
-           "vae.hip"]
+           "vae.hip", "residual_norm_api.cpp", "residual_norm.hip", "mx_api.cpp", "mx.hip", "mx_attn.hip"]
 ARCH = "gfx950"
 # MFMA results in VGPRs: the score tiles feed VALU softmax code directly, and
 # read-only operands may then live in AGPRs.  Not for the tile kernels of the

@@ -39,6 +39,13 @@ inline Range range_of(const void *p, int64_t bytes)
     const uintptr_t b = reinterpret_cast<uintptr_t>(p);
     return Range{b, b + (uintptr_t)bytes};
 }
+// Checks a [B, S, H, D] view (pointer, alignment, strides, offsets) and gives the bytes that it can touch.
+regenvc_status view_range(const char *name, const regenvc_tensor *t, int64_t B, int64_t S, int64_t H, int64_t D,
+                          size_t elem, Range *r);
+// No two elements of the view share an address (what an output needs).
+bool view_injective(const regenvc_tensor *t, int64_t B, int64_t S, int64_t H, int64_t D);
+// REGENVC_OK if s is finite and not negative.
+regenvc_status softmax_scale_ok(float s);
 inline bool overlaps(const Range &a, const Range &b)
 {
     return a.lo < b.hi && b.lo < a.hi;

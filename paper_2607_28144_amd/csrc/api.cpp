@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstring>
 
+#include "abi_util.hpp"
 #include "attn_kernels.hpp"
 
 namespace {
@@ -763,6 +764,25 @@ regenvc_status launch_status(hipError_t e, const char *what)
 void clear_error()
 {
     g_last_error[0] = '\0';
+}
+
+regenvc_status view_range(const char *name, const regenvc_tensor *t, int64_t B, int64_t S, int64_t H, int64_t D,
+                          size_t elem, Range *r)
+{
+    Extent e{};
+    const regenvc_status st = check_view(name, t, B, S, H, D, elem, &e);
+    *r = Range{e.lo, e.hi};
+    return st;
+}
+
+bool view_injective(const regenvc_tensor *t, int64_t B, int64_t S, int64_t H, int64_t D)
+{
+    return view_is_injective(t, B, S, H, D);
+}
+
+regenvc_status softmax_scale_ok(float s)
+{
+    return check_scale(s);
 }
 
 }  // namespace abi

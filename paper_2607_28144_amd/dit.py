@@ -9,7 +9,7 @@ and normalization scales bf16 [n]; modulation vectors float32.
 from __future__ import annotations
 
 import ctypes
-from typing import Dict, Optional
+from typing import Dict, NamedTuple, Optional, Tuple
 
 import torch
 
@@ -125,6 +125,137 @@ def modulation(w_mod: torch.Tensor, b_mod: torch.Tensor, e: torch.Tensor,
                                             rows, C, _stream(e.device))
     _lib.check(st, "regenvc_dit_modulation")
     return out
+
+
+_NORM = {None: 0, "layer": 1, "rms": 2}
+
+
+def _norm(kind: Optional[str], eps: float, w, b, C: int, name: str) -> _lib.Norm:
+    if kind not in _NORM:
+        raise ValueError(f"{name}={kind!r} ('layer', 'rms'" + (" or None)" if name == "post" else ")"))
+    return _lib.Norm(_NORM[kind], eps, _vec(w, f"{name} w", torch.bfloat16, C), _vec(b, f"{name} b", torch.bfloat16, C))
+
+
+def _row_vectors(rows: int, C: int, group_rows: int, device, **vectors) -> _lib.RowVectors:
+    """gate, scale, shift: float32 [C] or [groups, C] with one row stride."""
+    groups = -(-rows // group_rows) if group_rows > 0 else 1
+    ld = None
+    ptrs = {}
+    for name, t in vectors.items():
+        if t is None:
+            ptrs[name] = None
+            continue
+        if t.device != device or t.dtype != torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != C \
+                or (C > 1 and t.stride(-1) != 1) or (t.dim() == 2 and t.shape[0] != groups and rows > 0) \
+                or (t.dim() == 1 and groups > 1):
+            raise ValueError(f"{name} must be float32 [{groups}, {C}] on {device} with unit column stride")
+        if t.dim() == 2 and groups > 1:
+            if ld is not None and t.stride(0) != ld:
+                raise ValueError("gate, scale and shift must have one row stride")
+            ld = t.stride(0)
+        ptrs[name] = t.data_ptr()
+    return _lib.RowVectors(ptrs["gate"], ptrs["scale"], ptrs["shift"], C if ld is None else ld, group_rows)
+
+
+def residual_norm_fwd(x: torch.Tensor, y: torch.Tensor, norm: str = "layer", post: Optional[str] = None,
+                      gate: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                      shift: Optional[torch.Tensor] = None, w: Optional[torch.Tensor] = None,
+                      b: Optional[torch.Tensor] = None, post_w: Optional[torch.Tensor] = None,
+                      post_b: Optional[torch.Tensor] = None, alpha: float = 1.0, eps: float = 1e-6,
+                      group_rows: int = 0, out: Optional[torch.Tensor] = None,
+                      h: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The seam between two branches (regenvc_residual_norm_fwd): x' = alpha x +
+    gate N_post(y), h = N_pre(x') (1 + scale) + shift (or w, b).  x: float32
+    [rows, C]; y: bf16 or float32; post, norm: 'layer' or 'rms' (post may be
+    None); gate, scale, shift: float32 [C], or [groups, C] with a set for every
+    group_rows rows.  out may be x.  Returns (x', h), h in y's type."""
+    rows, C = x.shape
+    ldx = _rows(x, "x", torch.float32)
+    if y.dtype not in (torch.bfloat16, torch.float32) or tuple(y.shape) != (rows, C):
+        raise ValueError(f"y must be bfloat16 or float32 {(rows, C)}")
+    ldy = _rows(y, "y", y.dtype)
+    out = torch.empty((rows, C), dtype=torch.float32, device=x.device) if out is None else out
+    h = torch.empty((rows, C), dtype=y.dtype, device=x.device) if h is None else h
+    if tuple(out.shape) != (rows, C) or tuple(h.shape) != (rows, C):
+        raise ValueError(f"out and h must be {(rows, C)}")
+    ldo, ldh = _rows(out, "out", torch.float32), _rows(h, "h", y.dtype)
+    v = _row_vectors(rows, C, group_rows, x.device, gate=gate, scale=scale, shift=shift)
+    np, nq = _norm(post, eps, post_w, post_b, C, "post"), _norm(norm, eps, w, b, C, "norm")
+    _lib.same_device(x.device, y=y, out=out, h=h, w=w, b=b, post_w=post_w, post_b=post_b)
+    with _lib.on_device(x.device):
+        st = _lib.load().regenvc_residual_norm_fwd(
+            x.data_ptr(), ldx, y.data_ptr(), ldy, _lib.F32 if y.dtype == torch.float32 else _lib.BF16, ctypes.byref(np),
+            ctypes.byref(nq), ctypes.byref(v), float(alpha), out.data_ptr(), ldo, h.data_ptr(), ldh, rows, C,
+            _stream(x.device))
+    _lib.check(st, "regenvc_residual_norm_fwd")
+    return out, h
+
+
+class ResidualNormGrads(NamedTuple):
+    """Gradients of residual_norm_fwd; those of vectors that were not given are None."""
+    dx: torch.Tensor
+    dy: torch.Tensor
+    dgate: Optional[torch.Tensor] = None
+    dscale: Optional[torch.Tensor] = None
+    dshift: Optional[torch.Tensor] = None
+    dw: Optional[torch.Tensor] = None
+    db: Optional[torch.Tensor] = None
+    dpost_w: Optional[torch.Tensor] = None
+    dpost_b: Optional[torch.Tensor] = None
+
+
+def residual_norm_bwd(x_out: torch.Tensor, y: torch.Tensor, gh: torch.Tensor, gx: Optional[torch.Tensor] = None,
+                      norm: str = "layer", post: Optional[str] = None, gate: Optional[torch.Tensor] = None,
+                      scale: Optional[torch.Tensor] = None, w: Optional[torch.Tensor] = None,
+                      b: Optional[torch.Tensor] = None, post_w: Optional[torch.Tensor] = None,
+                      post_b: Optional[torch.Tensor] = None, alpha: float = 1.0, eps: float = 1e-6,
+                      group_rows: int = 0, dx: Optional[torch.Tensor] = None,
+                      dy: Optional[torch.Tensor] = None) -> ResidualNormGrads:
+    """Gradients of residual_norm_fwd (regenvc_residual_norm_bwd), given those
+    of h (gh, in y's type) and of x' from the rest of the program (gx, float32,
+    or None).  x_out: the forward call's x'.  dx may be gx.  The gradients of
+    the vectors are float32, shaped [groups, C] (gate, scale, shift) and [C]."""
+    rows, C = x_out.shape
+    ldx = _rows(x_out, "x_out", torch.float32)
+    if y.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("y must be bfloat16 or float32")
+    dev = x_out.device
+    dx = torch.empty((rows, C), dtype=torch.float32, device=dev) if dx is None else dx
+    dy = torch.empty((rows, C), dtype=y.dtype, device=dev) if dy is None else dy
+    for name, t in (("y", y), ("gh", gh), ("gx", gx), ("dx", dx), ("dy", dy)):
+        if t is not None and tuple(t.shape) != (rows, C):
+            raise ValueError(f"{name} must be {(rows, C)}")
+    ldy, ldgh, lddy = _rows(y, "y", y.dtype), _rows(gh, "gh", y.dtype), _rows(dy, "dy", y.dtype)
+    ldgx = 0 if gx is None else _rows(gx, "gx", torch.float32)
+    lddx = _rows(dx, "dx", torch.float32)
+    v = _row_vectors(rows, C, group_rows, dev, gate=gate, scale=scale, shift=None)
+    np, nq = _norm(post, eps, post_w, post_b, C, "post"), _norm(norm, eps, w, b, C, "norm")
+    _lib.same_device(dev, y=y, gh=gh, gx=gx, dx=dx, dy=dy, w=w, b=b, post_w=post_w, post_b=post_b)
+    groups = -(-rows // group_rows) if group_rows > 0 else 1
+
+    def grad(of, *shape):
+        return None if of is None else torch.empty(shape, dtype=torch.float32, device=dev)
+    g = ResidualNormGrads(dx, dy, grad(gate, groups, C), grad(scale, groups, C), grad(scale, groups, C), grad(w, C),
+                          grad(b, C), grad(post_w, C), grad(post_b, C))
+    if rows == 0:  # sums over no rows
+        for t in g[2:]:
+            if t is not None:
+                t.zero_()
+        return g
+    grads = _lib.NormGrads(*[None if t is None else t.data_ptr() for t in g[2:]])
+    need = ctypes.c_int64()
+    _lib.check(_lib.load().regenvc_residual_norm_bwd_workspace(
+        rows, C, group_rows, sum(t is not None for t in g[2:5]), sum(t is not None for t in g[5:]),
+        _lib.compute_units(dev), ctypes.byref(need)), "regenvc_residual_norm_bwd_workspace")
+    with _lib.on_device(dev):
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value > 0 else None
+        st = _lib.load().regenvc_residual_norm_bwd(
+            x_out.data_ptr(), ldx, y.data_ptr(), ldy, _lib.F32 if y.dtype == torch.float32 else _lib.BF16,
+            ctypes.byref(np), ctypes.byref(nq), ctypes.byref(v), float(alpha), gh.data_ptr(), ldgh,
+            gx.data_ptr() if gx is not None else None, ldgx, dx.data_ptr(), lddx, dy.data_ptr(), lddy,
+            ctypes.byref(grads), rows, C, ws.data_ptr() if ws is not None else None, need.value, _stream(dev))
+    _lib.check(st, "regenvc_residual_norm_bwd")
+    return g
 
 
 class DitBlock:
