@@ -272,8 +272,8 @@ regenvc_status regenvc_mx_cache_append(const regenvc_mx_cache *cache, const rege
     if (meets_itself(rc) || meets(rc, rk) || meets(rc, rv) || (start && meets(rc, range_of(start, nb))) ||
         (count && meets(rc, range_of(count, nb))))
         return failf(REGENVC_ERR_INVALID_ARG, "%s: the cache overlaps itself or an input", fn);
-    if ((int64_t)cache->B * S > ((int64_t)1 << 38) / ((int64_t)cache->heads * (cache->D / 8)))
-        return failf(REGENVC_ERR_UNSUPPORTED, "%s: too many tokens for one call", fn);
+    if (cache->B > 65535 || (int64_t)S > INT32_MAX / ((int64_t)cache->heads * (cache->D / 8)))
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: too many sequences or tokens for one call", fn);
     if ((st = regenvc::abi::device_ok()) != REGENVC_OK) return st;
     const mx::AppendArgs a{cache_of(*cache), k->ptr,      v->ptr,      k->stride_b, k->stride_s, k->stride_h, v->stride_b,
                            v->stride_s,      v->stride_h, start,       count,       S};
@@ -295,7 +295,8 @@ regenvc_status regenvc_mx_cache_values(const regenvc_mx_cache *cache, void *k, v
     const Range rk = range_of(k, n * (dtype == REGENVC_F32 ? 4 : 2)), rv = range_of(v, n * (dtype == REGENVC_F32 ? 4 : 2));
     if (overlaps(rk, rv) || meets(rc, rk) || meets(rc, rv))
         return failf(REGENVC_ERR_INVALID_ARG, "%s: k, v and the cache overlap", fn);
-    if (n > (int64_t)1 << 41) return failf(REGENVC_ERR_UNSUPPORTED, "%s: the cache is too large for one call", fn);
+    if (cache->B > 65535 || (int64_t)cache->capacity > INT32_MAX / ((int64_t)cache->heads * (cache->D / 8)))
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: too many sequences or places for one call", fn);
     if ((st = regenvc::abi::device_ok()) != REGENVC_OK) return st;
     const mx::ValuesArgs a{cache_of(*cache), k, v, dtype == REGENVC_F32};
     return regenvc::abi::launch_status(mx::launch_values(a, static_cast<hipStream_t>(stream)), fn);
