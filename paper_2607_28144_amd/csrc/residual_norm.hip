@@ -87,15 +87,18 @@ __device__ __forceinline__ F8 vec_f32(const float *p, int64_t at, float missing)
     for (int i = 0; i < 8; ++i) r.v[i] = q[i];
     return r;
 }
+__device__ __forceinline__ Raw<false> raw_bf16(const uint16_t *p, int at, float missing)
+{
+    if (p != nullptr) return load_raw<false>(p, at);
+    Raw<false> r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.a[i] = (__bf16)missing;
+    return r;
+}
 __device__ __forceinline__ F8 vec_bf16(const uint16_t *p, int at, float missing)
 {
+    const Raw<false> q = raw_bf16(p, at, missing);
     F8 r;
-    if (p == nullptr) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = missing;
-        return r;
-    }
-    const Raw<false> q = load_raw<false>(p, at);
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.v[i] = q[i];
     return r;
@@ -115,57 +118,68 @@ __device__ __forceinline__ F8 pre_add(const ResidualNormArgs &a, int64_t gv, int
     return a.shift != nullptr ? vec_f32(a.shift, gv + c, 0.f) : vec_bf16(a.pre.b, c, 0.f);
 }
 
-// Sums of N values over the lanes of a row: its wave, or its workgroup's four
-// waves (through LDS; `turn` names the half that this sum uses, so that one
-// barrier a sum suffices).
-template <int WPR, int N>
-__device__ __forceinline__ void row_sum(float (&s)[N], float (*lds)[2 * kWaves], int &turn)
+// x summed over the wave: four steps within rows of 16 lanes by DPP, two
+// exchanges of rows; no LDS.  Every lane gets the sum.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x)
 {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1)
-#pragma unroll
-        for (int k = 0; k < N; ++k) s[k] += __shfl_xor(s[k], m, 64);
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x = dpp_add<0xb1>(x);   // lane ^ 1
+    x = dpp_add<0x4e>(x);   // lane ^ 2
+    x = dpp_add<0x141>(x);  // 7 - lane, of 8
+    x = dpp_add<0x140>(x);  // 15 - lane, of 16
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(u[0]) + __uint_as_float(u[1]);
+}
+
+// Sum over the lanes of a row: its wave, or its workgroup's four waves
+// (through LDS; `turn` names the half that this sum uses, so that one barrier
+// a sum suffices).
+template <int WPR>
+__device__ __forceinline__ float row_sum(float s, float (*lds)[kWaves], int &turn)
+{
+    s = wave_sum(s);
     if constexpr (WPR > 1) {
         float *slot = lds[turn];
         turn ^= 1;
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) slot[k * kWaves + (threadIdx.x >> 6)] = s[k];
-        }
+        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = s;
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < N; ++k) s[k] = (slot[k * kWaves] + slot[k * kWaves + 1]) + (slot[k * kWaves + 2] + slot[k * kWaves + 3]);
+        s = (slot[0] + slot[1]) + (slot[2] + slot[3]);
     }
+    return s;
 }
 
 // Mean (0 for RMS) and 1/sigma of the row whose values val(v, i) this lane
 // holds for v < NV with on[v].
 template <int WPR, int NV, class Val>
 __device__ __forceinline__ void row_stats(const Val &val, const bool (&on)[NV], int kind, float inv_c, float eps,
-                                          float (*lds)[2 * kWaves], int &turn, float &mu, float &rstd)
+                                          float (*lds)[kWaves], int &turn, float &mu, float &rstd)
 {
     mu = 0.f;
     if (kind == kNormLayer) {
-        float s[1] = {0.f};
+        float s = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += val(v, i);
-        row_sum<WPR>(s, lds, turn);
-        mu = s[0] * inv_c;
+            for (int i = 0; i < 8; ++i) s += val(v, i);
+        mu = row_sum<WPR>(s, lds, turn) * inv_c;
     }
-    float q[1] = {0.f};
+    float q = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
         if (on[v]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = val(v, i) - mu;
-                q[0] = fmaf(d, d, q[0]);
+                q = fmaf(d, d, q);
             }
         }
-    row_sum<WPR>(q, lds, turn);
-    rstd = rsqrtf(q[0] * inv_c + eps);
+    rstd = rsqrtf(row_sum<WPR>(q, lds, turn) * inv_c + eps);
 }
 
 // Forward: WPR waves per row, NV eight-channel chunks per lane.
@@ -173,7 +187,7 @@ template <int NV, int WPR, bool F32>
 __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(ResidualNormArgs a)
 {
     constexpr int TPR = 64 * WPR;  // lanes of a row
-    __shared__ float lds[2][2 * kWaves];
+    __shared__ float lds[2][kWaves];
     int turn = 0;
     const int t = threadIdx.x % TPR;
     const int64_t row = __builtin_amdgcn_readfirstlane((int)blockIdx.x * (kThreads / TPR) + (int)threadIdx.x / TPR);
@@ -226,8 +240,39 @@ __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(ResidualNor
     }
 }
 
-// Sums over rows that the backward pass keeps per lane, one F8 per chunk.
+// Sums over rows that the backward pass keeps per lane.
 enum Sum { kSumGate, kSumMul, kSumAdd, kSumPostW, kSumPostB };
+
+// A row's values of one lane, as loaded.
+template <bool F32>
+struct RowIn {
+    Raw<true> x, gx;
+    Raw<F32> y, gh;
+};
+
+// What a row's waves tell each other: count, mean and sum of squared
+// deviations of their columns (a mean of 0 for RMS norms), or plain sums.
+struct Share {
+    float v[4];
+};
+
+// Mean and 1/sigma of a row from its waves' shares (Chan's combination, exact
+// in the mean's square); wave w holds min(512, C - 512 w) columns.
+__device__ __forceinline__ void join_stats(const Share *sh, int waves, int C, int at, bool layer, float inv_c, float eps,
+                                           float &mu, float &rstd)
+{
+    float s = 0.f, q = 0.f;
+    mu = 0.f;
+    if (layer) {
+        for (int w = 0; w < waves; ++w) s = fmaf((float)min(512, C - 512 * w), sh[w].v[at], s);
+        mu = s * inv_c;
+    }
+    for (int w = 0; w < waves; ++w) {
+        const float d = sh[w].v[at] - mu;
+        q += layer ? fmaf((float)min(512, C - 512 * w) * d, d, sh[w].v[at + 1]) : sh[w].v[at + 1];
+    }
+    rstd = rsqrtf(q * inv_c + eps);
+}
 
 // Backward of one row, in the order of the chain rule (m = mean over the C
 // channels, n = N_pre(x'), p = N_post(y)):
@@ -236,53 +281,75 @@ enum Sum { kSumGate, kSumMul, kSumAdd, kSumPostW, kSumPostB };
 //     q  = du w_post               dy = (q - m(q) - p m(q p)) / sigma_y
 //     dscale, dw = sum gh n        dshift, db = sum gh
 //     dpost_w = sum du p           dpost_b = sum du
-// (without m(g), m(q) for RMS norms; dy = du without a post-norm).  A
-// workgroup walks the rows of its segments, keeps the sums over them in
-// registers and adds its waves' through LDS at the end of a segment, in a
-// fixed order: no atomics.  NS: sums held (3, 4 with a post-norm, 5 with its bias).
-template <int NV, int WPR, bool F32, int NS>
-__global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(ResidualNormArgs a, ResidualNormPlan p,
-                                                                     float *group_ws, float *row_ws)
+// (without m(g), m(q) for RMS norms; dy = du without a post-norm).
+//
+// A row is worked on by W = ceil(C / 512) waves, eight channels per lane, so
+// that the sums over rows, a row's values and the next row's, already requested,
+// fit 128 registers a lane; a workgroup works on R rows at a time.  The waves
+// of a row exchange their shares of its statistics through LDS: of both norms
+// in one step, then m(g), m(g n), then m(q), m(q p).  The sums over rows stay
+// in registers until a segment ends and are then added over the R rows through
+// LDS, in a fixed order: no atomics.  NS: sums held (3, 4 with a post-norm, 5
+// with its bias).
+// WIDE: more than eight waves.
+template <bool F32, int NS, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 512) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : NS == 3 ? 3 : 2)))
+void residual_norm_bwd_kernel(ResidualNormArgs a, ResidualNormPlan p, float *group_ws,
+                                                                 float *row_ws)
 {
-    constexpr int TPR = 64 * WPR, RPB = kThreads / TPR;  // lanes of a row, rows at a time
     constexpr bool POST = NS > 3;
-    __shared__ float lds[2][2 * kWaves];
-    __shared__ __attribute__((aligned(16))) float stage[RPB > 1 ? RPB * NV * TPR * 8 : 4];
-    int turn = 0;
-    const int t = threadIdx.x % TPR, lane_row = threadIdx.x / TPR;
-    const float inv_c = 1.0f / (float)a.C;
-    const bool modulated = a.scale != nullptr;
-    bool on[NV];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) on[v] = (v * TPR + t) * 8 < a.C;
+    __shared__ Share share[3][16];
+    __shared__ __attribute__((aligned(16))) float stage[8 * 512];
+    const int W = p.row_waves, R = p.rows_at_once;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int slot = wave / W, rw = wave - slot * W;  // which of the R rows, which wave of it
+    const int c = rw * 512 + lane * 8;
+    const bool on = c < a.C;
+    const float inv_c = 1.0f / (float)a.C, inv_n = 1.0f / (float)min(512, a.C - 512 * rw);
+    const bool modulated = a.scale != nullptr, pre_layer = a.pre.kind == kNormLayer, post_layer = a.post.kind == kNormLayer;
 
-    F8 sum[NS][NV];
-    auto clear = [&](int s) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) sum[s][v] = F8{};
-    };
+    F8 sum[NS] = {};
     // the workgroup's sum s to out [C] (null: dropped)
     auto flush = [&](int s, float *out) {
         if (out == nullptr) return;
-        if constexpr (RPB > 1) {
+        if (R > 1) {
             __syncthreads();
-#pragma unroll
-            for (int v = 0; v < NV; ++v) store8<true>(stage, (lane_row * NV + v) * TPR * 8 + t * 8, sum[s][v]);
+            store8<true>(stage, (slot * W + rw) * 512 + lane * 8, sum[s]);
             __syncthreads();
-            for (int c = threadIdx.x; c < a.C; c += kThreads) {
-                float z = stage[c];
-#pragma unroll
-                for (int k = 1; k < RPB; ++k) z += stage[k * NV * TPR * 8 + c];
-                out[c] = z;
+            for (int k = threadIdx.x; k < a.C; k += blockDim.x) {
+                float z = stage[k];
+                for (int j = 1; j < R; ++j) z += stage[j * W * 512 + k];
+                out[k] = z;
             }
-        } else {
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-                if (on[v]) store8<true>(out, (v * TPR + t) * 8, sum[s][v]);
+        } else if (on) {
+            store8<true>(out, c, sum[s]);
         }
     };
+    auto load = [&](RowIn<F32> &in, int64_t row, bool valid) {
+        in = RowIn<F32>{};
+        if (!valid || !on) return;
+        in.x = load_raw<true>(a.x, row * a.ldx + c);
+        in.gh = load_raw<F32>(a.gh, row * a.ldgh + c);
+        in.y = load_raw<F32>(a.y, row * a.ldy + c);
+        if (a.gx != nullptr) in.gx = load_raw<true>(a.gx, row * a.ldgx + c);
+    };
+    // this wave's count-free share of a row's statistics
+    auto wave_stats = [&](const auto &v, bool layer, float &mean, float &dev) {
+        mean = 0.f;
+        if (layer) {
+            float s = 0.f;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) clear(s);
+            for (int i = 0; i < 8; ++i) s += v[i];
+            mean = wave_sum(s) * inv_n;
+        }
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = v[i] - mean;
+            q = fmaf(d, d, q);
+        }
+        dev = wave_sum(on ? q : 0.f);
+    };
 
     for (int64_t seg = blockIdx.x; seg < p.segments(); seg += gridDim.x) {
         const int group = (int)(seg / p.per_group), part = (int)(seg % p.per_group);
@@ -290,92 +357,102 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(ResidualNor
         const int64_t n = min((int64_t)a.group_rows, a.rows - gr0);
         const int64_t r0 = gr0 + n * part / p.per_group, r1 = gr0 + n * (part + 1) / p.per_group;
         const int64_t gv = (int64_t)group * a.ldv;
-        for (int64_t rr = r0; rr < r1; rr += RPB) {
-            const int64_t row = __builtin_amdgcn_readfirstlane((int)rr + lane_row);
-            if (row >= r1) break;  // with WPR > 1 never within a row
-            Raw<F32> y[NV], gh[NV];
-            Raw<true> x[NV], gx[NV];
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * TPR + t) * 8;
-                y[v] = gh[v] = Raw<F32>{};
-                x[v] = gx[v] = Raw<true>{};
-                if (on[v]) {
-                    x[v] = load_raw<true>(a.x, row * a.ldx + c);
-                    gh[v] = load_raw<F32>(a.gh, row * a.ldgh + c);
-                    y[v] = load_raw<F32>(a.y, row * a.ldy + c);
-                    if (a.gx != nullptr) gx[v] = load_raw<true>(a.gx, row * a.ldgx + c);
-                }
+        // the vectors stay in registers too: a load of them within a row would wait, as loads return in order, for the
+        // next row's
+        F8 mul{}, gate{};
+        Raw<false> pw{}, pb{};
+        if (on) {
+            mul = pre_mul(a, gv, c);
+            gate = vec_f32(a.gate, gv + c, 1.f);
+            if constexpr (POST) pw = raw_bf16(a.post.w, c, 1.f), pb = raw_bf16(a.post.b, c, 0.f);
+        }
+        RowIn<F32> next;
+        load(next, r0 + slot, r0 + slot < r1);
+        for (int64_t rr = r0; rr < r1; rr += R) {  // the same number of rounds, and of barriers, for all R rows
+            const int64_t row = rr + slot;
+            const bool valid = row < r1;
+            const RowIn<F32> in = next;
+            load(next, row + R, row + R < r1);
+            // statistics of both norms
+            Share mine{};
+            wave_stats(in.x, pre_layer, mine.v[0], mine.v[1]);
+            if constexpr (POST) wave_stats(in.y, post_layer, mine.v[2], mine.v[3]);
+            float mu, rstd, mu_y = 0.f, rstd_y = 1.f;
+            if (W > 1) {
+                if (lane == 0) share[0][wave] = mine;
+                __syncthreads();
             }
-            float mu, rstd;
-            row_stats<WPR, NV>([&](int v, int i) { return x[v][i]; }, on, a.pre.kind, inv_c, a.pre.eps, lds, turn, mu,
-                               rstd);
-            float m[2] = {0.f, 0.f};
-            F8 g[NV];
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                if (!on[v]) continue;
-                const F8 mul = pre_mul(a, gv, (v * TPR + t) * 8);
+            if (W > 1) {
+                join_stats(share[0] + slot * W, W, a.C, 0, pre_layer, inv_c, a.pre.eps, mu, rstd);
+                if constexpr (POST) join_stats(share[0] + slot * W, W, a.C, 2, post_layer, inv_c, a.post.eps, mu_y, rstd_y);
+            } else {
+                mu = mine.v[0], rstd = rsqrtf(mine.v[1] * inv_c + a.pre.eps);
+                if constexpr (POST) mu_y = mine.v[2], rstd_y = rsqrtf(mine.v[3] * inv_c + a.post.eps);
+            }
+            // m(g), m(g n)
+            F8 g{};
+            float m0 = 0.f, m1 = 0.f;
+            if (on && valid) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float nn = (x[v][i] - mu) * rstd;
-                    g[v].v[i] = gh[v][i] * mul.v[i];
-                    m[0] += g[v].v[i];
-                    m[1] = fmaf(g[v].v[i], nn, m[1]);
-                    sum[kSumMul][v].v[i] = fmaf(gh[v][i], nn, sum[kSumMul][v].v[i]);
-                    sum[kSumAdd][v].v[i] += gh[v][i];
+                    const float nn = (in.x[i] - mu) * rstd;
+                    g.v[i] = in.gh[i] * mul.v[i];
+                    m0 += g.v[i];
+                    m1 = fmaf(g.v[i], nn, m1);
+                    sum[kSumMul].v[i] = fmaf(in.gh[i], nn, sum[kSumMul].v[i]);
+                    sum[kSumAdd].v[i] += in.gh[i];
                 }
             }
-            row_sum<WPR>(m, lds, turn);
-            const float mg = a.pre.kind == kNormLayer ? m[0] * inv_c : 0.f, mgn = m[1] * inv_c;
-            float mu_y = 0.f, rstd_y = 1.f;
-            if constexpr (POST)
-                row_stats<WPR, NV>([&](int v, int i) { return y[v][i]; }, on, a.post.kind, inv_c, a.post.eps, lds, turn,
-                                   mu_y, rstd_y);
-            m[0] = m[1] = 0.f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                if (!on[v]) continue;
-                const int c = (v * TPR + t) * 8;
-                const F8 gate = vec_f32(a.gate, gv + c, 1.f);
-                F8 w, b, dx;
-                if constexpr (POST) w = vec_bf16(a.post.w, c, 1.f), b = vec_bf16(a.post.b, c, 0.f);
+            auto row_means = [&](int buf) {  // m0, m1 summed over the row, times 1 / C
+                m0 = wave_sum(m0), m1 = wave_sum(m1);
+                if (W > 1) {
+                    if (lane == 0) share[buf][wave].v[0] = m0, share[buf][wave].v[1] = m1;
+                    __syncthreads();
+                    m0 = m1 = 0.f;
+                    for (int w = 0; w < W; ++w) m0 += share[buf][slot * W + w].v[0], m1 += share[buf][slot * W + w].v[1];
+                }
+                m0 *= inv_c, m1 *= inv_c;
+            };
+            row_means(1);
+            const float mg = pre_layer ? m0 : 0.f, mgn = m1;
+            m0 = m1 = 0.f;
+            if (on && valid) {
+                F8 dx;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float nn = (x[v][i] - mu) * rstd;
-                    const float dr = gx[v][i] + rstd * (g[v].v[i] - mg - nn * mgn);
+                    const float nn = (in.x[i] - mu) * rstd;
+                    const float dr = in.gx[i] + rstd * (g.v[i] - mg - nn * mgn);
                     dx.v[i] = a.alpha * dr;
                     const float du = gate.v[i] * dr;
-                    float u = y[v][i];
-                    g[v].v[i] = du;
+                    float u = in.y[i];
+                    g.v[i] = du;
                     if constexpr (POST) {
                         const float pn = (u - mu_y) * rstd_y;
-                        u = fmaf(pn, w.v[i], b.v[i]);
-                        sum[kSumPostW][v].v[i] = fmaf(du, pn, sum[kSumPostW][v].v[i]);
-                        if constexpr (NS > 4) sum[kSumPostB][v].v[i] += du;
-                        const float q = du * w.v[i];
-                        g[v].v[i] = q;
-                        m[0] += q;
-                        m[1] = fmaf(q, pn, m[1]);
+                        u = fmaf(pn, pw[i], pb[i]);
+                        sum[kSumPostW].v[i] = fmaf(du, pn, sum[kSumPostW].v[i]);
+                        if constexpr (NS > 4) sum[kSumPostB].v[i] += du;
+                        g.v[i] = du * pw[i];
+                        m0 += g.v[i];
+                        m1 = fmaf(g.v[i], pn, m1);
                     }
-                    sum[kSumGate][v].v[i] = fmaf(dr, u, sum[kSumGate][v].v[i]);
+                    sum[kSumGate].v[i] = fmaf(dr, u, sum[kSumGate].v[i]);
                 }
                 store8<true>(a.dx, row * a.lddx + c, dx);
             }
             float mq = 0.f, mqp = 0.f;
             if constexpr (POST) {
-                row_sum<WPR>(m, lds, turn);
-                mq = a.post.kind == kNormLayer ? m[0] * inv_c : 0.f, mqp = m[1] * inv_c;
+                row_means(2);
+                mq = post_layer ? m0 : 0.f, mqp = m1;
             }
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                if (!on[v]) continue;
+            if (on && valid) {
                 F8 dy;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    dy.v[i] = POST ? rstd_y * (g[v].v[i] - mq - (y[v][i] - mu_y) * rstd_y * mqp) : g[v].v[i];
-                store8<F32>(a.dy, row * a.lddy + (v * TPR + t) * 8, dy);
+                    dy.v[i] = POST ? rstd_y * (g.v[i] - mq - (in.y[i] - mu_y) * rstd_y * mqp) : g.v[i];
+                store8<F32>(a.dy, row * a.lddy + c, dy);
             }
+            // without a post-norm the first exchange of the next row lies one barrier behind the last read of this
+            // one's share[0], as with one
         }
         // the sums over a group's rows: whole, or this segment's share
         const bool whole = p.per_group == 1;
@@ -385,12 +462,11 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(ResidualNor
             return whole ? out + (int64_t)group * a.C : group_ws + ((int64_t)k++ * p.segments() + seg) * a.C;
         };
         flush(kSumGate, to(a.dgate));
-        clear(kSumGate);
+        sum[kSumGate] = F8{};
         if (modulated) {
             flush(kSumMul, to(a.dscale));
             flush(kSumAdd, to(a.dshift));
-            clear(kSumMul);
-            clear(kSumAdd);
+            sum[kSumMul] = sum[kSumAdd] = F8{};
         }
     }
     int k = 0;
@@ -405,30 +481,35 @@ __global__ __launch_bounds__(kThreads) void residual_norm_bwd_kernel(ResidualNor
     if constexpr (NS > 4) flush(kSumPostB, to(a.dpost_b));
 }
 
-// out[j][g][c] = sum over k < n of part[j][g n + k][c], for the outputs asked
-// for: workgroup (c / 64, g, j), 64 columns by 16 slices of k.
+// The sums of segments and workgroups joined, in order: workgroup (c / 64, y)
+// adds, for job y, n rows of C that lie behind one another; 64 columns by 16
+// slices of the rows.  Jobs: for each sum over a group's rows and each group,
+// then for each sum over all rows.
 struct ReduceArgs {
-    const float *part;
-    float *out[4];
-    int32_t n, C;
+    const float *group_part, *row_part;
+    float *group_out[3], *row_out[4];
+    int32_t groups, group_jobs, group_n, row_n, C;
 };
 __global__ __launch_bounds__(1024) void residual_norm_reduce_kernel(ReduceArgs a)
 {
     __shared__ float lds[16][64];
     const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
-    const int64_t g = blockIdx.y, groups = gridDim.y;
-    const float *p = a.part + ((int64_t)blockIdx.z * groups + g) * a.n * a.C;
+    const int job = blockIdx.y, rj = job - a.group_jobs;
+    const bool grouped = rj < 0;
+    const int n = grouped ? a.group_n : a.row_n;
+    const float *p = grouped ? a.group_part + (int64_t)job * n * a.C : a.row_part + (int64_t)rj * n * a.C;
+    float *out = grouped ? a.group_out[job / a.groups] + (int64_t)(job % a.groups) * a.C : a.row_out[rj];
     float s = 0.f;
     if (c < a.C) {
 #pragma unroll 8
-        for (int k = slice; k < a.n; k += 16) s += p[(int64_t)k * a.C + c];
+        for (int k = slice; k < n; k += 16) s += p[(int64_t)k * a.C + c];
     }
     lds[slice][threadIdx.x & 63] = s;
     __syncthreads();
     if (slice != 0 || c >= a.C) return;
 #pragma unroll
     for (int k = 1; k < 16; ++k) s += lds[k][threadIdx.x & 63];
-    a.out[blockIdx.z][g * a.C + c] = s;
+    out[c] = s;
 }
 
 template <int NV, int WPR, bool F32>
@@ -440,16 +521,16 @@ hipError_t fwd_t(const ResidualNormArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-template <int NV, int WPR, bool F32>
+template <bool F32, bool WIDE>
 hipError_t bwd_t(const ResidualNormArgs &a, const ResidualNormPlan &p, float *gws, float *rws, hipStream_t stream)
 {
-    const dim3 grid((unsigned)p.blocks), block(kThreads);
+    const dim3 grid((unsigned)p.blocks), block(64 * p.row_waves * p.rows_at_once);
     if (a.post.kind == kNormNone)
-        hipLaunchKernelGGL((residual_norm_bwd_kernel<NV, WPR, F32, 3>), grid, block, 0, stream, a, p, gws, rws);
+        hipLaunchKernelGGL((residual_norm_bwd_kernel<F32, 3, WIDE>), grid, block, 0, stream, a, p, gws, rws);
     else if (a.dpost_b == nullptr)
-        hipLaunchKernelGGL((residual_norm_bwd_kernel<NV, WPR, F32, 4>), grid, block, 0, stream, a, p, gws, rws);
+        hipLaunchKernelGGL((residual_norm_bwd_kernel<F32, 4, WIDE>), grid, block, 0, stream, a, p, gws, rws);
     else
-        hipLaunchKernelGGL((residual_norm_bwd_kernel<NV, WPR, F32, 5>), grid, block, 0, stream, a, p, gws, rws);
+        hipLaunchKernelGGL((residual_norm_bwd_kernel<F32, 5, WIDE>), grid, block, 0, stream, a, p, gws, rws);
     return hipGetLastError();
 }
 
@@ -476,18 +557,6 @@ struct Fwd {
         return a.f32 ? fwd_t<NV, WPR, true>(a, s) : fwd_t<NV, WPR, false>(a, s);
     }
 };
-struct Bwd {
-    const ResidualNormArgs &a;
-    const ResidualNormPlan &p;
-    float *gws, *rws;
-    hipStream_t s;
-    template <int NV, int WPR>
-    hipError_t operator()() const
-    {
-        return a.f32 ? bwd_t<NV, WPR, true>(a, p, gws, rws, s) : bwd_t<NV, WPR, false>(a, p, gws, rws, s);
-    }
-};
-
 }  // namespace
 
 hipError_t launch_residual_norm_fwd(const ResidualNormArgs &a, hipStream_t stream)
@@ -499,9 +568,15 @@ ResidualNormPlan residual_norm_plan(int rows, int C, int group_rows, int n_cu)
 {
     ResidualNormPlan p{};
     p.groups = (rows + group_rows - 1) / group_rows;
-    const int at_once = C <= 2048 ? kWaves : 1;  // rows that a workgroup works on at a time
-    const int want = 2 * n_cu;
-    p.per_group = std::max(1, std::min((want + p.groups - 1) / p.groups, group_rows / (2 * at_once)));
+    p.row_waves = (C + 511) / 512;
+    p.rows_at_once = std::max(1, 4 / p.row_waves);
+    // Workgroups per compute unit: as many as its registers hold, for the more rows are under way the better memory
+    // latency passes, but each costs a row per sum in the workspace: a third one pays from 8 rows per workgroup on
+    // (10920 rows of 1536 channels: 106, 65 and 63 us with one, two and three; 1560 of 2048: 23, 18 and 20).  Never
+    // more workgroups than run at once: a second round costs as much as the first.
+    const int per_cu = p.row_waves > 4 ? 1 : p.row_waves <= 3 && rows >= 24 * n_cu ? 3 : 2;
+    const int want = per_cu * n_cu;
+    p.per_group = std::max(1, std::min(want / p.groups, group_rows / p.rows_at_once));
     p.blocks = (int)std::min<int64_t>(p.segments(), want);
     return p;
 }
@@ -514,27 +589,25 @@ int64_t residual_norm_workspace(const ResidualNormPlan &p, int C, int group_sums
 hipError_t launch_residual_norm_bwd(const ResidualNormArgs &a, int n_cu, hipStream_t stream)
 {
     const ResidualNormPlan p = residual_norm_plan(a.rows, a.C, a.group_rows, n_cu);
-    ReduceArgs group{}, all{};
+    ReduceArgs r{};
     int ng = 0, na = 0;
     const bool modulated = a.scale != nullptr;
     // in the kernel's order
     if (p.per_group > 1)
         for (float *o : {a.dgate, modulated ? a.dscale : nullptr, modulated ? a.dshift : nullptr})
-            if (o != nullptr) group.out[ng++] = o;
+            if (o != nullptr) r.group_out[ng++] = o;
     for (float *o : {modulated ? nullptr : a.dw, modulated ? nullptr : a.db, a.dpost_w, a.dpost_b})
-        if (o != nullptr) all.out[na++] = o;
+        if (o != nullptr) r.row_out[na++] = o;
     float *row_ws = a.ws + (int64_t)ng * p.segments() * a.C;
-    hipError_t e = by_width(a.C, Bwd{a, p, a.ws, row_ws, stream});
-    auto reduce = [&](ReduceArgs &r, const float *part, int n, int groups, int outs) {
-        if (e != hipSuccess || outs == 0) return;
-        r.part = part, r.n = n, r.C = a.C;
-        hipLaunchKernelGGL(residual_norm_reduce_kernel, dim3((unsigned)((a.C + 63) / 64), (unsigned)groups, (unsigned)outs),
-                           dim3(1024), 0, stream, r);
-        e = hipGetLastError();
-    };
-    reduce(group, a.ws, p.per_group, p.groups, ng);
-    reduce(all, row_ws, p.blocks, 1, na);
-    return e;
+    const bool wide = p.row_waves > 8;
+    const hipError_t e = a.f32 ? (wide ? bwd_t<true, true>(a, p, a.ws, row_ws, stream) : bwd_t<true, false>(a, p, a.ws, row_ws, stream))
+                               : (wide ? bwd_t<false, true>(a, p, a.ws, row_ws, stream) : bwd_t<false, false>(a, p, a.ws, row_ws, stream));
+    if (e != hipSuccess || ng + na == 0) return e;
+    r.group_part = a.ws, r.row_part = row_ws;
+    r.groups = p.groups, r.group_jobs = ng * p.groups, r.group_n = p.per_group, r.row_n = p.blocks, r.C = a.C;
+    hipLaunchKernelGGL(residual_norm_reduce_kernel, dim3((unsigned)((a.C + 63) / 64), (unsigned)(r.group_jobs + na)),
+                       dim3(1024), 0, stream, r);
+    return hipGetLastError();
 }
 
 }  // namespace regenvc

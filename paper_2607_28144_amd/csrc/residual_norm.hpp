@@ -50,6 +50,7 @@ hipError_t launch_residual_norm_fwd(const ResidualNormArgs &a, hipStream_t strea
 // (sums of all rows), which a second kernel adds in order.
 struct ResidualNormPlan {
     int32_t groups, per_group, blocks;
+    int32_t row_waves, rows_at_once;  // of a row, of a workgroup
     __host__ __device__ int64_t segments() const { return (int64_t)groups * per_group; }
 };
 ResidualNormPlan residual_norm_plan(int rows, int C, int group_rows, int n_cu);
