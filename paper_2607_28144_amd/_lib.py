@@ -215,36 +215,57 @@ _NOTHING = _Nothing()
 
 
 def on_device(device):
-    """Context with a torch device current (nothing to do where it is already)."""
+    """Context with a torch device (or the device of an index) current; nothing to do where it is already."""
     import torch
-    return _NOTHING if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    idx = device if isinstance(device, int) else device.index
+    return _NOTHING if torch.cuda.current_device() == idx else torch.cuda.device(device)
 
 
-def same_device(device, **tensors) -> None:
-    """Refuses tensors (None: not given) that lie elsewhere than on `device`."""
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+def index_of(t, name: str) -> int:
+    """The index of the device that a tensor lies on."""
+    idx = t.get_device()
+    if idx < 0:
+        raise ValueError(f"{name} must be a device tensor, got {t.device}")
+    return idx
 
 
-def device_index(device) -> int:
-    """The index of a torch device (the current one's where it has none)."""
-    import torch
-    idx = torch.device(device).index
-    return torch.cuda.current_device() if idx is None else idx
+def matrix(t, name: str, dtype, rows: int, cols: int, idx: int) -> int:
+    """The row stride of a [rows, cols] tensor of this type on device idx; refuses any other."""
+    s, st = t.shape, t.stride()
+    if t.dtype is dtype and t.get_device() == idx and len(st) == 2 and s[0] == rows and s[1] == cols \
+            and (st[1] == 1 or cols <= 1):
+        return st[0]
+    raise ValueError(f"{name} must be a {dtype} tensor [{rows}, {cols}] with unit column stride on cuda:{idx}, got "
+                     f"{t.dtype} {tuple(s)} on {t.device}")
+
+
+def vector(t, name: str, dtype, n: int, idx: int):
+    """The address of a contiguous tensor of n elements of this type on device idx (None for None); refuses any other."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == idx and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on cuda:{idx}, got {t.dtype} "
+                     f"{tuple(t.shape)} on {t.device}")
 
 
 _N_CU = {}  # device index -> compute units
 
 
-def compute_units(device) -> int:
-    """Compute units of a torch device."""
-    import torch
-    idx = device_index(device)
+def compute_units(idx: int) -> int:
+    """Compute units of the device of an index."""
     n = _N_CU.get(idx)
     if n is None:
+        import torch
         n = _N_CU[idx] = torch.cuda.get_device_properties(idx).multi_processor_count
     return n
+
+
+def raw_stream(idx: int) -> int:
+    """torch's current stream of the device of an index, as the address the C ABI takes."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(idx) if raw is not None else torch.cuda.current_stream(idx).cuda_stream
 
 
 def split_workspace(need: int, device):

@@ -128,33 +128,38 @@ def modulation(w_mod: torch.Tensor, b_mod: torch.Tensor, e: torch.Tensor,
 
 
 _NORM = {None: 0, "layer": 1, "rms": 2}
+_ACT = {torch.bfloat16: _lib.BF16, torch.float32: _lib.F32}
 
 
-def _norm(kind: Optional[str], eps: float, w, b, C: int, name: str) -> _lib.Norm:
-    if kind not in _NORM:
+def _norm(kind: Optional[str], eps: float, w, b, C: int, name: str, idx: int) -> _lib.Norm:
+    if kind not in _NORM or (kind is None and name == "norm"):
         raise ValueError(f"{name}={kind!r} ('layer', 'rms'" + (" or None)" if name == "post" else ")"))
-    return _lib.Norm(_NORM[kind], eps, _vec(w, f"{name} w", torch.bfloat16, C), _vec(b, f"{name} b", torch.bfloat16, C))
+    return _lib.Norm(_NORM[kind], eps, _lib.vector(w, f"{name} w", torch.bfloat16, C, idx) if w is not None else None,
+                     _lib.vector(b, f"{name} b", torch.bfloat16, C, idx) if b is not None else None)
 
 
-def _row_vectors(rows: int, C: int, group_rows: int, device, **vectors) -> _lib.RowVectors:
-    """gate, scale, shift: float32 [C] or [groups, C] with one row stride."""
-    groups = -(-rows // group_rows) if group_rows > 0 else 1
+def _row_vectors(groups: int, C: int, group_rows: int, idx: int, gate, scale, shift) -> _lib.RowVectors:
+    """gate, scale, shift (or None): float32 [C], or [groups, C] with one row stride."""
     ld = None
-    ptrs = {}
-    for name, t in vectors.items():
+    ptrs = []
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
         if t is None:
-            ptrs[name] = None
+            ptrs.append(None)
             continue
-        if t.device != device or t.dtype != torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != C \
-                or (C > 1 and t.stride(-1) != 1) or (t.dim() == 2 and t.shape[0] != groups and rows > 0) \
-                or (t.dim() == 1 and groups > 1):
-            raise ValueError(f"{name} must be float32 [{groups}, {C}] on {device} with unit column stride")
-        if t.dim() == 2 and groups > 1:
-            if ld is not None and t.stride(0) != ld:
+        if t.dim() == 1 and groups == 1:
+            ptrs.append(_lib.vector(t, name, torch.float32, C, idx))
+            continue
+        step = _lib.matrix(t, name, torch.float32, groups, C, idx)
+        if groups > 1:
+            if ld is not None and step != ld:
                 raise ValueError("gate, scale and shift must have one row stride")
-            ld = t.stride(0)
-        ptrs[name] = t.data_ptr()
-    return _lib.RowVectors(ptrs["gate"], ptrs["scale"], ptrs["shift"], C if ld is None else ld, group_rows)
+            ld = step
+        ptrs.append(t.data_ptr())
+    return _lib.RowVectors(ptrs[0], ptrs[1], ptrs[2], C if ld is None else ld, group_rows)
+
+
+def _groups(rows: int, group_rows: int) -> int:
+    return -(-rows // group_rows) if 0 < group_rows < rows else 1
 
 
 def residual_norm_fwd(x: torch.Tensor, y: torch.Tensor, norm: str = "layer", post: Optional[str] = None,
@@ -169,24 +174,27 @@ def residual_norm_fwd(x: torch.Tensor, y: torch.Tensor, norm: str = "layer", pos
     [rows, C]; y: bf16 or float32; post, norm: 'layer' or 'rms' (post may be
     None); gate, scale, shift: float32 [C], or [groups, C] with a set for every
     group_rows rows.  out may be x.  Returns (x', h), h in y's type."""
+    idx = _lib.index_of(x, "x")
     rows, C = x.shape
-    ldx = _rows(x, "x", torch.float32)
-    if y.dtype not in (torch.bfloat16, torch.float32) or tuple(y.shape) != (rows, C):
-        raise ValueError(f"y must be bfloat16 or float32 {(rows, C)}")
-    ldy = _rows(y, "y", y.dtype)
-    out = torch.empty((rows, C), dtype=torch.float32, device=x.device) if out is None else out
-    h = torch.empty((rows, C), dtype=y.dtype, device=x.device) if h is None else h
-    if tuple(out.shape) != (rows, C) or tuple(h.shape) != (rows, C):
-        raise ValueError(f"out and h must be {(rows, C)}")
-    ldo, ldh = _rows(out, "out", torch.float32), _rows(h, "h", y.dtype)
-    v = _row_vectors(rows, C, group_rows, x.device, gate=gate, scale=scale, shift=shift)
-    np, nq = _norm(post, eps, post_w, post_b, C, "post"), _norm(norm, eps, w, b, C, "norm")
-    _lib.same_device(x.device, y=y, out=out, h=h, w=w, b=b, post_w=post_w, post_b=post_b)
-    with _lib.on_device(x.device):
+    act = y.dtype
+    if act not in _ACT:
+        raise ValueError(f"y must be bfloat16 or float32, got {act}")
+    ldx, ldy = _lib.matrix(x, "x", torch.float32, rows, C, idx), _lib.matrix(y, "y", act, rows, C, idx)
+    dev = x.device
+    if out is None:
+        out, ldo = torch.empty(rows, C, dtype=torch.float32, device=dev), C
+    else:
+        ldo = _lib.matrix(out, "out", torch.float32, rows, C, idx)
+    if h is None:
+        h, ldh = torch.empty(rows, C, dtype=act, device=dev), C
+    else:
+        ldh = _lib.matrix(h, "h", act, rows, C, idx)
+    v = _row_vectors(_groups(rows, group_rows), C, group_rows, idx, gate, scale, shift)
+    np, nq = _norm(post, eps, post_w, post_b, C, "post", idx), _norm(norm, eps, w, b, C, "norm", idx)
+    with _lib.on_device(idx):
         st = _lib.load().regenvc_residual_norm_fwd(
-            x.data_ptr(), ldx, y.data_ptr(), ldy, _lib.F32 if y.dtype == torch.float32 else _lib.BF16, ctypes.byref(np),
-            ctypes.byref(nq), ctypes.byref(v), float(alpha), out.data_ptr(), ldo, h.data_ptr(), ldh, rows, C,
-            _stream(x.device))
+            x.data_ptr(), ldx, y.data_ptr(), ldy, _ACT[act], ctypes.byref(np), ctypes.byref(nq), ctypes.byref(v), alpha,
+            out.data_ptr(), ldo, h.data_ptr(), ldh, rows, C, _lib.raw_stream(idx))
     _lib.check(st, "regenvc_residual_norm_fwd")
     return out, h
 
@@ -204,6 +212,23 @@ class ResidualNormGrads(NamedTuple):
     dpost_b: Optional[torch.Tensor] = None
 
 
+_BWD_NEED = {}  # (device index, shape, sums) -> workspace bytes of a backward call
+
+
+def _bwd_need(rows: int, C: int, group_rows: int, group_sums: int, row_sums: int, idx: int) -> int:
+    key = (idx, rows, C, group_rows, group_sums, row_sums)
+    need = _BWD_NEED.get(key)
+    if need is None:
+        out = ctypes.c_int64()
+        st = _lib.load().regenvc_residual_norm_bwd_workspace(rows, C, group_rows, group_sums, row_sums,
+                                                             _lib.compute_units(idx), ctypes.byref(out))
+        need = out.value if st == _lib.OK else 0  # a shape the call itself refuses: let it say so
+        if len(_BWD_NEED) >= 4096:
+            _BWD_NEED.clear()
+        _BWD_NEED[key] = need
+    return need
+
+
 def residual_norm_bwd(x_out: torch.Tensor, y: torch.Tensor, gh: torch.Tensor, gx: Optional[torch.Tensor] = None,
                       norm: str = "layer", post: Optional[str] = None, gate: Optional[torch.Tensor] = None,
                       scale: Optional[torch.Tensor] = None, w: Optional[torch.Tensor] = None,
@@ -214,48 +239,49 @@ def residual_norm_bwd(x_out: torch.Tensor, y: torch.Tensor, gh: torch.Tensor, gx
     """Gradients of residual_norm_fwd (regenvc_residual_norm_bwd), given those
     of h (gh, in y's type) and of x' from the rest of the program (gx, float32,
     or None).  x_out: the forward call's x'.  dx may be gx.  The gradients of
-    the vectors are float32, shaped [groups, C] (gate, scale, shift) and [C]."""
+    the vectors are float32, [groups, C] (gate, scale, shift) and [C]; those of
+    one kind share an allocation."""
+    idx = _lib.index_of(x_out, "x_out")
     rows, C = x_out.shape
-    ldx = _rows(x_out, "x_out", torch.float32)
-    if y.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("y must be bfloat16 or float32")
+    act = y.dtype
+    if act not in _ACT:
+        raise ValueError(f"y must be bfloat16 or float32, got {act}")
+    ldx, ldy = _lib.matrix(x_out, "x_out", torch.float32, rows, C, idx), _lib.matrix(y, "y", act, rows, C, idx)
+    ldgh = _lib.matrix(gh, "gh", act, rows, C, idx)
+    ldgx = 0 if gx is None else _lib.matrix(gx, "gx", torch.float32, rows, C, idx)
     dev = x_out.device
-    dx = torch.empty((rows, C), dtype=torch.float32, device=dev) if dx is None else dx
-    dy = torch.empty((rows, C), dtype=y.dtype, device=dev) if dy is None else dy
-    for name, t in (("y", y), ("gh", gh), ("gx", gx), ("dx", dx), ("dy", dy)):
-        if t is not None and tuple(t.shape) != (rows, C):
-            raise ValueError(f"{name} must be {(rows, C)}")
-    ldy, ldgh, lddy = _rows(y, "y", y.dtype), _rows(gh, "gh", y.dtype), _rows(dy, "dy", y.dtype)
-    ldgx = 0 if gx is None else _rows(gx, "gx", torch.float32)
-    lddx = _rows(dx, "dx", torch.float32)
-    v = _row_vectors(rows, C, group_rows, dev, gate=gate, scale=scale, shift=None)
-    np, nq = _norm(post, eps, post_w, post_b, C, "post"), _norm(norm, eps, w, b, C, "norm")
-    _lib.same_device(dev, y=y, gh=gh, gx=gx, dx=dx, dy=dy, w=w, b=b, post_w=post_w, post_b=post_b)
-    groups = -(-rows // group_rows) if group_rows > 0 else 1
+    if dx is None:
+        dx, lddx = torch.empty(rows, C, dtype=torch.float32, device=dev), C
+    else:
+        lddx = _lib.matrix(dx, "dx", torch.float32, rows, C, idx)
+    if dy is None:
+        dy, lddy = torch.empty(rows, C, dtype=act, device=dev), C
+    else:
+        lddy = _lib.matrix(dy, "dy", act, rows, C, idx)
+    groups = _groups(rows, group_rows)
+    v = _row_vectors(groups, C, group_rows, idx, gate, scale, None)
+    np, nq = _norm(post, eps, post_w, post_b, C, "post", idx), _norm(norm, eps, w, b, C, "norm", idx)
 
-    def grad(of, *shape):
-        return None if of is None else torch.empty(shape, dtype=torch.float32, device=dev)
-    g = ResidualNormGrads(dx, dy, grad(gate, groups, C), grad(scale, groups, C), grad(scale, groups, C), grad(w, C),
-                          grad(b, C), grad(post_w, C), grad(post_b, C))
-    if rows == 0:  # sums over no rows
-        for t in g[2:]:
-            if t is not None:
-                t.zero_()
-        return g
-    grads = _lib.NormGrads(*[None if t is None else t.data_ptr() for t in g[2:]])
-    need = ctypes.c_int64()
-    _lib.check(_lib.load().regenvc_residual_norm_bwd_workspace(
-        rows, C, group_rows, sum(t is not None for t in g[2:5]), sum(t is not None for t in g[5:]),
-        _lib.compute_units(dev), ctypes.byref(need)), "regenvc_residual_norm_bwd_workspace")
-    with _lib.on_device(dev):
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value > 0 else None
-        st = _lib.load().regenvc_residual_norm_bwd(
-            x_out.data_ptr(), ldx, y.data_ptr(), ldy, _lib.F32 if y.dtype == torch.float32 else _lib.BF16,
-            ctypes.byref(np), ctypes.byref(nq), ctypes.byref(v), float(alpha), gh.data_ptr(), ldgh,
-            gx.data_ptr() if gx is not None else None, ldgx, dx.data_ptr(), lddx, dy.data_ptr(), lddy,
-            ctypes.byref(grads), rows, C, ws.data_ptr() if ws is not None else None, need.value, _stream(dev))
-    _lib.check(st, "regenvc_residual_norm_bwd")
-    return g
+    # what is asked for: of gate and modulation, of the weights
+    make = torch.empty if rows > 0 else torch.zeros  # (sums over no rows)
+    at = (gate is not None, scale is not None, scale is not None)
+    at_rows = (w is not None, b is not None, post_w is not None, post_b is not None)
+    ng, nr = sum(at), sum(at_rows)
+    grouped = iter(make(ng, groups, C, dtype=torch.float32, device=dev).unbind(0)) if ng else None
+    whole = iter(make(nr, C, dtype=torch.float32, device=dev).unbind(0)) if nr else None
+    vec = [next(grouped) if on else None for on in at] + [next(whole) if on else None for on in at_rows]
+    if rows > 0:
+        grads = _lib.NormGrads(*[None if t is None else t.data_ptr() for t in vec])
+        need = _bwd_need(rows, C, group_rows, ng, nr, idx)
+        with _lib.on_device(idx):
+            ws = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+            st = _lib.load().regenvc_residual_norm_bwd(
+                x_out.data_ptr(), ldx, y.data_ptr(), ldy, _ACT[act], ctypes.byref(np), ctypes.byref(nq), ctypes.byref(v),
+                alpha, gh.data_ptr(), ldgh, gx.data_ptr() if gx is not None else None, ldgx, dx.data_ptr(), lddx,
+                dy.data_ptr(), lddy, ctypes.byref(grads), rows, C, ws.data_ptr() if ws is not None else None, need,
+                _lib.raw_stream(idx))
+        _lib.check(st, "regenvc_residual_norm_bwd")
+    return ResidualNormGrads(dx, dy, *vec)
 
 
 class DitBlock:

@@ -16,10 +16,7 @@ import torch
 
 from . import _lib
 from .api import _DT, _desc, _fptr, _scale
-from .dit import EPI, _rows, _vec
-
-_stream = _lib.stream_of
-_same_device = _lib.same_device
+from .dit import EPI
 
 
 class MxTensor:
@@ -30,11 +27,9 @@ class MxTensor:
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
         nc, ns = mx_bytes(rows, cols)
-        for name, t, n in (("codes", codes, nc), ("scales", scales, ns)):
-            if t.device.type != "cuda" or t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != n:
-                raise ValueError(f"{name} of a [{rows}, {cols}] matrix must be a contiguous uint8 device tensor of {n} bytes")
-        if codes.device != scales.device:
-            raise ValueError("codes and scales must be on one device")
+        idx = _lib.index_of(codes, "codes")
+        _lib.vector(codes, "codes", torch.uint8, nc, idx)
+        _lib.vector(scales, "scales", torch.uint8, ns, idx)
         self.codes, self.scales, self.rows, self.cols = codes, scales, int(rows), int(cols)
 
     @property
@@ -62,18 +57,18 @@ def _float_dtype(t: torch.Tensor, name: str) -> int:
 def quantize(x: torch.Tensor, out: Optional[MxTensor] = None) -> MxTensor:
     """x (bf16 or float32 [rows, cols], unit column stride) in MXFP4 (regenvc_mx_quantize)."""
     dt = _float_dtype(x, "x")
-    ldx = _rows(x, "x", x.dtype)
+    idx = _lib.index_of(x, "x")
     rows, cols = x.shape
+    ldx = _lib.matrix(x, "x", x.dtype, rows, cols, idx)
     if out is None:
         nc, ns = mx_bytes(rows, cols)
         out = MxTensor(torch.empty(nc, dtype=torch.uint8, device=x.device),
                        torch.empty(ns, dtype=torch.uint8, device=x.device), rows, cols)
-    elif out.shape != (rows, cols):
-        raise ValueError(f"out is {out.shape}, x {tuple(x.shape)}")
-    _same_device(x.device, out=out.codes)
-    with _lib.on_device(x.device):
+    elif out.shape != (rows, cols) or out.codes.get_device() != idx:
+        raise ValueError(f"out is {out.shape} on {out.device}, x {tuple(x.shape)} on {x.device}")
+    with _lib.on_device(idx):
         st = _lib.load().regenvc_mx_quantize(x.data_ptr(), dt, ldx, out.codes.data_ptr(), out.scales.data_ptr(), rows,
-                                             cols, _stream(x.device))
+                                             cols, _lib.raw_stream(idx))
     _lib.check(st, "regenvc_mx_quantize")
     return out
 
@@ -82,14 +77,12 @@ def dequantize(m: MxTensor, dtype: torch.dtype = torch.float32, out: Optional[to
     """The values of an MXFP4 matrix as float32 or bf16 (regenvc_mx_dequantize)."""
     if out is None:
         out = torch.empty(m.shape, dtype=dtype, device=m.device)
-    if tuple(out.shape) != m.shape:
-        raise ValueError(f"out is {tuple(out.shape)}, the matrix {m.shape}")
     dt = _float_dtype(out, "out")
-    ldo = _rows(out, "out", out.dtype)
-    _same_device(m.device, out=out)
-    with _lib.on_device(m.device):
+    idx = m.codes.get_device()
+    ldo = _lib.matrix(out, "out", out.dtype, m.rows, m.cols, idx)
+    with _lib.on_device(idx):
         st = _lib.load().regenvc_mx_dequantize(m.codes.data_ptr(), m.scales.data_ptr(), out.data_ptr(), dt, ldo, m.rows,
-                                               m.cols, _stream(m.device))
+                                               m.cols, _lib.raw_stream(idx))
     _lib.check(st, "regenvc_mx_dequantize")
     return out
 
@@ -97,14 +90,14 @@ def dequantize(m: MxTensor, dtype: torch.dtype = torch.float32, out: Optional[to
 _NEED = {}  # (device index, shape, epilogue, quantized) -> least and total workspace bytes of a linear layer
 
 
-def linear_workspace_bytes(M: int, N: int, K: int, epilogue: str, quantized: bool, device) -> Tuple[int, int]:
-    """Workspace bytes that a linear layer must have and can use (regenvc_mx_linear_workspace)."""
-    idx = _lib.device_index(device)
+def linear_workspace_bytes(M: int, N: int, K: int, epilogue: str, quantized: bool, idx: int) -> Tuple[int, int]:
+    """Workspace bytes that a linear layer must have and can use on the device
+    of an index (regenvc_mx_linear_workspace)."""
     key = (idx, M, N, K, epilogue, quantized)
     need = _NEED.get(key)
     if need is None:
         least, total = ctypes.c_int64(), ctypes.c_int64()
-        st = _lib.load().regenvc_mx_linear_workspace(M, N, K, EPI[epilogue], int(quantized), _lib.compute_units(device),
+        st = _lib.load().regenvc_mx_linear_workspace(M, N, K, EPI[epilogue], int(quantized), _lib.compute_units(idx),
                                                      ctypes.byref(least), ctypes.byref(total))
         # a shape the call itself refuses: let it say so
         need = (least.value, total.value) if st == _lib.OK else (0, 0)
@@ -125,37 +118,36 @@ def linear_fwd(a: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[tor
     if w.cols != K:
         raise ValueError(f"w is {w.shape}, a {tuple(a.shape)}")
     quantized = isinstance(a, MxTensor)
-    lda = 0 if quantized else _rows(a, "a", torch.bfloat16)
+    idx = w.codes.get_device()
+    if quantized:
+        ac = a.codes
+        if ac.get_device() != idx:
+            raise ValueError(f"a is on {a.device}, w on {w.device}")
+        a_ptr, lda, c_ptr, s_ptr = None, 0, ac.data_ptr(), a.scales.data_ptr()
+    else:
+        lda = _lib.matrix(a, "a", torch.bfloat16, M, K, idx)
+        a_ptr, c_ptr, s_ptr = a.data_ptr(), None, None
     epi = EPI[epilogue]
-    if out is None:
-        if epi == 2:
-            raise ValueError("the gated-residual epilogue needs out (the float32 residual stream)")
-        out = torch.empty((M, N), dtype=torch.bfloat16, device=a.device)
-    elif tuple(out.shape) != (M, N):
-        raise ValueError(f"out is {tuple(out.shape)}, y {(M, N)}")
-    ldo = _rows(out, "out", torch.float32 if epi == 2 else torch.bfloat16)
-    bp, gp = _vec(bias, "bias", torch.bfloat16, N), _vec(gate, "gate", torch.float32, N)
-    _same_device(a.device, w=w.codes, bias=bias, gate=gate, out=out)
-    least, total = linear_workspace_bytes(M, N, K, epilogue, quantized, a.device)
-    with _lib.on_device(a.device):
-        ws = _lib.split_workspace(total, a.device)
-        if ws is None and least > 0:  # without the partial sums of a split of K
-            ws = torch.empty(least, dtype=torch.uint8, device=a.device)
+    if out is not None:
+        ldo = _lib.matrix(out, "out", torch.float32 if epi == 2 else torch.bfloat16, M, N, idx)
+    elif epi == 2:
+        raise ValueError("the gated-residual epilogue needs out (the float32 residual stream)")
+    else:
+        out, ldo = torch.empty(M, N, dtype=torch.bfloat16, device=a.device), N
+    bp = _lib.vector(bias, "bias", torch.bfloat16, N, idx)
+    gp = _lib.vector(gate, "gate", torch.float32, N, idx)
+    least, total = linear_workspace_bytes(M, N, K, epilogue, quantized, idx)
+    with _lib.on_device(idx):
+        ws = None
+        if total > 0:
+            ws = _lib.split_workspace(total, a.device)
+            if ws is None and least > 0:  # without the partial sums of a split of K
+                ws = torch.empty(least, dtype=torch.uint8, device=a.device)
         st = _lib.load().regenvc_mx_linear_fwd(
-            None if quantized else a.data_ptr(), lda, a.codes.data_ptr() if quantized else None,
-            a.scales.data_ptr() if quantized else None, w.codes.data_ptr(), w.scales.data_ptr(), bp, gp, out.data_ptr(),
-            ldo, M, N, K, epi, ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0,
-            _stream(a.device))
+            a_ptr, lda, c_ptr, s_ptr, w.codes.data_ptr(), w.scales.data_ptr(), bp, gp, out.data_ptr(), ldo, M, N, K, epi,
+            ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, _lib.raw_stream(idx))
     _lib.check(st, "regenvc_mx_linear_fwd")
     return out
-
-
-def _ints(t: Optional[torch.Tensor], name: str, n: int, device: torch.device) -> Optional[int]:
-    if t is None:
-        return None
-    if t.device != device or t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != (n,):
-        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements on {device}")
-    return t.data_ptr()
 
 
 class KvCache:
@@ -176,38 +168,39 @@ class KvCache:
         self.k_codes, self.v_codes = (torch.zeros(*shape, D // 2, dtype=torch.uint8, device=self.device) for _ in range(2))
         self.k_scales, self.v_scales = (torch.zeros(*shape, D // 32, dtype=torch.uint8, device=self.device)
                                         for _ in range(2))
-
-    def _c(self) -> _lib.MxCache:
-        return _lib.MxCache(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
-                            self.v_scales.data_ptr(), self.batch, self.capacity, self.heads, self.D)
+        self._c = _lib.MxCache(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
+                               self.v_scales.data_ptr(), self.batch, self.capacity, self.heads, self.D)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
                count: Optional[torch.Tensor] = None) -> None:
         """Tokens k, v (bf16 [batch, S, heads, D]) to places (start[b] + i) mod
         capacity, the first count[b] of each sequence (int32 device tensors;
         default 0 and S) (regenvc_mx_cache_append)."""
+        if k.dim() != 4 or v.shape != k.shape or k.shape[0] != self.batch or k.shape[2] != self.heads \
+                or k.shape[3] != self.D:
+            raise ValueError(f"k, v must be [{self.batch}, S, {self.heads}, {self.D}], got {tuple(k.shape)}, {tuple(v.shape)}")
         S = k.shape[1]
-        want = (self.batch, S, self.heads, self.D)
-        if tuple(k.shape) != want or tuple(v.shape) != want:
-            raise ValueError(f"k, v must be {list(want)}, got {tuple(k.shape)}, {tuple(v.shape)}")
+        idx = self.device.index
         kd, vd = _desc(k, "k", torch.bfloat16), _desc(v, "v", torch.bfloat16)
-        _same_device(self.device, k=k, v=v)
-        sp, cp = _ints(start, "start", self.batch, self.device), _ints(count, "count", self.batch, self.device)
-        c = self._c()
-        with _lib.on_device(self.device):
-            st = _lib.load().regenvc_mx_cache_append(ctypes.byref(c), ctypes.byref(kd), ctypes.byref(vd), S, sp, cp,
-                                                     _stream(self.device))
+        if k.get_device() != idx or v.get_device() != idx:
+            raise ValueError(f"k and v must be on {self.device}, got {k.device}, {v.device}")
+        sp = _lib.vector(start, "start", torch.int32, self.batch, idx)
+        cp = _lib.vector(count, "count", torch.int32, self.batch, idx)
+        with _lib.on_device(idx):
+            st = _lib.load().regenvc_mx_cache_append(ctypes.byref(self._c), ctypes.byref(kd), ctypes.byref(vd), S, sp, cp,
+                                                     _lib.raw_stream(idx))
         _lib.check(st, "regenvc_mx_cache_append")
 
     def values(self, dtype: torch.dtype = torch.float32) -> Tuple[torch.Tensor, torch.Tensor]:
         """The cache's keys and values as float32 or bf16 [batch, capacity,
         heads, D] (regenvc_mx_cache_values)."""
-        k, v = (torch.empty((self.batch, self.capacity, self.heads, self.D), dtype=dtype, device=self.device)
+        k, v = (torch.empty(self.batch, self.capacity, self.heads, self.D, dtype=dtype, device=self.device)
                 for _ in range(2))
         dt = _float_dtype(k, "dtype")
-        c = self._c()
-        with _lib.on_device(self.device):
-            st = _lib.load().regenvc_mx_cache_values(ctypes.byref(c), k.data_ptr(), v.data_ptr(), dt, _stream(self.device))
+        idx = self.device.index
+        with _lib.on_device(idx):
+            st = _lib.load().regenvc_mx_cache_values(ctypes.byref(self._c), k.data_ptr(), v.data_ptr(), dt,
+                                                     _lib.raw_stream(idx))
         _lib.check(st, "regenvc_mx_cache_values")
         return k, v
 
@@ -215,12 +208,13 @@ class KvCache:
 _ATTN_NEED = {}  # (device index, shape) -> workspace bytes of a call
 
 
-def _attn_need(B: int, H: int, heads: int, Sq: int, max_len: int, D: int, device: torch.device) -> int:
-    key = (device.index, B, H, heads, Sq, max_len, D)
+def _attn_need(B: int, H: int, heads: int, Sq: int, max_len: int, D: int, idx: int) -> int:
+    key = (idx, B, H, heads, Sq, max_len, D)
     need = _ATTN_NEED.get(key)
     if need is None:
         out = ctypes.c_int64()
-        st = _lib.load().regenvc_mx_attn_cache_workspace(B, H, heads, Sq, max_len, D, _lib.compute_units(device), ctypes.byref(out))
+        st = _lib.load().regenvc_mx_attn_cache_workspace(B, H, heads, Sq, max_len, D, _lib.compute_units(idx),
+                                                         ctypes.byref(out))
         need = out.value if st == _lib.OK else 0  # a shape the call itself refuses: let it say so
         if len(_ATTN_NEED) >= 4096:
             _ATTN_NEED.clear()
@@ -242,25 +236,35 @@ def attn_cache_fwd(q: torch.Tensor, cache: KvCache, lens: Optional[torch.Tensor]
     B, Sq, H, D = q.shape
     if B != cache.batch or D != cache.D:
         raise ValueError(f"q is {tuple(q.shape)}, the cache holds {cache.batch} sequences of D={cache.D}")
-    if out is None:
-        out = torch.empty((B, Sq, H, D), dtype=out_dtype, device=q.device)
-    elif tuple(out.shape) != (B, Sq, H, D):
-        raise ValueError(f"out is {tuple(out.shape)}, q {tuple(q.shape)}")
-    if lse_out is None and return_lse:
-        lse_out = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device)
     if out_dtype not in _DT:
         raise TypeError(f"out_dtype must be bfloat16 or float32, got {out_dtype}")
-    qd, od = _desc(q, "q", torch.bfloat16), _desc(out, "out", out_dtype)
-    lp = _fptr(lse_out, "lse", (B, H, Sq))
-    _same_device(cache.device, q=q, out=out, lse_out=lse_out)
-    np = _ints(lens, "lens", B, cache.device)
+    idx, dev = cache.device.index, cache.device
+    if out is None:
+        out = torch.empty(B, Sq, H, D, dtype=out_dtype, device=dev)
+        od = _lib.Tensor(out.data_ptr(), Sq * H * D, H * D, D)
+    elif tuple(out.shape) != (B, Sq, H, D) or out.get_device() != idx:
+        raise ValueError(f"out must be {(B, Sq, H, D)} on {dev}, got {tuple(out.shape)} on {out.device}")
+    else:
+        od = _desc(out, "out", out_dtype)
+    qd = _desc(q, "q", torch.bfloat16)
+    if q.get_device() != idx:
+        raise ValueError(f"q is on {q.device}, the cache on {dev}")
+    if lse_out is not None:
+        lp = _fptr(lse_out, "lse", (B, H, Sq))
+        if lse_out.get_device() != idx:
+            raise ValueError(f"lse is on {lse_out.device}, the cache on {dev}")
+    elif return_lse:
+        lse_out = torch.empty(B, H, Sq, dtype=torch.float32, device=dev)
+        lp = lse_out.data_ptr()
+    else:
+        lp = None
+    np = _lib.vector(lens, "lens", torch.int32, B, idx)
     n = cache.capacity if max_len is None else int(max_len)
-    need = _attn_need(B, H, cache.heads, Sq, n, D, cache.device)
-    c = cache._c()
-    with _lib.on_device(cache.device):
-        ws = torch.empty(need, dtype=torch.uint8, device=cache.device) if need > 0 else None
+    need = _attn_need(B, H, cache.heads, Sq, n, D, idx)
+    with _lib.on_device(idx):
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
         st = _lib.load().regenvc_mx_attn_cache_fwd(
-            ctypes.byref(qd), ctypes.byref(c), np, n, ctypes.byref(od), _DT[out_dtype], lp, B, H, Sq, _scale(scale, D),
-            ws.data_ptr() if ws is not None else None, need, _stream(cache.device))
+            ctypes.byref(qd), ctypes.byref(cache._c), np, n, ctypes.byref(od), _DT[out_dtype], lp, B, H, Sq,
+            _scale(scale, D), ws.data_ptr() if ws is not None else None, need, _lib.raw_stream(idx))
     _lib.check(st, "regenvc_mx_attn_cache_fwd")
     return out, lse_out
