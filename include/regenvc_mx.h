@@ -60,25 +60,21 @@ regenvc_status regenvc_mx_dequantize(const void *codes, const void *scales, void
      w_codes, w_scales: [N, K] in MXFP4
      bias, gate, out, ldo, epilogue: as regenvc_linear_fwd
    M, N, K >= 0; K a multiple of 8, at most 2^20; N a multiple of 16; pointers
-   16-byte aligned.  workspace: 256-byte aligned, at least `least` bytes of
-   regenvc_mx_linear_workspace (a's codes and scales); with more, up to
-   `total`, K may be cut into ranges whose f32 partial sums a second kernel
-   adds in order.  The kernel and the number of ranges depend on the sizes, the
-   compute units and the workspace, and with them the order of the fp32 sum. */
+   16-byte aligned.  workspace: 256-byte aligned, at least
+   regenvc_mx_linear_workspace bytes (a's codes and scales; NULL if that is 0).
+   The kernel, chosen by size, sets the order of the fp32 sum: a row may come
+   out a rounding apart in calls of different numbers of rows. */
 regenvc_status regenvc_mx_linear_fwd(const void *a, int64_t lda, const void *a_codes, const void *a_scales,
                                      const void *w_codes, const void *w_scales, const void *bias, const float *gate,
                                      void *out, int64_t ldo, int32_t M, int32_t N, int32_t K, int32_t epilogue,
                                      void *workspace, int64_t workspace_bytes, void *stream);
 
-/* Workspace bytes of such a call: `least` it must have and `total` it can
-   use; `quantized`: a is in MXFP4 already.  Host-only. */
-regenvc_status regenvc_mx_linear_workspace(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t quantized,
-                                           int32_t n_cu, int64_t *least, int64_t *total);
+/* Workspace bytes of such a call; `quantized`: a is in MXFP4 already.  Host-only. */
+regenvc_status regenvc_mx_linear_workspace(int32_t M, int32_t N, int32_t K, int32_t quantized, int64_t *bytes);
 
-/* The decomposition of such a call with workspace_bytes left for partial sums
-   (INT64_MAX: as many as it can use).  Host-only. */
+/* The decomposition of such a call (k_ranges is 1).  Host-only. */
 regenvc_status regenvc_mx_linear_plan_query(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t n_cu,
-                                            int64_t workspace_bytes, regenvc_tile_plan *plan);
+                                            regenvc_tile_plan *plan);
 
 /* A key/value cache of B sequences of `heads` key heads and `capacity` places,
    in caller memory: codes [B, heads, capacity, D / 2] (channel 2 i of a place

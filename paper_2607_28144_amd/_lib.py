@@ -154,8 +154,8 @@ _SIGNATURES = {
     "regenvc_mx_quantize": [_p, ctypes.c_int, _i64, _p, _p, _i32, _i32, _p],
     "regenvc_mx_dequantize": [_p, _p, _p, ctypes.c_int, _i64, _i32, _i32, _p],
     "regenvc_mx_linear_fwd": [_p, _i64, _p, _p, _p, _p, _p, _p, _p, _i64, _i32, _i32, _i32, _i32, _p, _i64, _p],
-    "regenvc_mx_linear_workspace": [_i32, _i32, _i32, _i32, _i32, _i32, _PI64, _PI64],
-    "regenvc_mx_linear_plan_query": [_i32, _i32, _i32, _i32, _i32, _i64, ctypes.POINTER(TilePlan)],
+    "regenvc_mx_linear_workspace": [_i32, _i32, _i32, _i32, _PI64],
+    "regenvc_mx_linear_plan_query": [_i32, _i32, _i32, _i32, _i32, ctypes.POINTER(TilePlan)],
     "regenvc_mx_cache_append": [_PC, _PT, _PT, _i32, _p, _p, _p],
     "regenvc_mx_cache_values": [_PC, _p, _p, ctypes.c_int, _p],
     "regenvc_mx_attn_cache_fwd": [_PT, _PC, _p, _i32, _PT, ctypes.c_int, _p, _i32, _i32, _i32, ctypes.c_float, _p, _i64,

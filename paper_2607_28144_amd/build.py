@@ -21,7 +21,7 @@ ARCH = "gfx950"
 # MFMA results in VGPRs: the score tiles feed VALU softmax code directly, and
 # read-only operands may then live in AGPRs.  Not for the tile kernels of the
 # linear layers, whose accumulators fill the AGPRs.
-VGPR_FORM = {"attn_fwd.hip"}
+VGPR_FORM = {"attn_fwd.hip", "mx.hip", "mx_attn.hip"}
 # Sources with tiles whose MFMAs are instructions of their own (inline
 # assembly, around which the compiler places no wait states): their assembly is
 # checked (check_tile_kernels).

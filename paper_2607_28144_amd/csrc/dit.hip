@@ -326,7 +326,12 @@ hipError_t launch_linear4(const LinearArgs &a, int splits, hipStream_t stream)
         if (splits > 1) {
             const hipError_t e = launch_linear4_t<S, tile::kPartial, false>(a, splits, stream);
             if (e != hipSuccess) return e;
-            return launch_linear_reduce(a, splits, stream);
+            switch (a.epi) {
+            case kEpiBias: return launch_reduce_t<kEpiBias>(a, splits, stream);
+            case kEpiBiasGelu: return launch_reduce_t<kEpiBiasGelu>(a, splits, stream);
+            case kEpiGatedRes: return launch_reduce_t<kEpiGatedRes>(a, splits, stream);
+            }
+            return hipErrorInvalidValue;
         }
     }
     switch (a.epi) {
@@ -396,16 +401,6 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t stream)
     case kTile64x128: return launch_linear4<Tile64x128>(a, p.splits, stream);
     case kTile288x256: return launch_linear_bm<288>(a, stream);
     case kTile256x256By8: return launch_linear_bm<256>(a, stream);
-    }
-    return hipErrorInvalidValue;
-}
-
-hipError_t launch_linear_reduce(const LinearArgs &a, int splits, hipStream_t stream)
-{
-    switch (a.epi) {
-    case kEpiBias: return launch_reduce_t<kEpiBias>(a, splits, stream);
-    case kEpiBiasGelu: return launch_reduce_t<kEpiBiasGelu>(a, splits, stream);
-    case kEpiGatedRes: return launch_reduce_t<kEpiGatedRes>(a, splits, stream);
     }
     return hipErrorInvalidValue;
 }

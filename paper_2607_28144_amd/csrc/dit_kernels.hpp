@@ -50,8 +50,6 @@ TilePlan linear_plan(int M, int N, int K, int epi, int n_cu, int64_t ws_bytes);
 // Workspace bytes that give a linear launch its full split (0: it does not split).
 size_t linear_workspace_bytes(int M, int N, int K, int epi, int n_cu);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t stream);
-// out = epilogue(sum of the `splits` f32 planes [M, N] at a.ws + bias): the second kernel of a split of K.
-hipError_t launch_linear_reduce(const LinearArgs &a, int splits, hipStream_t stream);
 
 // Row normalization of x (f32 [rows, C], row stride ldx) into bf16 y (row
 // stride ldy): LN(x) (1 + scale) + shift with f32 shift/scale [C]

@@ -139,14 +139,14 @@ __device__ __forceinline__ uint32_t quantize_block(const uint16_t *row, int c, i
 // Up to 16 MB rows: the weights are read once and bound the time, and there
 // is little of everything, so a workgroup takes 16 output channels and all
 // rows, its W waves taking the steps of K in turn; their sums meet in LDS.
-// QUANT: a is bf16 and each workgroup brings its rows to MXFP4 itself (in
-// registers), which saves a launch.
+// QUANT: a is bf16 and each workgroup brings its rows to MXFP4 itself, in
+// registers.  blockIdx.y: tile of 16 MB rows.
 template <int MB, int W, int EPI, bool QUANT>
 __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int nk)
 {
     __shared__ f32x4 red[W][MB * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, x = lane & 15;
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MB;
     const uint8_t *wc = a.w_codes + (int64_t)(n0 + x) * nk * kStepBytes + g * 32;
     const uint8_t *wsc = a.w_scales + (int64_t)blockIdx.x * nk * 128 + lane * 2;
     f32x4 acc[MB];
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
         const uint32_t ws = *reinterpret_cast<const uint16_t *>(wsc + (int64_t)kt * 128);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            const int64_t row = min(mb * 16 + x, a.M - 1);
+            const int64_t row = min(m0 + mb * 16 + x, a.M - 1);
             u32x4 f[2];
             uint32_t as;
             if constexpr (QUANT) {
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
                 const uint8_t *p = a.a_codes + (row * nk + kt) * kStepBytes + g * 32;
                 f[0] = *reinterpret_cast<const u32x4 *>(p);
                 f[1] = *reinterpret_cast<const u32x4 *>(p + 16);
-                as = *reinterpret_cast<const uint16_t *>(a.a_scales + ((int64_t)min(mb, (a.M - 1) >> 4) * nk + kt) * 128 +
+                as = *reinterpret_cast<const uint16_t *>(a.a_scales + ((int64_t)min((m0 >> 4) + mb, (a.M - 1) >> 4) * nk + kt) * 128 +
                                                          lane * 2);
             }
 #pragma unroll
@@ -184,7 +184,8 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
         f32x4 y = red[0][t];
 #pragma unroll
         for (int k = 1; k < W; ++k) y += red[k][t];
-        const int m = (t >> 6) * 16 + (t & 15), n = n0 + 4 * ((t & 63) >> 4);
+        const int64_t m = m0 + (t >> 6) * 16 + (t & 15);
+        const int n = n0 + 4 * ((t & 63) >> 4);
         if (m >= a.M) continue;
         y += tile::load_bias4(static_cast<const uint16_t *>(a.bias), n);
         if constexpr (EPI == kEpiGatedRes) {
@@ -202,79 +203,185 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
 }
 
 // ---------------------------------------------------------------- tiles
-// Four waves per tile of (32 MB) rows x (32 NB) channels, WPE workgroups per
-// compute unit, two LDS stages of codes and of scale lines.
-template <int MB_, int NB_, int WPE_>
+// Four waves per tile of (32 MB) rows x (32 NB) channels, each with a quarter
+// of it, WPE workgroups per compute unit.  A workgroup walks tiles (or K ranges
+// of tiles) blockIdx.x, blockIdx.x + gridDim.x, ...: the steps of all of them
+// form one stream through an LDS ring of ST stages of codes and scale lines,
+// so that the next tile's first steps land while this one's last are
+// multiplied and its output is stored.
+//
+// Per 128 x 128 tile and step: 512 cycles of matrix instructions per SIMD, and
+// 1024 of LDS (34 KB of copies at 64 bytes a cycle, 64 KB of fragment reads at
+// 128), which bounds it.
+template <int MB_, int NB_, int WPE_, int ST_>
 struct Shape {
-    static constexpr int MB = MB_, NB = NB_, WPE = WPE_;
+    static constexpr int MB = MB_, NB = NB_, WPE = WPE_, ST = ST_;
     static constexpr int BM = 32 * MB, BN = 32 * NB;
     static constexpr int A_BYTES = BM * kStepBytes, W_BYTES = BN * kStepBytes;
     static constexpr int S_CHUNKS = 8 * 2 * (MB + NB);  // 16-byte chunks of a step's scale lines, A's first
     static constexpr int S_COPIES = (S_CHUNKS + 63) / 64;
     static constexpr int S_BYTES = S_COPIES * 1024;
-    static constexpr int RINGS = 2 * (A_BYTES + W_BYTES + S_BYTES);
-    static constexpr int LDS = RINGS > BM * BN * 2 ? RINGS : BM * BN * 2;  // the output is staged there too
-    static_assert(LDS * WPE <= 160 * 1024 && S_COPIES <= 4, "tile shape");
+    static constexpr int OUT = ST * (A_BYTES + W_BYTES + S_BYTES);  // where 16 rows of each wave's output are staged
+    static constexpr int OUT_ROW = 16 * NB * 2;
+    static constexpr bool STAGED = NB == 4 && (OUT + 4 * 16 * OUT_ROW) * WPE <= 160 * 1024;  // else stored straight
+    static constexpr int LDS = OUT + (STAGED ? 4 * 16 * OUT_ROW : 0);
+    static_assert(LDS * WPE <= 160 * 1024 && S_COPIES <= 4 && (!STAGED || NB == 4), "tile shape");
 };
 
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) uint16_t lds_u16;
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
-// The K loop over steps [k0, k1): acc[nb][mb][i] as in tile::mma4.  A step's
-// second half (ks = 1) is read beside the MFMAs of its first, the next step's
-// first half beside those of its second; copies run two steps ahead.
-template <class S>
-__device__ __forceinline__ void mma_mx(const tile::Dense<false> &as, const tile::Dense<false> &ws, const uint8_t *a_sc,
-                                       const uint8_t *w_sc, int nk, int k0, int k1, char *smem,
-                                       f32x4 (&acc)[S::NB][S::MB])
+// A pointer that is the same in every lane, in scalar registers.
+__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
 {
-    constexpr int MB = S::MB, NB = S::NB, NM = MB * NB, NF = MB + NB;
-    constexpr int AP = S::A_BYTES / 4096, WP = S::W_BYTES / 4096;  // copies per wave and step, and one of scales
-    constexpr uint32_t W0 = 2 * S::A_BYTES, S0 = W0 + 2 * S::W_BYTES;
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return reinterpret_cast<const uint8_t *>((uint64_t)hi << 32 | lo);
+}
+
+// The tiles of a launch, and the rows and channels that one begins at.
+struct Tiles {
+    int nk, tiles_n, n_tiles;
+};
+struct Item {
+    int m0, n0;
+};
+template <class S>
+__device__ __forceinline__ Item item_of(const Tiles &t, int id)
+{
+    int tm, tn;
+    tile::tile_of(id, t.tiles_n, t.n_tiles, tm, tn);
+    return Item{tm * S::BM, tn * S::BN};
+}
+
+// 16 rows of a wave's 64 channels at a time through its own LDS, so that each
+// store writes whole 16-byte chunks, 128 bytes of a row; f32 outputs (64 bytes
+// of a row per 16 channels) go straight from the accumulators.
+template <class S, int EPI>
+__device__ __forceinline__ void store_tile(const LinearArgs &a, const Item &it, char *smem, f32x4 (&acc)[S::NB][S::MB])
+{
+    constexpr int MB = S::MB, NB = S::NB;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, g = lane >> 4, x = lane & 15;
-
-    tile::Dense<false>::Row arow[AP], wrow[WP];
+    const int m0 = it.m0 + wm * 16 * MB, n0 = it.n0 + wn * 16 * NB;
+    const uint16_t *bias = static_cast<const uint16_t *>(a.bias);
+    f32x4 bv[NB];
 #pragma unroll
-    for (int i = 0; i < AP; ++i) {
-        const int r = (wave * AP + i) * 8 + (lane >> 3);
-        arow[i] = as.row(r, tile::swz(r, lane & 7));
-    }
+    for (int nb = 0; nb < NB; ++nb)
+        bv[nb] = n0 + nb * 16 < a.N ? tile::load_bias4(bias, n0 + nb * 16 + 4 * g) : f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (EPI == kEpiGatedRes || !S::STAGED) {
 #pragma unroll
-    for (int i = 0; i < WP; ++i) {
-        const int r = (wave * WP + i) * 8 + (lane >> 3);
-        wrow[i] = ws.row(r, tile::swz(r, lane & 7));
+        for (int nb = 0; nb < NB; ++nb) {
+            const int n = n0 + nb * 16 + 4 * g;
+            if (n0 + nb * 16 >= a.N) continue;
+            f32x4 gv = {1.f, 1.f, 1.f, 1.f};
+            if (EPI == kEpiGatedRes && a.gate != nullptr) gv = *reinterpret_cast<const f32x4 *>(a.gate + n);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                const int m = m0 + mb * 16 + x;
+                if (m >= a.M) continue;
+                if constexpr (EPI == kEpiGatedRes) {
+                    f32x4 *p = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + (int64_t)m * a.ldo + n);
+                    *p = *p + gv * (acc[nb][mb] + bv[nb]);
+                } else {
+                    const f32x4 y = acc[nb][mb] + bv[nb];
+                    bf16x4 w;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = (__bf16)tile::activate<EPI>(y[i]);
+                    *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.out) + (int64_t)m * a.ldo + n) = w;
+                }
+            }
+        }
+    } else {
+        tile::lds_char *stg = (tile::lds_char *)smem + S::OUT + wave * 16 * S::OUT_ROW;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const f32x4 y = acc[nb][mb] + bv[nb];
+                bf16x4 w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = (__bf16)tile::activate<EPI>(y[i]);
+                *(lds_bf16x4 *)(stg + x * S::OUT_ROW + ((nb * 2 + g / 2) ^ (x & 7)) * 16 + (g & 1) * 8) = w;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = j * 8 + (lane >> 3), c = lane & 7;
+                const u32x4 v = *(const lds_u32x4 *)(stg + r * S::OUT_ROW + (c ^ (r & 7)) * 16);
+                const int m = m0 + mb * 16 + r, n = n0 + c * 8;
+                if (m < a.M && n < a.N)
+                    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + (int64_t)m * a.ldo + n) = v;
+            }
+        }
     }
-    // this wave's copy of scale lines (waves past the number of copies repeat one)
-    const int scopy = wave % S::S_COPIES, chunk = min(scopy * 64 + lane, S::S_CHUNKS - 1), line = chunk >> 3;
-    const int64_t rb = line < 2 * MB ? min((as.r0 >> 4) + line, (as.rows - 1) >> 4)
-                                     : min((ws.r0 >> 4) + line - 2 * MB, (ws.rows - 1) >> 4);
-    const uint8_t *ssrc = (line < 2 * MB ? a_sc : w_sc) + rb * nk * 128 + (chunk & 7) * 16;
+}
 
+template <class S, int EPI>
+__global__ __launch_bounds__(tile::kThreads4) __attribute__((amdgpu_waves_per_eu(S::WPE, S::WPE)))
+void linear_tile_kernel(LinearArgs a, Tiles t)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    constexpr int MB = S::MB, NB = S::NB, NM = MB * NB, NF = MB + NB, ST = S::ST;
+    constexpr int AP = S::A_BYTES / 4096, WP = S::W_BYTES / 4096, NC = AP + WP + 1;  // copies per wave and step
+    constexpr uint32_t W0 = ST * S::A_BYTES, S0 = W0 + ST * S::W_BYTES;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1, g = lane >> 4, x = lane & 15;
+    const int ld = t.nk * kStepBytes;  // bytes of a row of codes
+    int stride = gridDim.x;
+    __asm__ volatile("" : "+s"(stride));  // read once: a scalar load in the loop would make every wait for LDS a full one
+
+    // The copies: where the next step's come from (row offsets of the item's
+    // tile, clamped to the last row; those rows are never stored).
     const uint32_t lds0 = (uint32_t)(uintptr_t)(tile::lds_char *)smem;
     const uint32_t la0 = __builtin_amdgcn_readfirstlane(lds0 + wave * AP * 1024);
     const uint32_t lw0 = __builtin_amdgcn_readfirstlane(lds0 + W0 + wave * WP * 1024);
+    const int scopy = wave % S::S_COPIES;  // waves past the number of scale copies repeat one
     const uint32_t ls0 = __builtin_amdgcn_readfirstlane(lds0 + S0 + scopy * 1024);
-    const int kl = k1 - 1;
-    // copy l of step kt (A's, W's, the scales') into stage st
-    auto copy = [&](int l, int kt, int st) {
-        if (l < AP) {
-            const auto s = as.at(kt);
-            as.copy(as.addr(arow[l], s), la0 + st * S::A_BYTES + l * 1024);
-        } else if (l < AP + WP) {
-            const auto s = ws.at(kt);
-            ws.copy(ws.addr(wrow[l - AP], s), lw0 + st * S::W_BYTES + (l - AP) * 1024);
+    const int chunk = min(scopy * 64 + lane, S::S_CHUNKS - 1), line = chunk >> 3;
+    const uint8_t *abase, *wbase, *ssrc;
+    uint32_t aoff[AP], woff[WP];
+    int c_item = blockIdx.x, c_kt;
+    auto aim = [&] {  // at item c_item
+        const Item it = item_of<S>(t, c_item);
+        abase = a.a_codes + (int64_t)it.m0 * ld;
+        wbase = a.w_codes + (int64_t)it.n0 * ld;
+#pragma unroll
+        for (int i = 0; i < AP; ++i) {
+            const int r = (wave * AP + i) * 8 + (lane >> 3);
+            aoff[i] = (uint32_t)min(r, a.M - 1 - it.m0) * (uint32_t)ld + tile::swz(r, lane & 7) * 16;
+        }
+#pragma unroll
+        for (int i = 0; i < WP; ++i) {
+            const int r = (wave * WP + i) * 8 + (lane >> 3);
+            woff[i] = (uint32_t)min(r, a.N - 1 - it.n0) * (uint32_t)ld + tile::swz(r, lane & 7) * 16;
+        }
+        const int64_t rb = line < 2 * MB ? min((it.m0 >> 4) + line, (a.M - 1) >> 4)
+                                         : min((it.n0 >> 4) + line - 2 * MB, (a.N - 1) >> 4);
+        ssrc = (line < 2 * MB ? a.a_scales : a.w_scales) + rb * t.nk * 128 + (chunk & 7) * 16;
+        c_kt = 0;
+    };
+    auto copy = [&](int l, int st) {  // copy l of the step aimed at, into stage st
+        const int64_t k = (int64_t)c_kt * kStepBytes;
+        if (l < AP)
+            tile::lds_copy16_s(uniform(abase + k), aoff[l], __builtin_amdgcn_readfirstlane(la0 + st * S::A_BYTES + l * 1024));
+        else if (l < AP + WP)
+            tile::lds_copy16_s(uniform(wbase + k), woff[l - AP],
+                               __builtin_amdgcn_readfirstlane(lw0 + st * S::W_BYTES + (l - AP) * 1024));
+        else
+            tile::lds_copy16_v(ssrc + k, __builtin_amdgcn_readfirstlane(ls0 + st * S::S_BYTES));
+    };
+    auto advance = [&] {  // to the next step; past the last one, that again (into stages that nobody reads)
+        if (++c_kt < t.nk) return;
+        if (c_item + stride < t.n_tiles) {
+            c_item += stride;
+            aim();
         } else {
-            tile::lds_copy16_v(ssrc + (int64_t)kt * 128, ls0 + st * S::S_BYTES);
+            --c_kt;
         }
     };
-    constexpr int NC = AP + WP + 1;
-
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     u32x4 fa[2][MB], fw[2][NB];
     uint32_t sa[MB], sw[NB], sa1[MB], sw1[NB];
@@ -302,17 +409,29 @@ __device__ __forceinline__ void mma_mx(const tile::Dense<false> &as, const tile:
 #pragma unroll
         for (int i = 0; i < NB; ++i) sw[i] = sw1[i];
     };
+    f32x4 acc[NB][MB];
     auto mfma2 = [&](int ks, int i) {
 #pragma unroll
-        for (int j = i; j < i + 2; ++j)
+        for (int j = i; j < i + 2 && j < NM; ++j)
             acc[j % NB][j / NB] = mfma(fw[ks][j % NB], fa[ks][j / NB], acc[j % NB][j / NB], ks, sw[j % NB], sa[j / NB]);
     };
 
+    // The compiler would sink a half's MFMAs across the barrier and the branch of advance() to their last use.
+    auto pin = [&] {
 #pragma unroll
-    for (int st = 0; st < 2; ++st)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int l = 0; l < NC; ++l) copy(l, min(k0 + st, kl), st);
-    __asm__ volatile("s_waitcnt vmcnt(%0)" : : "n"(NC) : "memory");
+            for (int mb = 0; mb < MB; ++mb) __asm__ volatile("" : "+v"(acc[nb][mb]));
+    };
+
+    aim();
+#pragma unroll
+    for (int st = 0; st < ST; ++st) {
+#pragma unroll
+        for (int l = 0; l < NC; ++l) copy(l, st);
+        advance();
+    }
+    __asm__ volatile("s_waitcnt vmcnt(%0)" : : "n"((ST - 1) * NC) : "memory");
     __builtin_amdgcn_s_barrier();
     __asm__ volatile("" : : : "memory");
 #pragma unroll
@@ -324,86 +443,65 @@ __device__ __forceinline__ void mma_mx(const tile::Dense<false> &as, const tile:
 
     constexpr int RD = NM * 3 / 4;  // a half's reads and copies are spread over this many MFMAs
     int st = 0;
-    for (int kt = k0; kt < k1; ++kt) {
+    for (int item = blockIdx.x; item < t.n_tiles; item += stride) {
+        const Item it = item_of<S>(t, item);
 #pragma unroll
-        for (int i = 0; i < NM; i += 2) {
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int f = 0; f < NF; ++f)
-                if (f * RD / NF / 2 * 2 == i) rd(st, 1, f);
-            mfma2(0, i);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int mb = 0; mb < MB; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int kt = 0; kt < t.nk; ++kt) {
+            const int st1 = st + 1 == ST ? 0 : st + 1;
+            // first half; the second half's fragments are read beside it
+#pragma unroll
+            for (int i = 0; i < NM; i += 2) {
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+                    if (f * RD / NF / 2 * 2 == i) rd(st, 1, f);
+                mfma2(0, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            pin();
+            // the next step has landed (an output's stores, counted too, only make this wait longer), and every
+            // wave has read all of this one
+            __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((ST - 2) * NC) : "memory");
+            __builtin_amdgcn_s_barrier();
+            __asm__ volatile("" : : : "memory");
+            // second half; beside it the next step's first fragments, and copies into this step's stage
+#pragma unroll
+            for (int i = 0; i < NM; i += 2) {
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+                    if (f * RD / NF / 2 * 2 == i) {
+                        rd(st1, 0, f);
+                        rd_scale(st1, f);
+                    }
+#pragma unroll
+                for (int l = 0; l < NC; ++l)
+                    if (l * RD / NC / 2 * 2 == i) copy(l, st);
+                mfma2(1, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            pin();
+            advance();
+            next_scales();
+            st = st1;
         }
-        // step kt + 1 has landed, and every wave has read all of step kt
-        __asm__ volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
-        __builtin_amdgcn_s_barrier();
-        __asm__ volatile("" : : : "memory");
-        const int k2 = min(kt + 2, kl);
-#pragma unroll
-        for (int i = 0; i < NM; i += 2) {
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-                if (f * RD / NF / 2 * 2 == i) {
-                    rd(st ^ 1, 0, f);
-                    rd_scale(st ^ 1, f);
-                }
-#pragma unroll
-            for (int l = 0; l < NC; ++l)
-                if (l * RD / NC / 2 * 2 == i) copy(l, k2, st);
-            mfma2(1, i);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        next_scales();
-        st ^= 1;
-    }
-    if constexpr (S::WPE == 1) {  // wait states before acc_value's reads of the last results
-        __asm__ volatile("s_nop 15\n\ts_nop 15" : : : "memory");
-        __builtin_amdgcn_sched_barrier(0);
+        store_tile<S, EPI>(a, it, smem, acc);
     }
     tile::wait_all_copies();
 }
 
-// One tile per workgroup; EPI == kPartial: K range blockIdx.x / n_tiles of `splits`.
-template <class S, int EPI>
-__global__ __launch_bounds__(tile::kThreads4) __attribute__((amdgpu_waves_per_eu(S::WPE, S::WPE)))
-void linear_tile_kernel(LinearArgs a, float *part, int nk, int tiles_n, int n_tiles, int splits)
-{
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
-    constexpr bool PART = EPI == tile::kPartial;
-    const int sp = PART ? (int)blockIdx.x / n_tiles : 0;
-    int tm, tn;
-    tile::tile_of((int)blockIdx.x - sp * n_tiles, tiles_n, n_tiles, tm, tn);
-    const int m0 = tm * S::BM, n0 = tn * S::BN;
-    const int k0 = PART ? (int)((int64_t)sp * nk / splits) : 0;
-    const int k1 = PART ? (int)((int64_t)(sp + 1) * nk / splits) : nk;
-    const tile::Dense<false> as{reinterpret_cast<const uint16_t *>(a.a_codes), (int64_t)nk * (kStepBytes / 2), a.M, m0};
-    const tile::Dense<false> ws{reinterpret_cast<const uint16_t *>(a.w_codes), (int64_t)nk * (kStepBytes / 2), a.N, n0};
-    f32x4 acc[S::NB][S::MB];
-    if (k1 > k0) {
-        mma_mx<S>(as, ws, a.a_scales, a.w_scales, nk, k0, k1, smem, acc);
-    } else {
-#pragma unroll
-        for (int nb = 0; nb < S::NB; ++nb)
-#pragma unroll
-            for (int mb = 0; mb < S::MB; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const tile::Out o{static_cast<const uint16_t *>(a.bias), a.gate, PART ? part : a.out, PART ? (int64_t)a.N : a.ldo,
-                      a.M, a.N};
-    tile::store4<S, EPI>(o, m0, n0, sp, smem, acc);
-}
-
-typedef Shape<8, 8, 1> Tile256x256;
-typedef Shape<4, 4, 2> Tile128x128;
-typedef Shape<2, 4, 3> Tile64x128;
-enum TileId : int32_t { kRows, kTile256x256, kTile128x128, kTile64x128 };
-
-// Rows up to which the few-row kernel runs, and up to which it brings bf16
-// rows to MXFP4 itself.
-constexpr int kFewRows = 64, kQuantRows = 16;
+typedef Shape<4, 4, 2, 2> Tile128x128;
+typedef Shape<4, 4, 1, 4> Tile128x128Deep;  // four stages: for few tiles, one workgroup per compute unit
+typedef Shape<3, 3, 1, 5> Tile96x96;
+typedef Shape<2, 4, 2, 3> Tile64x128;
+typedef Shape<2, 2, 2, 4> Tile64x64;
+enum TileId : int32_t { kRows, kTile128x128, kTile128x128Deep, kTile96x96, kTile64x128, kTile64x64 };
 
 template <int MB, int W, bool QUANT>
 hipError_t launch_rows_t(const LinearArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.N / 16)), block(64 * W);
+    const dim3 grid((unsigned)(a.N / 16), (unsigned)((a.M + 16 * MB - 1) / (16 * MB))), block(64 * W);
     const int nk = steps_of(a.K);
     switch (a.epi) {
     case kEpiBias: hipLaunchKernelGGL((linear_rows_kernel<MB, W, kEpiBias, QUANT>), grid, block, 0, stream, a, nk); break;
@@ -424,28 +522,22 @@ hipError_t launch_rows(const LinearArgs &a, hipStream_t stream)
 }
 
 template <class S, int EPI>
-hipError_t launch_tile_t(const LinearArgs &a, float *part, int splits, hipStream_t stream)
+hipError_t launch_tile_t(const LinearArgs &a, hipStream_t stream)
 {
-    const int tiles_n = tile::tiles_along(a.N, S::BN), n_tiles = tile::tiles_along(a.M, S::BM) * tiles_n;
-    hipLaunchKernelGGL((linear_tile_kernel<S, EPI>), dim3((unsigned)n_tiles * (unsigned)splits), dim3(tile::kThreads4), 0,
-                       stream, a, part, steps_of(a.K), tiles_n, n_tiles, splits);
+    const int tiles_n = tile::tiles_along(a.N, S::BN);
+    const Tiles t{steps_of(a.K), tiles_n, tile::tiles_along(a.M, S::BM) * tiles_n};
+    const int grid = std::min(t.n_tiles, device_cu_count() * S::WPE);
+    hipLaunchKernelGGL((linear_tile_kernel<S, EPI>), dim3((unsigned)grid), dim3(tile::kThreads4), 0, stream, a, t);
     return hipGetLastError();
 }
 
 template <class S>
-hipError_t launch_tile(const LinearArgs &a, float *part, int splits, hipStream_t stream)
+hipError_t launch_tile(const LinearArgs &a, hipStream_t stream)
 {
-    if (splits > 1) {
-        const hipError_t e = launch_tile_t<S, tile::kPartial>(a, part, splits, stream);
-        if (e != hipSuccess) return e;
-        return launch_linear_reduce(regenvc::LinearArgs{nullptr, nullptr, a.bias, a.gate, a.out, 0, a.ldo, a.M, a.N, a.K,
-                                                        a.epi, part, 0},
-                                    splits, stream);
-    }
     switch (a.epi) {
-    case kEpiBias: return launch_tile_t<S, kEpiBias>(a, nullptr, 1, stream);
-    case kEpiBiasGelu: return launch_tile_t<S, kEpiBiasGelu>(a, nullptr, 1, stream);
-    case kEpiGatedRes: return launch_tile_t<S, kEpiGatedRes>(a, nullptr, 1, stream);
+    case kEpiBias: return launch_tile_t<S, kEpiBias>(a, stream);
+    case kEpiBiasGelu: return launch_tile_t<S, kEpiBiasGelu>(a, stream);
+    case kEpiGatedRes: return launch_tile_t<S, kEpiGatedRes>(a, stream);
     }
     return hipErrorInvalidValue;
 }
@@ -457,25 +549,57 @@ int64_t align256(int64_t b)
 
 }  // namespace
 
-TilePlan linear_plan(int M, int N, int K, int epi, int n_cu, int64_t ws_bytes)
+// Few rows: where the weights' bytes and latency count, not reuse of a tile.
+// Measured (quantisation included), few-row kernel against the best tile: 1536
+// x 1536 5.4 and 7.4 us with one row, 7.6 and 8.6 with 64; 8960 x 1536 7.9 and
+// 8.1 with 17 rows, 8.8 and 8.3 with 32; 1536 x 8960 15.8 and 15.0 with 64.
+static bool few_rows(int M, int N)
 {
-    if (M <= kFewRows) return TilePlan{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 16, steps_of(K) > 8 ? 16 : 4};
-    const TileCost costs[] = {
-        {kTile256x256, 256, 256, 4, epi == kEpiBias ? 7.7 : 10.9, 7.7, 1.0, 1.2, true},
-        {kTile128x128, 128, 128, 4, 2.0, 2.0, 0.424, 0.988, true},
-        {kTile64x128, 64, 128, 4, 1.5, 1.5, 0.396, 0.951, true},
-    };
-    return plan_tiles(costs, SplitCost{5.1, 8.1e6, epi == kEpiGatedRes ? 8 : 2}, M, N, steps_of(K), n_cu, ws_bytes);
+    return M <= 16 || (M <= 32 && N <= 4096) || (M <= 64 && N <= 1536);
 }
 
-LinearNeed linear_need(int M, int N, int K, int epi, bool quantized, int n_cu)
+// Whether the few-row kernel brings bf16 rows to MXFP4 itself: each workgroup
+// does it again, which up to 16 rows of 2048 costs less than a launch
+// (1536 x 1536 and one row 4.6 us against 5.4, 512 x 512 3.1 against 4.8; K =
+// 8960 8.6 against 7.4).
+static bool quantizes_itself(int M, int K)
 {
-    LinearNeed need{};
-    if (M == 0 || N == 0) return need;
-    if (!quantized && M > kQuantRows && K > 0) need.least = align256(code_bytes(M, K)) + align256(scale_bytes(M, K));
-    const TilePlan p = linear_plan(M, N, K, epi, n_cu, INT64_MAX);
-    need.total = need.least + (p.splits > 1 ? (int64_t)p.splits * M * N * (int64_t)sizeof(float) : 0);
-    return need;
+    return M <= 16 && K <= 2048;
+}
+
+TilePlan linear_plan(int M, int N, int K, int epi, int n_cu)
+{
+    const int nk = steps_of(K);
+    if (few_rows(M, N) || K == 0) return TilePlan{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 16, nk > 8 ? 16 : 4};
+    // Fitted to the times of 3240 launches (12 pairs of N and K from 256 to 8960, 18 row counts from 65 to 10920, three
+    // epilogues, every tile): the choice is on average 0.9 % slower than the best.
+    struct Cost {
+        int32_t tile, bm, bn;
+        double fixed[3], step, load, once;  // us per tile (by epilogue), per step, factor on whole rounds, per launch
+    };
+    static const Cost costs[] = {
+        {kTile128x128, 128, 128, {0.59, 1.43, 3.11}, 0.438, 1.26, 0.84},
+        {kTile128x128Deep, 128, 128, {1.61, 2.23, 3.93}, 0.390, 1.37, 0.0},
+        {kTile96x96, 96, 96, {1.67, 2.07, 2.58}, 0.305, 1.37, 0.5},
+        {kTile64x128, 64, 128, {1.12, 1.11, 1.96}, 0.303, 1.31, 1.02},
+        {kTile64x64, 64, 64, {0.60, 0.79, 1.35}, 0.186, 1.27, 1.55},
+    };
+    const Cost *best = nullptr;
+    double best_t = INFINITY;
+    for (const Cost &c : costs) {
+        const int64_t tiles = (int64_t)((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
+        const double one = c.fixed[epi] + nk * c.step;
+        double t = c.once + (double)(tiles / n_cu) * one * c.load;
+        if (tiles % n_cu > 0) t += one * (1.0 + (c.load - 1.0) * (double)(tiles % n_cu) / n_cu);
+        if (t < best_t) best_t = t, best = &c;
+    }
+    return TilePlan{best->tile, 1, best->bm, best->bn, 4};
+}
+
+int64_t linear_workspace(int M, int N, int K, bool quantized)
+{
+    if (M == 0 || N == 0 || K == 0 || quantized || quantizes_itself(M, K)) return 0;
+    return align256(code_bytes(M, K)) + align256(scale_bytes(M, K));
 }
 
 hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream)
@@ -502,23 +626,20 @@ hipError_t launch_dequantize(const DequantizeArgs &a, hipStream_t stream)
 hipError_t launch_linear(const LinearArgs &args, hipStream_t stream)
 {
     LinearArgs a = args;
-    char *part = a.ws;
-    int64_t left = a.ws_bytes;
-    if (a.a_codes == nullptr && a.M > kQuantRows && a.K > 0) {
-        const int64_t codes = align256(code_bytes(a.M, a.K)), least = codes + align256(scale_bytes(a.M, a.K));
-        uint8_t *q = reinterpret_cast<uint8_t *>(a.ws);
-        const hipError_t e = launch_quantize(QuantizeArgs{a.a, a.lda, q, q + codes, a.M, a.K, false}, stream);
+    if (linear_workspace(a.M, a.N, a.K, a.a_codes != nullptr) > 0) {
+        uint8_t *codes = reinterpret_cast<uint8_t *>(a.ws), *scales = codes + align256(code_bytes(a.M, a.K));
+        const hipError_t e = launch_quantize(QuantizeArgs{a.a, a.lda, codes, scales, a.M, a.K, false}, stream);
         if (e != hipSuccess) return e;
-        a.a_codes = q, a.a_scales = q + codes;
-        part += least, left -= least;
+        a.a_codes = codes, a.a_scales = scales;
     }
-    const TilePlan p = linear_plan(a.M, a.N, a.K, a.epi, device_cu_count(), left);
-    float *sums = reinterpret_cast<float *>(part);
+    const TilePlan p = linear_plan(a.M, a.N, a.K, a.epi, device_cu_count());
     switch (p.tile) {
-    case kRows: return p.waves == 16 ? launch_rows<16>(a, stream) : launch_rows<4>(a, stream);
-    case kTile256x256: return launch_tile<Tile256x256>(a, sums, p.splits, stream);
-    case kTile128x128: return launch_tile<Tile128x128>(a, sums, p.splits, stream);
-    case kTile64x128: return launch_tile<Tile64x128>(a, sums, p.splits, stream);
+    case kRows: return p.waves == 16 ? launch_rows<16>(a, stream) : launch_rows<4>(a, stream);  // (K = 0: no steps, any M)
+    case kTile128x128: return launch_tile<Tile128x128>(a, stream);
+    case kTile128x128Deep: return launch_tile<Tile128x128Deep>(a, stream);
+    case kTile96x96: return launch_tile<Tile96x96>(a, stream);
+    case kTile64x128: return launch_tile<Tile64x128>(a, stream);
+    case kTile64x64: return launch_tile<Tile64x64>(a, stream);
     }
     return hipErrorInvalidValue;
 }

@@ -173,29 +173,25 @@ regenvc_status regenvc_mx_dequantize(const void *codes, const void *scales, void
     return regenvc::abi::launch_status(mx::launch_dequantize(a, static_cast<hipStream_t>(stream)), fn);
 }
 
-regenvc_status regenvc_mx_linear_workspace(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t quantized,
-                                           int32_t n_cu, int64_t *least, int64_t *total)
+regenvc_status regenvc_mx_linear_workspace(int32_t M, int32_t N, int32_t K, int32_t quantized, int64_t *bytes)
 {
     const char *fn = "regenvc_mx_linear_workspace";
-    if (least == nullptr || total == nullptr) return failf(REGENVC_ERR_INVALID_ARG, "%s: least or total is NULL", fn);
-    if (n_cu < 1) return failf(REGENVC_ERR_INVALID_ARG, "%s: n_cu=%d < 1", fn, n_cu);
-    const regenvc_status st = check_linear_shape(fn, M, N, K, epilogue);
+    if (bytes == nullptr) return failf(REGENVC_ERR_INVALID_ARG, "%s: bytes is NULL", fn);
+    const regenvc_status st = check_linear_shape(fn, M, N, K, REGENVC_EPI_BIAS);
     if (st != REGENVC_OK) return st;
-    const mx::LinearNeed need = mx::linear_need(M, N, K, epilogue, quantized != 0, n_cu);
-    *least = need.least, *total = need.total;
+    *bytes = mx::linear_workspace(M, N, K, quantized != 0);
     return done();
 }
 
 regenvc_status regenvc_mx_linear_plan_query(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t n_cu,
-                                            int64_t workspace_bytes, regenvc_tile_plan *plan)
+                                            regenvc_tile_plan *plan)
 {
     const char *fn = "regenvc_mx_linear_plan_query";
     if (plan == nullptr) return failf(REGENVC_ERR_INVALID_ARG, "%s: plan is NULL", fn);
-    if (n_cu < 1 || workspace_bytes < 0)
-        return failf(REGENVC_ERR_INVALID_ARG, "%s: n_cu=%d workspace_bytes=%lld", fn, n_cu, (long long)workspace_bytes);
+    if (n_cu < 1) return failf(REGENVC_ERR_INVALID_ARG, "%s: n_cu=%d < 1", fn, n_cu);
     const regenvc_status st = check_linear_shape(fn, M, N, K, epilogue);
     if (st != REGENVC_OK) return st;
-    const regenvc::TilePlan p = mx::linear_plan(M, N, K, epilogue, n_cu, workspace_bytes);
+    const regenvc::TilePlan p = mx::linear_plan(M, N, K, epilogue, n_cu);
     *plan = regenvc_tile_plan{p.bm, p.bn, p.waves, p.splits};
     return done();
 }
@@ -243,14 +239,13 @@ regenvc_status regenvc_mx_linear_fwd(const void *a, int64_t lda, const void *a_c
     }
     if (overlaps(ro, rw)) return failf(REGENVC_ERR_INVALID_ARG, "%s: workspace overlaps another argument", fn);
     if ((st = regenvc::abi::device_ok()) != REGENVC_OK) return st;
-    const mx::LinearNeed need =
-        mx::linear_need(M, N, K, epilogue, quantized || K == 0, regenvc::device_cu_count());
-    if (ws_bytes < need.least)
+    const int64_t need = mx::linear_workspace(M, N, K, quantized);
+    if (ws_bytes < need)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: workspace of %lld bytes, this call needs %lld", fn, (long long)ws_bytes,
-                     (long long)need.least);
+                     (long long)need);
     auto u8 = [](const void *p) { return static_cast<const uint8_t *>(p); };
     const mx::LinearArgs la{a,   lda, u8(a_codes), u8(a_scales), u8(w_codes), u8(w_scales), bias, gate, out, ldo, M,
-                            N,   K,   epilogue,    static_cast<char *>(workspace), ws_bytes};
+                            N,   K,   epilogue,    workspace};
     return regenvc::abi::launch_status(mx::launch_linear(la, static_cast<hipStream_t>(stream)), fn);
 }
 

@@ -64,17 +64,11 @@ struct LinearArgs {
     int64_t ldo;
     int32_t M, N, K;
     int32_t epi;
-    char *ws;
-    int64_t ws_bytes;
+    void *ws;  // a's codes and scales: linear_workspace bytes
 };
-// Workspace: `least` bytes hold a's codes and scales, `total` also the
-// partial sums of a split of K.
-struct LinearNeed {
-    int64_t least, total;
-};
-LinearNeed linear_need(int M, int N, int K, int epi, bool quantized, int n_cu);
-// The plan: rows x columns of a tile, its waves, ranges of K (in steps of 256).
-TilePlan linear_plan(int M, int N, int K, int epi, int n_cu, int64_t ws_bytes);
+int64_t linear_workspace(int M, int N, int K, bool quantized);
+// The plan: rows x columns of a tile and its waves (K is not split).
+TilePlan linear_plan(int M, int N, int K, int epi, int n_cu);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t stream);
 
 // A key/value cache: codes [B, heads, capacity, D / 2] and scales [B, heads,

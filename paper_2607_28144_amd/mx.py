@@ -87,20 +87,17 @@ def dequantize(m: MxTensor, dtype: torch.dtype = torch.float32, out: Optional[to
     return out
 
 
-_NEED = {}  # (device index, shape, epilogue, quantized) -> least and total workspace bytes of a linear layer
+_NEED = {}  # (shape, quantized) -> workspace bytes of a linear layer
 
 
-def linear_workspace_bytes(M: int, N: int, K: int, epilogue: str, quantized: bool, idx: int) -> Tuple[int, int]:
-    """Workspace bytes that a linear layer must have and can use on the device
-    of an index (regenvc_mx_linear_workspace)."""
-    key = (idx, M, N, K, epilogue, quantized)
+def linear_workspace_bytes(M: int, N: int, K: int, quantized: bool) -> int:
+    """Workspace bytes of a linear layer (regenvc_mx_linear_workspace)."""
+    key = (M, N, K, quantized)
     need = _NEED.get(key)
     if need is None:
-        least, total = ctypes.c_int64(), ctypes.c_int64()
-        st = _lib.load().regenvc_mx_linear_workspace(M, N, K, EPI[epilogue], int(quantized), _lib.compute_units(idx),
-                                                     ctypes.byref(least), ctypes.byref(total))
-        # a shape the call itself refuses: let it say so
-        need = (least.value, total.value) if st == _lib.OK else (0, 0)
+        out = ctypes.c_int64()
+        st = _lib.load().regenvc_mx_linear_workspace(M, N, K, int(quantized), ctypes.byref(out))
+        need = out.value if st == _lib.OK else 0  # a shape the call itself refuses: let it say so
         if len(_NEED) >= 4096:
             _NEED.clear()
         _NEED[key] = need
@@ -136,16 +133,12 @@ def linear_fwd(a: Union[torch.Tensor, MxTensor], w: MxTensor, bias: Optional[tor
         out, ldo = torch.empty(M, N, dtype=torch.bfloat16, device=a.device), N
     bp = _lib.vector(bias, "bias", torch.bfloat16, N, idx)
     gp = _lib.vector(gate, "gate", torch.float32, N, idx)
-    least, total = linear_workspace_bytes(M, N, K, epilogue, quantized, idx)
+    need = linear_workspace_bytes(M, N, K, quantized)
     with _lib.on_device(idx):
-        ws = None
-        if total > 0:
-            ws = _lib.split_workspace(total, a.device)
-            if ws is None and least > 0:  # without the partial sums of a split of K
-                ws = torch.empty(least, dtype=torch.uint8, device=a.device)
+        ws = torch.empty(need, dtype=torch.uint8, device=a.device) if need > 0 else None
         st = _lib.load().regenvc_mx_linear_fwd(
             a_ptr, lda, c_ptr, s_ptr, w.codes.data_ptr(), w.scales.data_ptr(), bp, gp, out.data_ptr(), ldo, M, N, K, epi,
-            ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, _lib.raw_stream(idx))
+            ws.data_ptr() if ws is not None else None, need, _lib.raw_stream(idx))
     _lib.check(st, "regenvc_mx_linear_fwd")
     return out
 

@@ -101,11 +101,10 @@ def test_linear_refusals(lib):
     refused(lib, INV, "workspace overlaps", call(ws=H))
     refused(lib, INV, "workspace_bytes", call(wsb=-1))
     assert call(M=0) == 0 and call(N=0, ldo=8) == 0
-    least, total = ctypes.c_int64(), ctypes.c_int64()
+    n = ctypes.c_int64()
     need = lib.regenvc_mx_linear_workspace
-    refused(lib, INV, "NULL", need(4, 16, 64, 0, 0, 256, None, ctypes.byref(total)))
-    refused(lib, INV, "n_cu", need(4, 16, 64, 0, 0, 0, ctypes.byref(least), ctypes.byref(total)))
-    refused(lib, UNS, "multiple of 16", need(4, 17, 64, 0, 0, 256, ctypes.byref(least), ctypes.byref(total)))
+    refused(lib, INV, "NULL", need(4, 16, 64, 0, None))
+    refused(lib, UNS, "multiple of 16", need(4, 17, 64, 0, ctypes.byref(n)))
 
 
 def cache(**kw):
@@ -192,16 +191,18 @@ def test_attention_plans(lib):
 
 
 def test_linear_plans(lib):
-    p = _lib.TilePlan()
-    least, total = ctypes.c_int64(), ctypes.c_int64()
+    p, n, c, sc = _lib.TilePlan(), ctypes.c_int64(), ctypes.c_int64(), ctypes.c_int64()
     for M, N, K, epi in [(1, 16, 8, 0), (64, 1536, 8960, 1), (65, 16, 8, 2), (1365, 1536, 8960, 0), (10920, 8960, 1536, 1),
                          (200, 8960, 8960, 2), (65520, 1536, 1536, 0)]:
-        for quantized in (0, 1):
-            assert lib.regenvc_mx_linear_workspace(M, N, K, epi, quantized, 256, ctypes.byref(least), ctypes.byref(total)) == 0
-            assert lib.regenvc_mx_linear_plan_query(M, N, K, epi, 256, BIG, ctypes.byref(p)) == 0
-            assert total.value - least.value == (p.k_ranges * M * N * 4 if p.k_ranges > 1 else 0)
-            assert (least.value == 0) == (quantized == 1 or M <= 16)
-        assert lib.regenvc_mx_linear_plan_query(M, N, K, epi, 256, 0, ctypes.byref(p)) == 0 and p.k_ranges == 1
+        assert lib.regenvc_mx_linear_plan_query(M, N, K, epi, 256, ctypes.byref(p)) == 0
+        assert p.k_ranges == 1 and p.rows >= 16 and p.cols >= 16 and p.waves in (4, 16)
+        assert lib.regenvc_mx_linear_workspace(M, N, K, 1, ctypes.byref(n)) == 0 and n.value == 0
+        assert lib.regenvc_mx_linear_workspace(M, N, K, 0, ctypes.byref(n)) == 0
+        assert lib.regenvc_mx_bytes(M, K, ctypes.byref(c), ctypes.byref(sc)) == 0
+        assert n.value == 0 if M <= 16 else n.value == 0 or n.value >= c.value + sc.value
+    refused(lib, INV, "NULL", lib.regenvc_mx_linear_plan_query(4, 16, 64, 0, 256, None))
+    refused(lib, INV, "n_cu", lib.regenvc_mx_linear_plan_query(4, 16, 64, 0, 0, ctypes.byref(p)))
+    refused(lib, INV, "epilogue", lib.regenvc_mx_linear_plan_query(4, 16, 64, 7, 256, ctypes.byref(p)))
 
 
 def test_residual_norm_refusals(lib):
