@@ -59,8 +59,8 @@ regenvc_status regenvc_mx_dequantize(const void *codes, const void *scales, void
                  MXFP4 by the call; or NULL with a_codes, a_scales: [M, K] in MXFP4
      w_codes, w_scales: [N, K] in MXFP4
      bias, gate, out, ldo, epilogue: as regenvc_linear_fwd
-   M, N, K >= 0; K a multiple of 8, at most 2^20; N a multiple of 16; pointers
-   16-byte aligned.  workspace: 256-byte aligned, at least
+   M, N, K >= 0; K a multiple of 8, at most 2^20; N a multiple of 16, below
+   2^20; M N at most 2^42; pointers 16-byte aligned.  workspace: 256-byte aligned, at least
    regenvc_mx_linear_workspace bytes (a's codes and scales; NULL if that is 0).
    The kernel, chosen by size, sets the order of the fp32 sum: a row may come
    out a rounding apart in calls of different numbers of rows. */

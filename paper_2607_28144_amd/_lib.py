@@ -261,11 +261,17 @@ def compute_units(idx: int) -> int:
     return n
 
 
+_raw_stream = None
+
+
 def raw_stream(idx: int) -> int:
     """torch's current stream of the device of an index, as the address the C ABI takes."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(idx) if raw is not None else torch.cuda.current_stream(idx).cuda_stream
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw_stream(idx)
 
 
 def split_workspace(need: int, device):

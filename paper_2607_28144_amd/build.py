@@ -19,8 +19,9 @@ SOURCES = ["api.cpp", "attn_fwd.hip", "lse_merge.hip", "norm_rope.hip", "dit_api
            "vae.hip", "residual_norm_api.cpp", "residual_norm.hip", "mx_api.cpp", "mx.hip", "mx_attn.hip"]
 ARCH = "gfx950"
 # MFMA results in VGPRs: the score tiles feed VALU softmax code directly, and
-# read-only operands may then live in AGPRs.  Not for the tile kernels of the
-# linear layers, whose accumulators fill the AGPRs.
+# read-only operands may then live in AGPRs; the MXFP4 tiles, whose accumulators
+# leave room beside them, are spared the moves between the two files.  Not for
+# the bf16 tile kernels, whose accumulators fill the AGPRs.
 VGPR_FORM = {"attn_fwd.hip", "mx.hip", "mx_attn.hip"}
 # Sources with tiles whose MFMAs are instructions of their own (inline
 # assembly, around which the compiler places no wait states): their assembly is

@@ -48,8 +48,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a, int nk)
 {
     __shared__ uint8_t sc[16][16];  // [row][block of the two steps]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t r0 = (int64_t)blockIdx.y * 16;
-    const int c = blockIdx.x * 512 + lane * 8;
+    const int64_t r0 = (int64_t)blockIdx.x * 16;
+    const int c = blockIdx.y * 512 + lane * 8;
     float x[4][8];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
@@ -68,9 +68,9 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a, int nk)
     }
     __syncthreads();
     const int t = threadIdx.x, step = t >> 6;  // of the two
-    if (t >= 128 || blockIdx.x * 2 + step >= nk) return;
+    if (t >= 128 || (int)blockIdx.y * 2 + step >= nk) return;
     const int r = lane & 15, b = step * 8 + 2 * (lane >> 4);
-    *reinterpret_cast<uint16_t *>(a.scales + ((int64_t)blockIdx.y * nk + blockIdx.x * 2 + step) * 128 + lane * 2) =
+    *reinterpret_cast<uint16_t *>(a.scales + ((int64_t)blockIdx.x * nk + blockIdx.y * 2 + step) * 128 + lane * 2) =
         (uint16_t)(sc[r][b] | sc[r][b + 1] << 8);
 }
 
@@ -78,8 +78,8 @@ template <bool F32>
 __global__ __launch_bounds__(256) void dequantize_kernel(DequantizeArgs a, int nk)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6);
-    const int c = blockIdx.x * 512 + lane * 8;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int c = blockIdx.y * 512 + lane * 8;
     if (row >= a.rows || c >= a.K) return;
     const uint32_t code = *reinterpret_cast<const uint32_t *>(a.codes + row * nk * kStepBytes + c / 2);
     const int kt = c / kStepK, blk = c % kStepK / kBlock;
@@ -140,15 +140,15 @@ __device__ __forceinline__ uint32_t quantize_block(const uint16_t *row, int c, i
 // is little of everything, so a workgroup takes 16 output channels and all
 // rows, its W waves taking the steps of K in turn; their sums meet in LDS.
 // QUANT: a is bf16 and each workgroup brings its rows to MXFP4 itself, in
-// registers.  blockIdx.y: tile of 16 MB rows.
+// registers.  blockIdx.x: tile of 16 MB rows.
 template <int MB, int W, int EPI, bool QUANT>
 __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int nk)
 {
     __shared__ f32x4 red[W][MB * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, x = lane & 15;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MB;
+    const int n0 = blockIdx.y * 16, m0 = blockIdx.x * 16 * MB;
     const uint8_t *wc = a.w_codes + (int64_t)(n0 + x) * nk * kStepBytes + g * 32;
-    const uint8_t *wsc = a.w_scales + (int64_t)blockIdx.x * nk * 128 + lane * 2;
+    const uint8_t *wsc = a.w_scales + (int64_t)blockIdx.y * nk * 128 + lane * 2;
     f32x4 acc[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) acc[mb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -204,15 +204,23 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
 
 // ---------------------------------------------------------------- tiles
 // Four waves per tile of (32 MB) rows x (32 NB) channels, each with a quarter
-// of it, WPE workgroups per compute unit.  A workgroup walks tiles (or K ranges
-// of tiles) blockIdx.x, blockIdx.x + gridDim.x, ...: the steps of all of them
-// form one stream through an LDS ring of ST stages of codes and scale lines,
-// so that the next tile's first steps land while this one's last are
-// multiplied and its output is stored.
+// of it, WPE workgroups per compute unit.  A workgroup walks tiles blockIdx.x,
+// blockIdx.x + gridDim.x, ...: the steps of all of them form one stream
+// through an LDS ring of ST stages of codes and scale lines, so that the next
+// tile's first steps land while this one's last are multiplied and its output
+// is stored (10920 x 8960 x 1536: 133 us with a workgroup per tile, 101 so).
 //
-// Per 128 x 128 tile and step: 512 cycles of matrix instructions per SIMD, and
-// 1024 of LDS (34 KB of copies at 64 bytes a cycle, 64 KB of fragment reads at
-// 128), which bounds it.
+// What bounds it: per 128 x 128 tile and step, 512 cycles of matrix
+// instructions per SIMD and 1024 of LDS (34 KB of copies at 64 bytes a cycle,
+// 64 KB of fragment reads at 128); two workgroups per compute unit take about
+// 1200 (8192 x 8192 x 8192: 278-292 us, 3.8-3.95 PFLOP/s), one alone 1350.
+// Larger tiles do less LDS work per MFMA, but 256 x 256 leaves a wave alone on
+// its SIMD with 256 accumulators: 310-338 us for the same product, and no
+// second workgroup beside its epilogue.  Where there are few tiles, their
+// steps wait for memory, all workgroups being at the same place in K: four or
+// five stages then pay (1365 x 1536 x 8960, 132 tiles: 29.8 us with two
+// stages, 22.7 with four; 240 tiles of 96 x 96: 20).  K is not split: over
+// 216 shapes the best split of each was 0.07 % faster than the best whole one.
 template <int MB_, int NB_, int WPE_, int ST_>
 struct Shape {
     static constexpr int MB = MB_, NB = NB_, WPE = WPE_, ST = ST_;
@@ -416,7 +424,8 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
             acc[j % NB][j / NB] = mfma(fw[ks][j % NB], fa[ks][j / NB], acc[j % NB][j / NB], ks, sw[j % NB], sa[j / NB]);
     };
 
-    // The compiler would sink a half's MFMAs across the barrier and the branch of advance() to their last use.
+    // The compiler would sink a half's MFMAs across the barrier and the branch of advance() to their last use (10920 x
+    // 8960 x 1536: 111 us, pinned 101).
     auto pin = [&] {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -501,7 +510,7 @@ enum TileId : int32_t { kRows, kTile128x128, kTile128x128Deep, kTile96x96, kTile
 template <int MB, int W, bool QUANT>
 hipError_t launch_rows_t(const LinearArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.N / 16), (unsigned)((a.M + 16 * MB - 1) / (16 * MB))), block(64 * W);
+    const dim3 grid((unsigned)((a.M + 16 * MB - 1) / (16 * MB)), (unsigned)(a.N / 16)), block(64 * W);
     const int nk = steps_of(a.K);
     switch (a.epi) {
     case kEpiBias: hipLaunchKernelGGL((linear_rows_kernel<MB, W, kEpiBias, QUANT>), grid, block, 0, stream, a, nk); break;
@@ -605,7 +614,7 @@ int64_t linear_workspace(int M, int N, int K, bool quantized)
 hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream)
 {
     const int nk = steps_of(a.K);
-    const dim3 grid((unsigned)((nk + 1) / 2), (unsigned)((a.rows + 15) / 16)), block(256);
+    const dim3 grid((unsigned)((a.rows + 15) / 16), (unsigned)((nk + 1) / 2)), block(256);
     if (a.f32)
         hipLaunchKernelGGL(quantize_kernel<true>, grid, block, 0, stream, a, nk);
     else
@@ -615,7 +624,7 @@ hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream)
 
 hipError_t launch_dequantize(const DequantizeArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((a.K + 511) / 512), (unsigned)((a.rows + 3) / 4)), block(256);
+    const dim3 grid((unsigned)((a.rows + 3) / 4), (unsigned)((a.K + 511) / 512)), block(256);
     if (a.f32)
         hipLaunchKernelGGL(dequantize_kernel<true>, grid, block, 0, stream, a, steps_of(a.K));
     else

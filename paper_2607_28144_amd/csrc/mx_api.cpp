@@ -20,6 +20,8 @@ namespace mx = regenvc::mx;
 namespace {
 
 constexpr int32_t kMaxK = 1 << 20;
+constexpr int32_t kMaxN = 65535 * 16;               // 16 channels per workgroup, in the grid's second dimension
+constexpr int64_t kMaxOut = (int64_t)1 << 42;        // 2^30 tiles of 64 x 64
 
 regenvc_status done()
 {
@@ -32,8 +34,6 @@ regenvc_status check_matrix(const char *fn, int32_t rows, int32_t K)
     if (rows < 0 || K < 0) return failf(REGENVC_ERR_INVALID_ARG, "%s: negative size (rows=%d K=%d)", fn, rows, K);
     if (K % 8 != 0 || K > kMaxK)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: K=%d is not a multiple of 8, at most %d", fn, K, kMaxK);
-    // the kernels' grids: rows in their second dimension
-    if (rows > 65535 * 4) return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d rows, at most %d", fn, rows, 65535 * 4);
     return REGENVC_OK;
 }
 
@@ -54,8 +54,9 @@ regenvc_status check_linear_shape(const char *fn, int32_t M, int32_t N, int32_t 
     if (epi != REGENVC_EPI_BIAS && epi != REGENVC_EPI_BIAS_GELU && epi != REGENVC_EPI_GATED_RESIDUAL)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: unknown epilogue %d", fn, epi);
     if (N % 16 != 0) return failf(REGENVC_ERR_UNSUPPORTED, "%s: N=%d is not a multiple of 16", fn, N);
-    const regenvc_status st = check_matrix(fn, M, K);
-    return st != REGENVC_OK ? st : check_matrix(fn, N, K);
+    if (N > kMaxN || (int64_t)M * N > kMaxOut)
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: an output of %d x %d (N at most %d, M N at most 2^42)", fn, M, N, kMaxN);
+    return check_matrix(fn, M, K);
 }
 
 regenvc_status check_cache(const char *fn, const regenvc_mx_cache *c, Range (&r)[4])
@@ -107,8 +108,8 @@ regenvc_status check_attn_shape(const char *fn, int32_t B, int32_t H, int32_t he
     if (H > 0 && (heads == 0 || H % heads != 0))
         return failf(REGENVC_ERR_INVALID_ARG, "%s: H=%d is not a multiple of the cache's %d heads", fn, H, heads);
     int64_t rows = 0;
-    if (__builtin_mul_overflow((int64_t)Sq * H, (int64_t)std::max(B, 1), &rows) || rows > (int64_t)1 << 31)
-        return failf(REGENVC_ERR_UNSUPPORTED, "%s: B * Sq * H is more than 2^31", fn);
+    if (__builtin_mul_overflow((int64_t)Sq * H, (int64_t)std::max(B, 1), &rows) || rows > (int64_t)1 << 30)
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: B * Sq * H is more than 2^30", fn);
     return REGENVC_OK;
 }
 

@@ -146,14 +146,13 @@ def _row_vectors(groups: int, C: int, group_rows: int, idx: int, gate, scale, sh
         if t is None:
             ptrs.append(None)
             continue
-        if t.dim() == 1 and groups == 1:
+        if groups == 1:  # [C] or [1, C]
             ptrs.append(_lib.vector(t, name, torch.float32, C, idx))
             continue
         step = _lib.matrix(t, name, torch.float32, groups, C, idx)
-        if groups > 1:
-            if ld is not None and step != ld:
-                raise ValueError("gate, scale and shift must have one row stride")
-            ld = step
+        if ld is not None and step != ld:
+            raise ValueError("gate, scale and shift must have one row stride")
+        ld = step
         ptrs.append(t.data_ptr())
     return _lib.RowVectors(ptrs[0], ptrs[1], ptrs[2], C if ld is None else ld, group_rows)
 

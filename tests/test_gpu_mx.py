@@ -6,7 +6,7 @@ A linear layer's products are exact in fp32 (two-bit magnitudes under powers of
 two), so its error is that of adding K of them: at most one rounding per
 addition of a 128-deep partial sum, which itself is taken to be off by no more
 than 4 roundings, all relative to the sum of magnitudes:
-(2 * steps + 8 + split joins) * 2^-24 * sum |a||w|.  A bf16 output adds half a
+(2 * steps + 8 + joins of waves) * 2^-24 * sum |a||w|.  A bf16 output adds half a
 step, 2^-8 of the value; GELU has a slope of at most 1.13 and an exponential
 good to 1e-6.
 """
@@ -118,7 +118,7 @@ def check(name, got, ref, tol):
 
 
 # every kernel and its borders: one to 64 rows (few-row kernels, K in few and in many steps), tiles of
-# each shape, ragged rows and channels, K that ends inside a block, a half step and a step, splits of K
+# each shape, ragged rows and channels, K that ends inside a block, a half step and a step
 SHAPES = [(1, 16, 8), (1, 1536, 1536), (3, 48, 40), (16, 272, 264), (17, 272, 2312), (33, 1536, 1536), (64, 160, 8960),
           (65, 16, 8), (65, 144, 72), (130, 272, 256), (129, 400, 512), (300, 1552, 1544), (577, 1536, 768),
           (1365, 1536, 8960), (700, 8960, 1536), (2500, 1040, 1000)]

@@ -89,6 +89,8 @@ def test_linear_refusals(lib):
     refused(lib, UNS, "lda", call(lda=260))
     refused(lib, UNS, "ldo", call(ldo=56))
     refused(lib, UNS, "ldo", call(ldo=68))
+    refused(lib, UNS, "an output of", call(N=1 << 20, ldo=1 << 20))
+    refused(lib, UNS, "an output of", call(M=1 << 30, N=1 << 14, ldo=1 << 14))
     refused(lib, INV, "give a, or", call(ac=F))
     refused(lib, INV, "NULL", call(a=None, ac=F))
     refused(lib, INV, "NULL", call(wc=None))
@@ -187,7 +189,7 @@ def test_attention_plans(lib):
     refused(lib, INV, "n_cu", lib.regenvc_mx_attn_cache_plan_query(1, 1, 1, 1, 1, 64, 0, ctypes.byref(p)))
     refused(lib, INV, "NULL", lib.regenvc_mx_attn_cache_plan_query(1, 1, 1, 1, 1, 64, 256, None))
     refused(lib, INV, "multiple", lib.regenvc_mx_attn_cache_workspace(1, 3, 2, 1, 1, 64, 256, ctypes.byref(b)))
-    refused(lib, UNS, "2^31", lib.regenvc_mx_attn_cache_workspace(1 << 12, 1 << 10, 1, 1 << 10, 1, 64, 256, ctypes.byref(b)))
+    refused(lib, UNS, "2^30", lib.regenvc_mx_attn_cache_workspace(1 << 12, 1 << 10, 1, 1 << 10, 1, 64, 256, ctypes.byref(b)))
 
 
 def test_linear_plans(lib):
