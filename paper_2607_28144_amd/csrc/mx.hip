@@ -240,6 +240,21 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) uint16_t lds_u16;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
+// Where a row's eight chunks lie in its 128 bytes of a stage.  A fragment read
+// takes chunk 2 g + ks of 16 rows, for g = 0 .. 3; 16 of its lanes are served
+// at a time, of two neighbouring g, eight rows each: their chunks have to lie
+// an odd number of places apart, or they share banks with rows of the same
+// parity (a read of 12 cycles instead of 8).
+__device__ __forceinline__ int place_of(int row, int g, int ks)
+{
+    return (g + 4 * ks) ^ (row & 7);
+}
+__device__ __forceinline__ int chunk_at(int row, int place)
+{
+    const int p = place ^ (row & 7);
+    return (p & 3) * 2 + (p >> 2);
+}
+
 // A pointer that is the same in every lane, in scalar registers.
 __device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
 {
@@ -359,12 +374,12 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
 #pragma unroll
         for (int i = 0; i < AP; ++i) {
             const int r = (wave * AP + i) * 8 + (lane >> 3);
-            aoff[i] = (uint32_t)min(r, a.M - 1 - it.m0) * (uint32_t)ld + tile::swz(r, lane & 7) * 16;
+            aoff[i] = (uint32_t)min(r, a.M - 1 - it.m0) * (uint32_t)ld + chunk_at(r, lane & 7) * 16;
         }
 #pragma unroll
         for (int i = 0; i < WP; ++i) {
             const int r = (wave * WP + i) * 8 + (lane >> 3);
-            woff[i] = (uint32_t)min(r, a.N - 1 - it.n0) * (uint32_t)ld + tile::swz(r, lane & 7) * 16;
+            woff[i] = (uint32_t)min(r, a.N - 1 - it.n0) * (uint32_t)ld + chunk_at(r, lane & 7) * 16;
         }
         const int64_t rb = line < 2 * MB ? min((it.m0 >> 4) + line, (a.M - 1) >> 4)
                                          : min((it.n0 >> 4) + line - 2 * MB, (a.N - 1) >> 4);
@@ -399,10 +414,10 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
     auto rd = [&](int st, int ks, int f) {
         if (f < NB)
             fw[ks][f] = *(const lds_u32x4 *)(s + W0 + st * S::W_BYTES + (rw + f * 16) * kStepBytes +
-                                             tile::swz(rw, 2 * g + ks) * 16);
+                                             place_of(rw, g, ks) * 16);
         else
             fa[ks][f - NB] = *(const lds_u32x4 *)(s + st * S::A_BYTES + (ra + (f - NB) * 16) * kStepBytes +
-                                                  tile::swz(ra, 2 * g + ks) * 16);
+                                                  place_of(ra, g, ks) * 16);
     };
     auto rd_scale = [&](int st, int f) {
         const tile::lds_char *p = s + S0 + st * S::S_BYTES + lane * 2;

@@ -124,20 +124,23 @@ __device__ __forceinline__ float quad_sum(float x)
 }
 
 // 16-byte chunk of a V row in LDS (2 D bytes a row) where chunk c of key row r
-// is kept: pairs of chunks change places with the row, so that neither the
-// stores of whole blocks nor the transposing reads (4 rows by 32 bytes per 16
-// lanes) meet in a bank.
+// is kept: pairs of chunks change places with the row, so that the transposing
+// reads (32 bytes of each of 8 rows at a time) do not meet in a bank.
 template <int D>
 __device__ __forceinline__ int v_slot(int r, int c)
 {
-    return c ^ ((r & (D / 16 - 1)) << 1);
+    return c ^ ((D == 128 ? r & 7 : r >> 1 & 3) << 1);
 }
 
-// The same for K rows: the fragment reads take one chunk of each of 16 rows.
+// The same for K rows.  A fragment read takes chunk D / 32 g + ks of 16 rows,
+// served for rows 0-3, 12-15 of one g with rows 4-11 of the next (or the other
+// way round): their chunks, a block or half a block apart, are kept apart by
+// rows 4-11 counting in that bit too (1560 queries x 32760 places x 12 heads, 303
+// us: 301 so, with a third of the conflict cycles).
 template <int D>
 __device__ __forceinline__ int k_slot(int r, int c)
 {
-    return c ^ (D == 128 ? r & 15 : (r >> 1) & 7);
+    return c ^ (D == 128 ? (r & 15) ^ ((r + 4 & 8) >> 1) : (r >> 1 & 1) | (r & 4 ? 6 : 0));
 }
 
 // log2(e) times the softmax scale.  Never 0, so that -inf, the score of a
