@@ -182,7 +182,9 @@ __device__ __forceinline__ void row_stats(const Val &val, const bool (&on)[NV], 
     rstd = rsqrtf(row_sum<WPR>(q, lds, turn) * inv_c + eps);
 }
 
-// Forward: WPR waves per row, NV eight-channel chunks per lane.
+// Forward: WPR waves per row, NV eight-channel chunks per lane.  10920 x 1536,
+// norms on both sides, a modulation per 1560 rows: 40.9 us, 201 MB, 4.9 TB/s (a
+// 2 GiB copy: 4.9); one row: 3.6 us.
 template <int NV, int WPR, bool F32>
 __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(ResidualNormArgs a)
 {
@@ -292,6 +294,9 @@ __device__ __forceinline__ void join_stats(const Share *sh, int waves, int C, in
 // LDS, in a fixed order: no atomics.  NS: sums held (3, 4 with a post-norm, 5
 // with its bias).
 // WIDE: more than eight waves.
+// 10920 x 1536 without a post-norm: 62 us, 302 MB, 4.9 TB/s; 1560 x 2048 with
+// one: 18.4 us, 57 MB, 3.1: 512 workgroups of three rows, whose sums (12.6 MB)
+// come on top.
 template <bool F32, int NS, bool WIDE>
 __global__ __launch_bounds__(WIDE ? 1024 : 512) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : NS == 3 ? 3 : 2)))
 void residual_norm_bwd_kernel(ResidualNormArgs a, ResidualNormPlan p, float *group_ws,
@@ -484,7 +489,7 @@ void residual_norm_bwd_kernel(ResidualNormArgs a, ResidualNormPlan p, float *gro
 // The sums of segments and workgroups joined, in order: workgroup (c / 64, y)
 // adds, for job y, n rows of C that lie behind one another; 64 columns by 16
 // slices of the rows.  Jobs: for each sum over a group's rows and each group,
-// then for each sum over all rows.
+// then for each sum over all rows.  4 to 5 us, most of it a launch.
 struct ReduceArgs {
     const float *group_part, *row_part;
     float *group_out[3], *row_out[4];
