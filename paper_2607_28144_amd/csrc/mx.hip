@@ -211,15 +211,19 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
 // through an LDS ring of ST stages of codes and scale lines, so that the next
 // tile's first steps land while this one's last are multiplied and its output
 // is stored (10920 x 8960 x 1536: 133 us with a workgroup per tile, 101 so).
+// What a tile needs besides its steps is kept short: its place without
+// divisions, its biases from one wait (a branch and a wait for each of them cost
+// 2800 cycles a tile: 103 us, 97 without).
 //
 // What bounds it: per 128 x 128 tile and step, 512 cycles of matrix
 // instructions per SIMD and 1024 of LDS (34 KB of copies at 64 bytes a cycle,
 // 64 KB of fragment reads at 128); two workgroups per compute unit take about
 // 1000.  8192 x 8192 x 8192: 273-292 us, 3.8-4.0 PFLOP/s, with the matrix units
 // busy for 52 % of the cycles and the clock down to 1.79 GHz: the power limit.
-// 10920 x 8960 x 1536: 101 us, with GELU 115 (2.6 PFLOP/s): 47 us of it are the
-// 196 MB of output at the rate of a copy, and an exponential and a reciprocal
-// for each of 98 million values.  1365 x 1536 x 8960: 18.5 us (2.0 PFLOP/s).
+// 10920 x 8960 x 1536: 95 us, with GELU 109 (2.75 PFLOP/s), of which the epilogue
+// (196 MB of output; an exponential and a reciprocal for each of 98 million
+// values) takes 15 and 29: without it 80.  1365 x 1536 x 8960: 17.4 us (2.2
+// PFLOP/s).
 // Larger tiles do less LDS work per MFMA, but 256 x 256 leaves a wave alone on
 // its SIMD with 256 accumulators: 310-338 us for the same product, and no
 // second workgroup beside its epilogue.  Where there are few tiles, their
@@ -237,7 +241,7 @@ struct Shape {
     static constexpr int S_BYTES = S_COPIES * 1024;
     static constexpr int OUT = ST * (A_BYTES + W_BYTES + S_BYTES);  // where 16 rows of each wave's output are staged
     static constexpr int OUT_ROW = 16 * NB * 2;
-    static constexpr bool STAGED = NB == 4 && (OUT + 4 * 16 * OUT_ROW) * WPE <= 160 * 1024;  // else stored straight
+    static constexpr bool STAGED = NB == 4 && (OUT + 4 * 16 * OUT_ROW) * WPE <= 160 * 1024;
     static constexpr int LDS = OUT + (STAGED ? 4 * 16 * OUT_ROW : 0);
     static_assert(LDS * WPE <= 160 * 1024 && S_COPIES <= 4 && (!STAGED || NB == 4), "tile shape");
 };
@@ -269,80 +273,132 @@ __device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
     return reinterpret_cast<const uint8_t *>((uint64_t)hi << 32 | lo);
 }
 
-// The tiles of a launch, and the rows and channels that one begins at.
+// The tiles of a launch: tiles_m x tiles_n of them in groups of kGroupM row
+// blocks, in the order of tile::tile_of.  inv_group, inv_last: 2^32 / d rounded
+// down, for the sizes of a group and the row blocks of the last one; a division
+// by them is a high product and one correction, where the compiler's own (four
+// for an item, twice per tile) would take longer than a step.
 struct Tiles {
-    int nk, tiles_n, n_tiles;
+    int nk, tiles_n, n_tiles, groups;
+    uint32_t group, inv_group, last, inv_last;
 };
+__device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t d, uint32_t inv)  // n < 2^31
+{
+    const uint32_t q = __umulhi(n, inv);  // right, or one too small
+    return n - q * d >= d ? q + 1 : q;
+}
 struct Item {
     int m0, n0;
 };
 template <class S>
 __device__ __forceinline__ Item item_of(const Tiles &t, int id)
 {
-    int tm, tn;
-    tile::tile_of(id, t.tiles_n, t.n_tiles, tm, tn);
-    return Item{tm * S::BM, tn * S::BN};
+    const int xcd = id & 7;
+    const uint32_t tile = (uint32_t)(xcd * (t.n_tiles >> 3) + min(xcd, t.n_tiles & 7) + (id >> 3));
+    const uint32_t group = quotient(tile, t.group, t.inv_group), in = tile - group * t.group;
+    const bool whole = (int)group + 1 < t.groups;
+    const uint32_t gm = whole ? (uint32_t)tile::kGroupM : t.last;
+    const uint32_t tn = whole ? in / (uint32_t)tile::kGroupM : quotient(in, t.last, t.inv_last);
+    return Item{(int)(group * tile::kGroupM + in - tn * gm) * S::BM, (int)tn * S::BN};
 }
 
-// 16 rows of a wave's 64 channels at a time through its own LDS, so that each
-// store writes whole 16-byte chunks, 128 bytes of a row; f32 outputs (64 bytes
-// of a row per 16 channels) go straight from the accumulators.
-template <class S, int EPI>
-__device__ __forceinline__ void store_tile(const LinearArgs &a, const Item &it, char *smem, f32x4 (&acc)[S::NB][S::MB])
+// A lane's biases of a wave's channels n0 .. n0 + 16 NB - 1 (4 g .. 4 g + 3 of
+// each 16; those past the last channel, which are not stored, repeat others).
+template <int NB>
+__device__ __forceinline__ void load_bias(const LinearArgs &a, int n0, int g, u32x2 (&raw)[NB])
+{
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) raw[nb] = u32x2{0, 0};
+    if (a.bias == nullptr) return;
+    const uint16_t *p = static_cast<const uint16_t *>(a.bias) + 4 * g;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) raw[nb] = *reinterpret_cast<const u32x2 *>(p + min(n0 + nb * 16, a.N - 16));
+}
+
+// A wave's quarter of a tile from its accumulators: row x of 16, channels 4 g ..
+// 4 g + 3 of 16 in a lane.  f32 outputs go straight from there, 64 bytes of a row
+// per 16 channels.  bf16: 64 channels go 16 rows at a time through LDS of the
+// wave's own, so that a store writes 128 bytes of each of 8 rows, past the caches
+// (the next reader is another launch; left in L2 they are written when the kernel
+// ends: 10920 x 1536 x 1536 23.1 us, past it 20.8).  Fewer channels: lanes of
+// neighbouring g exchange halves of two blocks of 16, so that each has eight
+// channels of one; such stores, of 64 bytes or 32 of a row, are slower past the
+// caches (1365 x 1536 x 8960: 18.4 and 19.7).  WHOLE: no row or channel of the
+// tile lies past the last one.
+template <class S, int EPI, bool WHOLE>
+__device__ __forceinline__ void store_tile(const LinearArgs &a, int m0, int n0, const u32x2 (&raw)[S::NB], char *smem,
+                                           f32x4 (&acc)[S::NB][S::MB])
 {
     constexpr int MB = S::MB, NB = S::NB;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave >> 1, wn = wave & 1, g = lane >> 4, x = lane & 15;
-    const int m0 = it.m0 + wm * 16 * MB, n0 = it.n0 + wn * 16 * NB;
-    const uint16_t *bias = static_cast<const uint16_t *>(a.bias);
+    const int g = lane >> 4, x = lane & 15;
     f32x4 bv[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
-        bv[nb] = n0 + nb * 16 < a.N ? tile::load_bias4(bias, n0 + nb * 16 + 4 * g) : f32x4{0.f, 0.f, 0.f, 0.f};
-    if constexpr (EPI == kEpiGatedRes || !S::STAGED) {
+        bv[nb] = f32x4{__uint_as_float(raw[nb][0] << 16), __uint_as_float(raw[nb][0] & 0xffff0000u),
+                       __uint_as_float(raw[nb][1] << 16), __uint_as_float(raw[nb][1] & 0xffff0000u)};
+    auto round4 = [&](int nb, int mb) {
+        const f32x4 y = acc[nb][mb] + bv[nb];
+        bf16x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (__bf16)tile::activate<EPI>(y[i]);
+        return w;
+    };
+    if constexpr (EPI == kEpiGatedRes) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const int n = n0 + nb * 16 + 4 * g;
-            if (n0 + nb * 16 >= a.N) continue;
+            if (!WHOLE && n0 + nb * 16 >= a.N) continue;
             f32x4 gv = {1.f, 1.f, 1.f, 1.f};
-            if (EPI == kEpiGatedRes && a.gate != nullptr) gv = *reinterpret_cast<const f32x4 *>(a.gate + n);
+            if (a.gate != nullptr) gv = *reinterpret_cast<const f32x4 *>(a.gate + n);
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
                 const int m = m0 + mb * 16 + x;
-                if (m >= a.M) continue;
-                if constexpr (EPI == kEpiGatedRes) {
-                    f32x4 *p = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + (int64_t)m * a.ldo + n);
-                    *p = *p + gv * (acc[nb][mb] + bv[nb]);
-                } else {
-                    const f32x4 y = acc[nb][mb] + bv[nb];
-                    bf16x4 w;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = (__bf16)tile::activate<EPI>(y[i]);
-                    *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.out) + (int64_t)m * a.ldo + n) = w;
-                }
+                if (!WHOLE && m >= a.M) continue;
+                f32x4 *p = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + (int64_t)m * a.ldo + n);
+                *p = *p + gv * (acc[nb][mb] + bv[nb]);
             }
         }
-    } else {
+    } else if constexpr (S::STAGED) {
         tile::lds_char *stg = (tile::lds_char *)smem + S::OUT + wave * 16 * S::OUT_ROW;
+        const int r0 = lane >> 3, c = lane & 7;
+        uint16_t *p = static_cast<uint16_t *>(a.out) + (int64_t)(m0 + r0) * a.ldo + n0 + c * 8;
+        const int64_t rows8 = 8 * a.ldo;
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const f32x4 y = acc[nb][mb] + bv[nb];
-                bf16x4 w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = (__bf16)tile::activate<EPI>(y[i]);
-                *(lds_bf16x4 *)(stg + x * S::OUT_ROW + ((nb * 2 + g / 2) ^ (x & 7)) * 16 + (g & 1) * 8) = w;
-            }
+            for (int nb = 0; nb < NB; ++nb)
+                *(lds_bf16x4 *)(stg + x * S::OUT_ROW + ((nb * 2 + g / 2) ^ (x & 7)) * 16 + (g & 1) * 8) = round4(nb, mb);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int r = j * 8 + (lane >> 3), c = lane & 7;
-                const u32x4 v = *(const lds_u32x4 *)(stg + r * S::OUT_ROW + (c ^ (r & 7)) * 16);
-                const int m = m0 + mb * 16 + r, n = n0 + c * 8;
-                if (m < a.M && n < a.N)
-                    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + (int64_t)m * a.ldo + n) = v;
+                const u32x4 v = *(const lds_u32x4 *)(stg + (j * 8 + r0) * S::OUT_ROW + (c ^ r0) * 16);
+                if (WHOLE || (m0 + mb * 16 + j * 8 + r0 < a.M && n0 + c * 8 < a.N))
+                    __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+                p += rows8;
             }
+        }
+    } else {
+        uint16_t *p = static_cast<uint16_t *>(a.out) + (int64_t)(m0 + x) * a.ldo;
+        const int64_t rows16 = 16 * a.ldo;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            const bool row = WHOLE || m0 + mb * 16 + x < a.M;
+            u32x2 w[NB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) w[nb] = __builtin_bit_cast(u32x2, round4(nb, mb));
+#pragma unroll
+            for (int nb = 0; nb + 1 < NB; nb += 2) {
+                const auto lo = __builtin_amdgcn_permlane16_swap(w[nb][0], w[nb + 1][0], false, false);
+                const auto hi = __builtin_amdgcn_permlane16_swap(w[nb][1], w[nb + 1][1], false, false);
+                const int n = n0 + (nb + (g & 1)) * 16 + (g >> 1) * 8;
+                if (row && (WHOLE || n < a.N)) *reinterpret_cast<u32x4 *>(p + n) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+            }
+            if constexpr (NB % 2 != 0) {
+                const int n = n0 + (NB - 1) * 16 + 4 * g;
+                if (row && (WHOLE || n < a.N)) *reinterpret_cast<u32x2 *>(p + n) = w[NB - 1];
+            }
+            p += rows16;
         }
     }
 }
@@ -370,7 +426,8 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
     const int scopy = wave % S::S_COPIES;  // waves past the number of scale copies repeat one
     const uint32_t ls0 = __builtin_amdgcn_readfirstlane(lds0 + S0 + scopy * 1024);
     const int chunk = min(scopy * 64 + lane, S::S_CHUNKS - 1), line = chunk >> 3;
-    const uint8_t *abase, *wbase, *ssrc;
+    const uint8_t *abase, *wbase, *ssrc, *a_scales = a.a_scales, *w_scales = a.w_scales;
+    __asm__ volatile("" : "+s"(a_scales), "+s"(w_scales));
     uint32_t aoff[AP], woff[WP];
     int c_item = blockIdx.x, c_kt;
     auto aim = [&] {  // at item c_item
@@ -389,7 +446,7 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
         }
         const int64_t rb = line < 2 * MB ? min((it.m0 >> 4) + line, (a.M - 1) >> 4)
                                          : min((it.n0 >> 4) + line - 2 * MB, (a.N - 1) >> 4);
-        ssrc = (line < 2 * MB ? a.a_scales : a.w_scales) + rb * t.nk * 128 + (chunk & 7) * 16;
+        ssrc = (line < 2 * MB ? a_scales : w_scales) + rb * t.nk * 128 + (chunk & 7) * 16;
         c_kt = 0;
     };
     auto copy = [&](int l, int st) {  // copy l of the step aimed at, into stage st
@@ -475,10 +532,14 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
     int st = 0;
     for (int item = blockIdx.x; item < t.n_tiles; item += stride) {
         const Item it = item_of<S>(t, item);
+        const int m0 = it.m0 + wm * 16 * MB, n0 = it.n0 + wn * 16 * NB;
+        u32x2 raw[NB];
+        load_bias<NB>(a, n0, g, raw);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        __builtin_amdgcn_s_setprio(1);  // before the other workgroup's epilogue (10920 x 8960 x 1536: 97.4 us, 95.4 so)
         for (int kt = 0; kt < t.nk; ++kt) {
             const int st1 = st + 1 == ST ? 0 : st + 1;
             // first half; the second half's fragments are read beside it
@@ -496,6 +557,11 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
             __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((ST - 2) * NC) : "memory");
             __builtin_amdgcn_s_barrier();
             __asm__ volatile("" : : : "memory");
+            if (ST == 2 && kt == 0) {
+                // the biases have landed too: known here, the compiler does not wait for later copies where they are used
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) __asm__ volatile("" : "+v"(raw[nb]));
+            }
             // second half; beside it the next step's first fragments, and copies into this step's stage
 #pragma unroll
             for (int i = 0; i < NM; i += 2) {
@@ -516,7 +582,11 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
             next_scales();
             st = st1;
         }
-        store_tile<S, EPI>(a, it, smem, acc);
+        __builtin_amdgcn_s_setprio(0);
+        if (m0 + 16 * MB <= a.M && n0 + 16 * NB <= a.N)
+            store_tile<S, EPI, true>(a, m0, n0, raw, smem, acc);
+        else
+            store_tile<S, EPI, false>(a, m0, n0, raw, smem, acc);
     }
     tile::wait_all_copies();
 }
@@ -555,7 +625,10 @@ template <class S, int EPI>
 hipError_t launch_tile_t(const LinearArgs &a, hipStream_t stream)
 {
     const int tiles_n = tile::tiles_along(a.N, S::BN);
-    const Tiles t{steps_of(a.K), tiles_n, tile::tiles_along(a.M, S::BM) * tiles_n};
+    const int tiles_m = tile::tiles_along(a.M, S::BM), groups = tile::tiles_along(tiles_m, tile::kGroupM);
+    const uint32_t group = (uint32_t)(tile::kGroupM * tiles_n), last = (uint32_t)(tiles_m - (groups - 1) * tile::kGroupM);
+    const Tiles t{steps_of(a.K), tiles_n, tiles_m * tiles_n, groups, group, (uint32_t)(((uint64_t)1 << 32) / group),
+                  last, (uint32_t)((((uint64_t)1 << 32) - 1) / last)};
     const int grid = std::min(t.n_tiles, device_cu_count() * S::WPE);
     hipLaunchKernelGGL((linear_tile_kernel<S, EPI>), dim3((unsigned)grid), dim3(tile::kThreads4), 0, stream, a, t);
     return hipGetLastError();
