@@ -317,7 +317,8 @@ __device__ __forceinline__ void load_bias(const LinearArgs &a, int n0, int g, u3
 
 // A wave's quarter of a tile from its accumulators: row x of 16, channels 4 g ..
 // 4 g + 3 of 16 in a lane.  f32 outputs go straight from there, 64 bytes of a row
-// per 16 channels.  bf16: 64 channels go 16 rows at a time through LDS of the
+// per 16 channels; what they are added to is read a block of channels ahead
+// (10920 x 4608 x 1536: 112 us with each read waited for, 97 so).  bf16: 64 channels go 16 rows at a time through LDS of the
 // wave's own, so that a store writes 128 bytes of each of 8 rows, past the caches
 // (the next reader is another launch; left in L2 they are written when the kernel
 // ends: 10920 x 1536 x 1536 23.1 us, past it 20.8).  Fewer channels: lanes of
@@ -346,19 +347,28 @@ __device__ __forceinline__ void store_tile(const LinearArgs &a, int m0, int n0, 
         return w;
     };
     if constexpr (EPI == kEpiGatedRes) {
+        // a block of 16 channels' values are read while the one before is added and stored
+        float *p = static_cast<float *>(a.out) + (int64_t)(m0 + x) * a.ldo + n0 + 4 * g;
+        const int64_t rows16 = 16 * a.ldo;
+        auto live = [&](int nb, int mb) { return WHOLE || (m0 + mb * 16 + x < a.M && n0 + nb * 16 < a.N); };
+        f32x4 old[2][MB], gv[2];
+        auto fetch = [&](int nb) {
+            gv[nb & 1] = f32x4{1.f, 1.f, 1.f, 1.f};
+            if (a.gate != nullptr && (WHOLE || n0 + nb * 16 < a.N))
+                gv[nb & 1] = *reinterpret_cast<const f32x4 *>(a.gate + n0 + nb * 16 + 4 * g);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+                if (live(nb, mb)) old[nb & 1][mb] = *reinterpret_cast<const f32x4 *>(p + mb * rows16 + nb * 16);
+        };
+        fetch(0);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const int n = n0 + nb * 16 + 4 * g;
-            if (!WHOLE && n0 + nb * 16 >= a.N) continue;
-            f32x4 gv = {1.f, 1.f, 1.f, 1.f};
-            if (a.gate != nullptr) gv = *reinterpret_cast<const f32x4 *>(a.gate + n);
+            if (nb + 1 < NB) fetch(nb + 1);
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                const int m = m0 + mb * 16 + x;
-                if (!WHOLE && m >= a.M) continue;
-                f32x4 *p = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + (int64_t)m * a.ldo + n);
-                *p = *p + gv * (acc[nb][mb] + bv[nb]);
-            }
+            for (int mb = 0; mb < MB; ++mb)
+                if (live(nb, mb))
+                    *reinterpret_cast<f32x4 *>(p + mb * rows16 + nb * 16) =
+                        old[nb & 1][mb] + gv[nb & 1] * (acc[nb][mb] + bv[nb]);
         }
     } else if constexpr (S::STAGED) {
         tile::lds_char *stg = (tile::lds_char *)smem + S::OUT + wave * 16 * S::OUT_ROW;
@@ -675,17 +685,18 @@ TilePlan linear_plan(int M, int N, int K, int epi, int n_cu)
     const int nk = steps_of(K);
     if (few_rows(M, N) || K == 0) return TilePlan{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 16, nk > 8 ? 16 : 4};
     // Fitted to the times of 3240 launches (12 pairs of N and K from 256 to 8960, 18 row counts from 65 to 10920, three
-    // epilogues, every tile): the choice is on average 0.9 % slower than the best.
+    // epilogues, every tile): the choice is on average 0.1 % slower than the best, at most 8 %; fitted to half of the
+    // row counts, 0.3 to 0.7 % on the others.
     struct Cost {
         int32_t tile, bm, bn;
         double fixed[3], step, load, once;  // us per tile (by epilogue), per step, factor on whole rounds, per launch
     };
     static const Cost costs[] = {
-        {kTile128x128, 128, 128, {0.59, 1.43, 3.11}, 0.438, 1.26, 0.84},
-        {kTile128x128Deep, 128, 128, {1.61, 2.23, 3.93}, 0.390, 1.37, 0.0},
-        {kTile96x96, 96, 96, {1.67, 2.07, 2.58}, 0.305, 1.37, 0.5},
-        {kTile64x128, 64, 128, {1.12, 1.11, 1.96}, 0.303, 1.31, 1.02},
-        {kTile64x64, 64, 64, {0.60, 0.79, 1.35}, 0.186, 1.27, 1.55},
+        {kTile128x128, 128, 128, {0.446, 1.130, 3.261}, 0.398, 1.247, 0.58},
+        {kTile128x128Deep, 128, 128, {1.016, 1.677, 3.688}, 0.379, 1.292, 0.00},
+        {kTile96x96, 96, 96, {1.218, 1.352, 1.774}, 0.324, 1.314, 0.06},
+        {kTile64x128, 64, 128, {0.472, 0.928, 1.582}, 0.293, 1.089, 0.52},
+        {kTile64x64, 64, 64, {0.426, 0.399, 0.792}, 0.188, 1.095, 0.34},
     };
     const Cost *best = nullptr;
     double best_t = INFINITY;
