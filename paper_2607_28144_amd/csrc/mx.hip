@@ -24,18 +24,25 @@ namespace mx {
 namespace {
 
 // ---------------------------------------------------------------- to MXFP4 and back
+// eight values of a row as they are held between load and use
 template <bool F32>
-__device__ __forceinline__ void load8(const void *p, int64_t at, float (&x)[8])
+struct Raw8 {
+    f32x4 a, b;
+    __device__ float operator[](int i) const { return i < 4 ? a[i] : b[i - 4]; }
+};
+template <>
+struct Raw8<false> {
+    bf16x8 a;
+    __device__ float operator[](int i) const { return (float)a[i]; }
+};
+template <bool F32>
+__device__ __forceinline__ Raw8<F32> load8(const void *p, int64_t at)
 {
     if constexpr (F32) {
-        const float *q = static_cast<const float *>(p) + at;
-        const f32x4 a = *reinterpret_cast<const f32x4 *>(q), b = *reinterpret_cast<const f32x4 *>(q + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+        const f32x4 *q = reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + at);
+        return Raw8<F32>{q[0], q[1]};
     } else {
-        const bf16x8 a = *reinterpret_cast<const bf16x8 *>(static_cast<const uint16_t *>(p) + at);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
+        return Raw8<F32>{*reinterpret_cast<const bf16x8 *>(static_cast<const uint16_t *>(p) + at)};
     }
 }
 
@@ -51,19 +58,27 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a, int nk)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t r0 = (int64_t)blockIdx.x * 16;
     const int c = blockIdx.y * 512 + lane * 8;
-    float x[4][8];
+    // All loads before the first use, and without branches where there are 16 rows (10920 x 1536: 9.9 us with branches,
+    // 9.1 so); past the last column they repeat columns, which become zeros.
+    Raw8<F32> v[4] = {};
+    auto load = [&](int p) { v[p] = load8<F32>(a.x, (r0 + 4 * p + wave) * a.ldx + min(c, a.K - 8)); };
+    if (r0 + 16 <= a.rows) {
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const int64_t row = r0 + 4 * p + wave;
+        for (int p = 0; p < 4; ++p) load(p);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[p][i] = 0.f;
-        if (row < a.rows && c < a.K) load8<F32>(a.x, row * a.ldx + c, x[p]);
+        for (int p = 0; p < 4; ++p)
+            if (r0 + 4 * p + wave < a.rows) load(p);
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int64_t row = r0 + 4 * p + wave;
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = c < a.K ? v[p][i] : 0.f;
         uint32_t code;
-        const uint32_t byte = quantize_quad(x[p], code);
+        const uint32_t byte = quantize_quad(x, code);
         if ((lane & 3) == 0) sc[4 * p + wave][lane >> 2] = (uint8_t)byte;
         if (row < a.rows && c < nk * kStepK) *reinterpret_cast<uint32_t *>(a.codes + (row * nk) * kStepBytes + c / 2) = code;
     }
@@ -110,29 +125,37 @@ __device__ __forceinline__ f32x4 mfma(u32x4 w, u32x4 a, f32x4 c, int ks, uint32_
                    : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, av, c, 4, 4, 1, (int)ws, 1, (int)as);
 }
 
-// One block of 32 columns of a bf16 row, brought to MXFP4 by one lane: its
-// codes, and its scale byte.  Columns from K on are zeros.
-__device__ __forceinline__ uint32_t quantize_block(const uint16_t *row, int c, int K, u32x4 &codes)
-{
+// 32 columns of a bf16 row, from c on, as loaded by one lane (past the end the
+// last ones again), and brought to MXFP4: codes and scale byte.  Columns from K on
+// are zeros.
+struct Block32 {
     bf16x8 v[4];
+};
+__device__ __forceinline__ Block32 load_block(const uint16_t *row, int c, int K)
+{
+    Block32 b;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        v[j] = bf16x8{};
-        if (c + 8 * j < K) v[j] = *reinterpret_cast<const bf16x8 *>(row + c + 8 * j);
-    }
+    for (int j = 0; j < 4; ++j) b.v[j] = *reinterpret_cast<const bf16x8 *>(row + min(c + 8 * j, K - 8));
+    return b;
+}
+__device__ __forceinline__ uint32_t quantize_block(const Block32 &b, int c, int K, u32x4 &codes)
+{
+    float x[4][8];
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint((float)v[j][i]) & 0x7fffffffu);
+        for (int i = 0; i < 8; ++i) {
+            x[j][i] = c + 8 * j < K ? (float)b.v[j][i] : 0.f;
+            m = max(m, __float_as_uint(x[j][i]) & 0x7fffffffu);
+        }
     const uint32_t byte = scale_byte(m);
     const float inv = scale_inverse(byte);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)v[j][i] * inv;
-        codes[j] = byte == kNanScale ? 0u : encode8(x);
+        for (int i = 0; i < 8; ++i) x[j][i] *= inv;
+        codes[j] = byte == kNanScale ? 0u : encode8(x[j]);
     }
     return byte;
 }
@@ -141,14 +164,25 @@ __device__ __forceinline__ uint32_t quantize_block(const uint16_t *row, int c, i
 // is little of everything, so a workgroup takes 16 output channels and all
 // rows, its W waves taking the steps of K in turn; their sums meet in LDS.
 // QUANT: a is bf16 and each workgroup brings its rows to MXFP4 itself, in
-// registers.  blockIdx.x: tile of 16 MB rows.  1 x 1536 x 1536: 4.7 us, of which
-// an empty kernel has about 3 and the weights' bytes 0.3.
+// registers.  blockIdx.x: tile of 16 MB rows.  1 x 1536 x 1536: 3.8 us in a graph of
+// such calls, of which an empty kernel has about 2.5 and the weights' bytes 0.3;
+// what is left is latency, so that loads do not wait for one another (4.5 with
+// branches around them and the epilogue's loads at the end).  The next step's loads
+// ahead of a step's products gained nothing.
 template <int MB, int W, int EPI, bool QUANT>
 __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int nk)
 {
+    static_assert(W >= MB, "a thread joins the sums of four channels of a row at most");
     __shared__ f32x4 red[W][MB * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, x = lane & 15;
     const int n0 = blockIdx.y * 16, m0 = blockIdx.x * 16 * MB;
+    // what this thread's share of the epilogue reads
+    const int64_t m = m0 + wave * 16 + x;
+    const int n = n0 + 4 * g;
+    u32x2 bias = {0, 0};
+    f32x4 gate = {1.f, 1.f, 1.f, 1.f};
+    if (a.bias != nullptr) bias = *reinterpret_cast<const u32x2 *>(static_cast<const uint16_t *>(a.bias) + n);
+    if (EPI == kEpiGatedRes && a.gate != nullptr) gate = *reinterpret_cast<const f32x4 *>(a.gate + n);
     const uint8_t *wc = a.w_codes + (int64_t)(n0 + x) * nk * kStepBytes + g * 32;
     const uint8_t *wsc = a.w_scales + (int64_t)blockIdx.y * nk * 128 + lane * 2;
     f32x4 acc[MB];
@@ -166,8 +200,11 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
             uint32_t as;
             if constexpr (QUANT) {
                 const uint16_t *p = static_cast<const uint16_t *>(a.a) + row * a.lda;
-                as = quantize_block(p, kt * kStepK + 64 * g, a.K, f[0]);
-                as |= quantize_block(p, kt * kStepK + 64 * g + 32, a.K, f[1]) << 8;
+                const int c = kt * kStepK + 64 * g;
+                const Block32 b0 = load_block(p, c, a.K), b1 = load_block(p, c + 32, a.K);
+                __builtin_amdgcn_sched_barrier(0);
+                as = quantize_block(b0, c, a.K, f[0]);
+                as |= quantize_block(b1, c + 32, a.K, f[1]) << 8;
             } else {
                 const uint8_t *p = a.a_codes + (row * nk + kt) * kStepBytes + g * 32;
                 f[0] = *reinterpret_cast<const u32x4 *>(p);
@@ -182,25 +219,24 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) red[wave][mb * 64 + lane] = acc[mb];
     __syncthreads();
-    for (int t = threadIdx.x; t < MB * 64; t += 64 * W) {
-        f32x4 y = red[0][t];
+    if (wave >= MB || m >= a.M) return;
+    f32x4 part[W];
 #pragma unroll
-        for (int k = 1; k < W; ++k) y += red[k][t];
-        const int64_t m = m0 + (t >> 6) * 16 + (t & 15);
-        const int n = n0 + 4 * ((t & 63) >> 4);
-        if (m >= a.M) continue;
-        y += tile::load_bias4(static_cast<const uint16_t *>(a.bias), n);
-        if constexpr (EPI == kEpiGatedRes) {
-            f32x4 *q = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + m * a.ldo + n);
-            const f32x4 gv =
-                a.gate != nullptr ? *reinterpret_cast<const f32x4 *>(a.gate + n) : f32x4{1.f, 1.f, 1.f, 1.f};
-            *q = *q + gv * y;
-        } else {
-            bf16x4 o;
+    for (int k = 0; k < W; ++k) part[k] = red[k][threadIdx.x];
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 y = part[0];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = (__bf16)tile::activate<EPI>(y[i]);
-            *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.out) + m * a.ldo + n) = o;
-        }
+    for (int k = 1; k < W; ++k) y += part[k];
+    y += f32x4{__uint_as_float(bias[0] << 16), __uint_as_float(bias[0] & 0xffff0000u), __uint_as_float(bias[1] << 16),
+               __uint_as_float(bias[1] & 0xffff0000u)};
+    if constexpr (EPI == kEpiGatedRes) {
+        f32x4 *q = reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + m * a.ldo + n);
+        *q = *q + gate * y;
+    } else {
+        bf16x4 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = (__bf16)tile::activate<EPI>(y[i]);
+        *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.out) + m * a.ldo + n) = o;
     }
 }
 
@@ -683,7 +719,9 @@ static bool quantizes_itself(int M, int K)
 TilePlan linear_plan(int M, int N, int K, int epi, int n_cu)
 {
     const int nk = steps_of(K);
-    if (few_rows(M, N) || K == 0) return TilePlan{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 16, nk > 8 ? 16 : 4};
+    // waves along K: one step for each, but four where there are workgroups for all compute units without that
+    if (few_rows(M, N) || K == 0)
+        return TilePlan{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 16, nk > 8 ? 16 : nk > 4 && N / 16 <= n_cu ? 8 : 4};
     // Fitted to the times of 3240 launches (12 pairs of N and K from 256 to 8960, 18 row counts from 65 to 10920, three
     // epilogues, every tile): the choice is on average 0.1 % slower than the best, at most 8 %; fitted to half of the
     // row counts, 0.3 to 0.7 % on the others.
@@ -748,7 +786,8 @@ hipError_t launch_linear(const LinearArgs &args, hipStream_t stream)
     }
     const TilePlan p = linear_plan(a.M, a.N, a.K, a.epi, device_cu_count());
     switch (p.tile) {
-    case kRows: return p.waves == 16 ? launch_rows<16>(a, stream) : launch_rows<4>(a, stream);  // (K = 0: no steps, any M)
+    case kRows:  // (K = 0: no steps, any M)
+        return p.waves == 16 ? launch_rows<16>(a, stream) : p.waves == 8 ? launch_rows<8>(a, stream) : launch_rows<4>(a, stream);
     case kTile128x128: return launch_tile<Tile128x128>(a, stream);
     case kTile128x128Deep: return launch_tile<Tile128x128Deep>(a, stream);
     case kTile96x96: return launch_tile<Tile96x96>(a, stream);
