@@ -254,10 +254,11 @@ __device__ __forceinline__ void weights32(const f32x4 (&s)[2], float c, float m,
 // tiles of its own, 32 keys at a time, with nothing shared: K's codes go from
 // memory to registers and the matrix unit; V's through 2 D x 32 bytes of
 // wave-private LDS, for the transposition.  The waves' results meet in LDS.
-// One query against 10920 places, 12 heads of 128 (17.8 MB): 9.5 us; 12 rows
-// each of 16 sequences x 4 key heads of 64 (18.8 MB, 69050 places in all): 11.3:
-// 1.7-1.9 TB/s.  A wave has two or three tiles, so that the time is a chain of
-// latencies (lengths, queries, first codes, join), not the bytes.
+// With its join, in a graph of such calls: one query against 10920 places, 12 heads
+// of 128 (17.8 MB), 11.7 us; 12 rows each of 16 sequences x 4 key heads of 64 (18.8
+// MB, 69050 places in all) 13.6; a query of each of 8 sequences of 10920 places x 12
+// heads (143 MB) 32, 4.5 TB/s; of 64 (1.14 GB) 193, 5.9 TB/s.  For few bytes the
+// time is a chain of latencies (lengths, queries, first codes, join).
 constexpr int kFewWaves = 4;
 
 template <int D, int MB>
@@ -291,7 +292,10 @@ void attn_few_kernel(AttnCacheArgs a, AttnCachePlan p)
     const uint8_t *ks = a.c.k_scales + head * NBLK, *vs = a.c.v_scales + head * NBLK;
 
     // this lane's pieces of a tile: of K, rows x and 16 + x, D / 8 bytes from D / 8 g on;
-    // of V, one block (16 bytes) of keys lane / NBLK + 64 / NBLK j.  Keys past the end: zeros.
+    // of V, one block (16 bytes) of keys lane / NBLK + 64 / NBLK j.  Past the end the last
+    // key again, with no weight: loads without branches are counted, and those of the next
+    // tile not waited for (8 sequences of 10920 places, a query each: 40.5 us, 36.1 so; two
+    // tiles ahead 35.8, but one query against 32760 17.9 instead of 17.1).
     constexpr int VK = 64 / NBLK, NVJ = 32 / VK;
     struct Piece {
         u32x4 kcode[2], vcode[NVJ];
@@ -300,35 +304,27 @@ void attn_few_kernel(AttnCacheArgs a, AttnCachePlan p)
     auto load = [&](Piece &t, int key0) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int key = key0 + 16 * j + x;
-            t.kcode[j] = u32x4{0, 0, 0, 0};
-            t.kscale[j] = 127;
-            if (key < w.k1) {
-                if constexpr (D == 128) {
-                    t.kcode[j] = *reinterpret_cast<const u32x4 *>(kc + (int64_t)key * 64 + g * 16);
-                } else {
-                    const u32x2 c2 = *reinterpret_cast<const u32x2 *>(kc + (int64_t)key * 32 + g * 8);
-                    t.kcode[j][0] = c2[0], t.kcode[j][1] = c2[1];
-                }
-                t.kscale[j] = ks[(int64_t)key * NBLK + g * NBLK / 4];
+            const int64_t key = min(key0 + 16 * j + x, w.k1 - 1);
+            if constexpr (D == 128) {
+                t.kcode[j] = *reinterpret_cast<const u32x4 *>(kc + key * 64 + g * 16);
+            } else {
+                const u32x2 c2 = *reinterpret_cast<const u32x2 *>(kc + key * 32 + g * 8);
+                t.kcode[j] = u32x4{c2[0], c2[1], 0, 0};
             }
+            t.kscale[j] = ks[key * NBLK + g * NBLK / 4];
         }
 #pragma unroll
         for (int j = 0; j < NVJ; ++j) {
-            const int key = key0 + lane / NBLK + VK * j;
-            t.vcode[j] = u32x4{0, 0, 0, 0};
-            t.vscale[j] = 127;
-            if (key < w.k1) {
-                t.vcode[j] = *reinterpret_cast<const u32x4 *>(vc + (int64_t)key * (D / 2) + lane % NBLK * 16);
-                t.vscale[j] = vs[(int64_t)key * NBLK + lane % NBLK];
-            }
+            const int64_t key = min(key0 + lane / NBLK + VK * j, w.k1 - 1);
+            t.vcode[j] = *reinterpret_cast<const u32x4 *>(vc + key * (D / 2) + lane % NBLK * 16);
+            t.vscale[j] = vs[key * NBLK + lane % NBLK];
         }
     };
     lds_char *vl = (lds_char *)smem + wave * V_BYTES;
     const int step = 32 * kFewWaves;
     int key0 = w.k0 + 32 * wave;
     Piece cur, nxt;
-    load(cur, key0);
+    if (key0 < w.k1) load(cur, key0);
     for (; key0 < w.k1; key0 += step) {
         load(nxt, key0 + step);  // in flight beside this tile
         // V to LDS as bf16
@@ -733,10 +729,11 @@ void attn_many_kernel(AttnCacheArgs a, AttnCachePlan p)
 }
 
 // The key ranges' partial results joined, in order.  Up to kFewRanges of them:
-// D / 4 lanes per (query, head); HBM- or cache-bound (3 ranges of 1560 x 12 x 128
-// in f32: 9 us, 34 MB).
+// D / 4 lanes per (query, head), R >= ranges of them read at once (8 ranges of one
+// query: 2.1 us less than one by one).  HBM- or cache-bound where there are many rows
+// (3 ranges of 1560 x 12 x 128 in f32: 9 us, 34 MB).
 constexpr int kFewRanges = 8;
-template <int D>
+template <int D, int R>
 __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnCacheArgs a, int ranges)
 {
     constexpr int LPR = D / 4;
@@ -744,15 +741,24 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnCacheArgs a, int
     if (id >= (int64_t)a.B * a.Sq * a.H) return;
     const int d = threadIdx.x % LPR * 4;
     const int64_t h = id % a.H, s = id / a.H % a.Sq, b = id / ((int64_t)a.H * a.Sq);
-    float m = -INFINITY;
-    for (int k = 0; k < ranges; ++k) m = fmaxf(m, *part_lse(a, ranges, k, b, s, h));
+    float lse[R];
+    f32x4 part[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {  // past the last range that again, with no weight
+        lse[k] = *part_lse(a, ranges, min(k, ranges - 1), b, s, h);
+        part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, min(k, ranges - 1), b, s, h) + d);
+    }
+    float m = lse[0];
+#pragma unroll
+    for (int k = 1; k < R; ++k) m = fmaxf(m, lse[k]);
     m = m == -INFINITY ? 0.f : m;
     float l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < ranges; ++k) {
-        const float f = __builtin_amdgcn_exp2f(*part_lse(a, ranges, k, b, s, h) - m);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const float f = k < ranges ? __builtin_amdgcn_exp2f(lse[k] - m) : 0.f;
         l += f;
-        o += *reinterpret_cast<const f32x4 *>(part_o(a, k, b, s, h) + d) * f;
+        o += part[k] * f;
     }
     store_out4(a, b, s, h, d, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.0f / l));
     if (d == 0 && a.lse != nullptr)
@@ -819,9 +825,13 @@ hipError_t launch_attn_t(const AttnCacheArgs &a, const AttnCachePlan &p, hipStre
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.key_ranges == 1) return e;
     const int64_t rows = (int64_t)a.B * a.Sq * a.H;
-    if (p.key_ranges <= kFewRanges)
-        hipLaunchKernelGGL((attn_join_few_kernel<D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, stream, a,
-                           p.key_ranges);
+    const dim3 few((unsigned)((rows * (D / 4) + 255) / 256));
+    if (p.key_ranges <= 2)
+        hipLaunchKernelGGL((attn_join_few_kernel<D, 2>), few, dim3(256), 0, stream, a, p.key_ranges);
+    else if (p.key_ranges <= 4)
+        hipLaunchKernelGGL((attn_join_few_kernel<D, 4>), few, dim3(256), 0, stream, a, p.key_ranges);
+    else if (p.key_ranges <= kFewRanges)
+        hipLaunchKernelGGL((attn_join_few_kernel<D, kFewRanges>), few, dim3(256), 0, stream, a, p.key_ranges);
     else
         hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)rows), dim3(256), 0, stream, a, p.key_ranges);
     return hipGetLastError();
@@ -836,9 +846,13 @@ AttnCachePlan attn_cache_plan(int B, int H, int heads, int Sq, int max_len, int 
     p.tile_rows = rows <= 16 ? 16 : rows <= 128 ? 32 : kManyRows;
     p.row_tiles = (int32_t)((rows + p.tile_rows - 1) / p.tile_rows);
     const int64_t units = (int64_t)B * heads * p.row_tiles;
-    // workgroups side by side; a range is at least two rounds of a workgroup's waves
-    const int64_t slots = p.tile_rows == kManyRows ? n_cu : (int64_t)n_cu * (p.tile_rows == 16 ? 4 : 2);
-    const int64_t most = std::max<int64_t>(1, max_len / (p.tile_rows == kManyRows ? 512 : 256));
+    // As many ranges as fill the compute units, with two workgroups of 16 rows or one of more each (measured at 3120 and
+    // 10920 places, 12 to 64 units: more cost up to a fifth, for the joining), of at least two rounds of a workgroup's
+    // waves; few rows against few places are not cut, which saves the joining launch: at 768 places 7.5 us against 7.6 in
+    // 3 ranges with D = 128, at 1024 6.8 against 7.2 in 4 with D = 64.
+    const bool many = p.tile_rows == kManyRows;
+    const int64_t slots = (int64_t)n_cu * (p.tile_rows == 16 ? 2 : 1);
+    const int64_t most = many ? max_len / 512 : (int64_t)max_len * (D + 128) <= 768 * 256 ? 1 : max_len / 256;
     p.key_ranges = (int32_t)std::max<int64_t>(1, std::min({slots / std::max<int64_t>(1, units), most, (int64_t)64}));
     p.ws_bytes = p.key_ranges > 1 ? p.key_ranges * ((int64_t)B * Sq * H * (D + 1)) * (int64_t)sizeof(float) : 0;
     return p;
