@@ -83,11 +83,16 @@ __global__ __launch_bounds__(256) void values_kernel(ValuesArgs a)
     const int64_t b = blockIdx.y;
     const uint32_t chunk = id % per, th = id / per, place = th / (uint32_t)a.c.heads, h = th - place * a.c.heads;
     const int64_t token = (b * a.c.heads + h) * a.c.capacity + place;
+    uint32_t code[2], byte[2];  // both before the first store, which the compiler would not move a load across
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
-        const uint32_t code = *reinterpret_cast<const uint32_t *>((v ? a.c.v_codes : a.c.k_codes) + token * (D / 2) + chunk * 4);
-        const float s = scale_value((v ? a.c.v_scales : a.c.k_scales)[token * (D / 32) + chunk / 4]);
-        const bf16x8 x = decode8(code, 1.0f);
+        code[v] = *reinterpret_cast<const uint32_t *>((v ? a.c.v_codes : a.c.k_codes) + token * (D / 2) + chunk * 4);
+        byte[v] = (v ? a.c.v_scales : a.c.k_scales)[token * (D / 32) + chunk / 4];
+    }
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        const float s = scale_value(byte[v]);
+        const bf16x8 x = decode8(code[v], 1.0f);
         const int64_t at = (b * n + id) * 8;
         if constexpr (F32) {
             float *o = static_cast<float *>(v ? a.v : a.k) + at;

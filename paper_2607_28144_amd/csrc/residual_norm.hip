@@ -372,6 +372,8 @@ void residual_norm_bwd_kernel(ResidualNormArgs a, ResidualNormPlan p, float *gro
         const int64_t n = min((int64_t)a.group_rows, a.rows - gr0);
         const int64_t r0 = gr0 + n * part / p.per_group, r1 = gr0 + n * (part + 1) / p.per_group;
         const int64_t gv = (int64_t)group * a.ldv;
+        RowIn<F32> next;
+        load(next, r0 + slot, r0 + slot < r1);
         // the vectors stay in registers too: a load of them within a row would wait, as loads return in order, for the
         // next row's
         F8 mul{}, gate{};
@@ -381,8 +383,6 @@ void residual_norm_bwd_kernel(ResidualNormArgs a, ResidualNormPlan p, float *gro
             gate = vec_f32(a.gate, gv + c, 1.f);
             if constexpr (POST) pw = raw_bf16(a.post.w, c, 1.f), pb = raw_bf16(a.post.b, c, 0.f);
         }
-        RowIn<F32> next;
-        load(next, r0 + slot, r0 + slot < r1);
         for (int64_t rr = r0; rr < r1; rr += R) {  // the same number of rounds, and of barriers, for all R rows
             const int64_t row = rr + slot;
             const bool valid = row < r1;
