@@ -31,8 +31,8 @@
 extern "C" {
 #endif
 
-/* Bytes of the codes and of the scales of a matrix [rows, K].  K is taken in
-   steps of 256 columns, the last one filled up with zeros.
+/* Bytes of the codes and of the scales of a matrix [rows, K], rows below 2^26.
+   K is taken in steps of 256 columns, the last one filled up with zeros.
      codes:  row-major, 128 bytes a step; column 2 i of a row in the low half
              of its byte i
      scales: for every 16 rows (the last ones filled up) and every step a line
@@ -60,7 +60,8 @@ regenvc_status regenvc_mx_dequantize(const void *codes, const void *scales, void
      w_codes, w_scales: [N, K] in MXFP4
      bias, gate, out, ldo, epilogue: as regenvc_linear_fwd
    M, N, K >= 0; K a multiple of 8, at most 2^20; N a multiple of 16, below
-   2^20; M N at most 2^42; pointers 16-byte aligned.  workspace: 256-byte aligned, at least
+   2^20; M below 2^26, M N at most 2^42; pointers 16-byte aligned.  workspace:
+   256-byte aligned, at least
    regenvc_mx_linear_workspace bytes (a's codes and scales; NULL if that is 0).
    The kernel, chosen by size, sets the order of the fp32 sum: a row may come
    out a rounding apart in calls of different numbers of rows. */
@@ -79,7 +80,7 @@ regenvc_status regenvc_mx_linear_plan_query(int32_t M, int32_t N, int32_t K, int
 /* A key/value cache of B sequences of `heads` key heads and `capacity` places,
    in caller memory: codes [B, heads, capacity, D / 2] (channel 2 i of a place
    in the low half of its byte i) and scales [B, heads, capacity, D / 32],
-   contiguous, codes 16-byte aligned.  D in {64, 128}.  A place is a token's
+   contiguous, codes 16-byte aligned.  D in {64, 128}, capacity at most 2^30.  A place is a token's
    keys and values; their order has no meaning (attention is unmasked; position
    is in the rotated keys), so a cache may be rolled over. */
 typedef struct {
@@ -107,7 +108,8 @@ regenvc_status regenvc_mx_cache_values(const regenvc_mx_cache *cache, void *k, v
            for all.  A sequence without a place gives O = 0, LSE = -inf.
      max_len: what the work is planned for, 0 <= max_len <= capacity; lens
            beyond it are computed right, only less evenly
-   What lies behind lens[b] is not read.  workspace: 256-byte aligned, at least
+   What lies behind lens[b] is not read.  B Sq H is at most 2^29, B times the
+   cache's heads below 2^22.  workspace: 256-byte aligned, at least
    regenvc_mx_attn_cache_workspace bytes (NULL if that is 0). */
 regenvc_status regenvc_mx_attn_cache_fwd(const regenvc_tensor *q, const regenvc_mx_cache *cache, const int32_t *lens,
                                          int32_t max_len, const regenvc_tensor *o, regenvc_dtype o_dtype, float *lse,

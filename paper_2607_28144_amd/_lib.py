@@ -230,11 +230,12 @@ def index_of(t, name: str) -> int:
 
 
 def matrix(t, name: str, dtype, rows: int, cols: int, idx: int) -> int:
-    """The row stride of a [rows, cols] tensor of this type on device idx; refuses any other."""
+    """The row stride of a [rows, cols] tensor of this type on device idx; refuses any other.  (Of a single row, whose
+    stride torch leaves to chance: cols.)"""
     s, st = t.shape, t.stride()
     if t.dtype is dtype and t.get_device() == idx and len(st) == 2 and s[0] == rows and s[1] == cols \
             and (st[1] == 1 or cols <= 1):
-        return st[0]
+        return st[0] if rows > 1 else cols
     raise ValueError(f"{name} must be a {dtype} tensor [{rows}, {cols}] with unit column stride on cuda:{idx}, got "
                      f"{t.dtype} {tuple(s)} on {t.device}")
 

@@ -22,6 +22,8 @@ namespace {
 constexpr int32_t kMaxK = 1 << 20;
 constexpr int32_t kMaxN = 65535 * 16;               // 16 channels per workgroup, in the grid's second dimension
 constexpr int64_t kMaxOut = (int64_t)1 << 42;        // 2^30 tiles of 64 x 64
+constexpr int32_t kMaxRows = 1 << 26;                // 2^32 threads at a wave per row
+constexpr int32_t kMaxPlaces = 1 << 30;              // a tile past the last place stays within int32
 
 regenvc_status done()
 {
@@ -34,6 +36,7 @@ regenvc_status check_matrix(const char *fn, int32_t rows, int32_t K)
     if (rows < 0 || K < 0) return failf(REGENVC_ERR_INVALID_ARG, "%s: negative size (rows=%d K=%d)", fn, rows, K);
     if (K % 8 != 0 || K > kMaxK)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: K=%d is not a multiple of 8, at most %d", fn, K, kMaxK);
+    if (rows >= kMaxRows) return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d rows, must be below %d", fn, rows, kMaxRows);
     return REGENVC_OK;
 }
 
@@ -66,6 +69,8 @@ regenvc_status check_cache(const char *fn, const regenvc_mx_cache *c, Range (&r)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: negative cache size (B=%d capacity=%d heads=%d)", fn, c->B, c->capacity,
                      c->heads);
     if (c->D != 64 && c->D != 128) return failf(REGENVC_ERR_UNSUPPORTED, "%s: head dim D=%d (only 64 and 128)", fn, c->D);
+    if (c->capacity > kMaxPlaces)
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: a capacity of %d, at most %d", fn, c->capacity, kMaxPlaces);
     int64_t n = 0;
     if (__builtin_mul_overflow((int64_t)c->B * c->heads, (int64_t)c->capacity, &n) || n > INT64_MAX / 512)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: the cache's offsets overflow int64", fn);
@@ -107,9 +112,13 @@ regenvc_status check_attn_shape(const char *fn, int32_t B, int32_t H, int32_t he
     if (D != 64 && D != 128) return failf(REGENVC_ERR_UNSUPPORTED, "%s: head dim D=%d (only 64 and 128)", fn, D);
     if (H > 0 && (heads == 0 || H % heads != 0))
         return failf(REGENVC_ERR_INVALID_ARG, "%s: H=%d is not a multiple of the cache's %d heads", fn, H, heads);
+    if (max_len > kMaxPlaces)
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: max_len=%d, at most %d", fn, max_len, kMaxPlaces);
+    // a launch has less than 2^32 threads: 256 per 16 or 32 rows that share a key head, 512 per 256 of more than 128
     int64_t rows = 0;
-    if (__builtin_mul_overflow((int64_t)Sq * H, (int64_t)std::max(B, 1), &rows) || rows > (int64_t)1 << 30)
-        return failf(REGENVC_ERR_UNSUPPORTED, "%s: B * Sq * H is more than 2^30", fn);
+    if (__builtin_mul_overflow((int64_t)Sq * H, (int64_t)std::max(B, 1), &rows) || rows > (int64_t)1 << 29 ||
+        (int64_t)B * heads >= (int64_t)1 << 22)
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: B * Sq * H is more than 2^29, or B * heads 2^22 or more", fn);
     return REGENVC_OK;
 }
 

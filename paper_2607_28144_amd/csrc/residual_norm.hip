@@ -193,8 +193,9 @@ __device__ __forceinline__ void row_stats(const Val &val, const bool (&on)[NV], 
 }
 
 // Forward: WPR waves per row, NV eight-channel chunks per lane.  10920 x 1536,
-// norms on both sides, a modulation per 1560 rows: 35 us, 201 MB, 5.7 TB/s (a 2
-// GiB copy: 4.9); one row: 3.6 us.
+// norms on both sides, a modulation per 1560 rows, 201 MB: 35 us where two sets of
+// rows take turns, 41 with three (5.7 and 4.9 TB/s; a 2 GiB copy: 4.9); one row:
+// 3.6 us.
 template <int NV, int WPR, bool F32>
 __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(ResidualNormArgs a)
 {
@@ -304,7 +305,7 @@ __device__ __forceinline__ void join_stats(const Share *sh, int waves, int C, in
 // LDS, in a fixed order: no atomics.  NS: sums held (3, 4 with a post-norm, 5
 // with its bias).
 // WIDE: more than eight waves.
-// 10920 x 1536 without a post-norm: 60 us, 302 MB, 5.0 TB/s; 1560 x 2048 with
+// 10920 x 1536 without a post-norm: 59 us, 302 MB, 5.1 TB/s; 1560 x 2048 with
 // one: 18.4 us, 57 MB, 3.1: 512 workgroups of three rows, whose sums (12.6 MB)
 // come on top.
 template <bool F32, int NS, bool WIDE>

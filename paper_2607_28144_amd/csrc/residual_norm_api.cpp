@@ -44,6 +44,9 @@ regenvc_status check_common(const char *fn, regenvc_dtype dtype, const regenvc_n
                             const regenvc_row_vectors *v, float alpha, int32_t rows, int32_t C, bool backward)
 {
     if (rows < 0) return failf(REGENVC_ERR_INVALID_ARG, "%s: rows=%d < 0", fn, rows);
+    // a launch has less than 2^32 threads: a wave per row, or four
+    if (rows >= 1 << (C <= 2048 ? 26 : 24))
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d rows, must be below 2^26 (2^24 with more than 2048 channels)", fn, rows);
     if (C < 8 || C % 8 != 0 || C > 8192)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: C=%d is not a multiple of 8 in [8, 8192]", fn, C);
     if (dtype != REGENVC_BF16 && dtype != REGENVC_F32) return failf(REGENVC_ERR_INVALID_ARG, "%s: dtype %d", fn, dtype);

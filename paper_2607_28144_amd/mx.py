@@ -158,11 +158,15 @@ class KvCache:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         shape = (self.batch, self.heads, self.capacity)
-        self.k_codes, self.v_codes = (torch.zeros(*shape, D // 2, dtype=torch.uint8, device=self.device) for _ in range(2))
-        self.k_scales, self.v_scales = (torch.zeros(*shape, D // 32, dtype=torch.uint8, device=self.device)
-                                        for _ in range(2))
-        self._c = _lib.MxCache(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
-                               self.v_scales.data_ptr(), self.batch, self.capacity, self.heads, self.D)
+        self._parts = tuple(torch.zeros(*shape, n, dtype=torch.uint8, device=self.device)
+                            for n in (D // 2, D // 32, D // 2, D // 32))
+        self._c = _lib.MxCache(*(t.data_ptr() for t in self._parts), self.batch, self.capacity, self.heads, self.D)
+
+    # read-only: the addresses of the four tensors are in what the calls get
+    k_codes = property(lambda self: self._parts[0])
+    k_scales = property(lambda self: self._parts[1])
+    v_codes = property(lambda self: self._parts[2])
+    v_scales = property(lambda self: self._parts[3])
 
     def append(self, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
                count: Optional[torch.Tensor] = None) -> None:

@@ -182,3 +182,21 @@ def test_gradients_of_the_seams():
             if z is not None:
                 near(f"{n}", z, ref[n], (2.0 ** -15 + S * 2.0 ** -24) * ref[f"|{n}|"] + (BF * np.abs(ref[n]) if n == "dy" else 0)
                      + 1e-30)
+
+
+def test_a_row_of_any_stride():
+    """A single row's stride, which torch leaves to chance, is not looked at."""
+    s = Step()
+    a = s.r(C)
+    odd = torch.as_strided(a, (1, C), (1, 1))
+    assert torch.equal(s.mx.linear_fwd(odd, s.q["o"]), s.mx.linear_fwd(a.view(1, C), s.q["o"]))
+    x = torch.as_strided(s.r(C, dtype=torch.float32), (1, C), (3, 1))
+    for got, ref in zip(s.dit.residual_norm_fwd(x, odd), s.dit.residual_norm_fwd(x.clone(), a.view(1, C))):
+        assert torch.equal(got, ref)
+
+
+def test_cache_tensors_stay():
+    s = Step()
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        with pytest.raises(AttributeError):
+            setattr(s.cache, name, getattr(s.cache, name).clone())

@@ -90,6 +90,7 @@ def test_linear_refusals(lib):
     refused(lib, UNS, "ldo", call(ldo=56))
     refused(lib, UNS, "ldo", call(ldo=68))
     refused(lib, UNS, "an output of", call(N=1 << 20, ldo=1 << 20))
+    refused(lib, UNS, "rows, must be below", call(M=1 << 26))
     refused(lib, UNS, "an output of", call(M=1 << 30, N=1 << 14, ldo=1 << 14))
     refused(lib, INV, "give a, or", call(ac=F))
     refused(lib, INV, "NULL", call(a=None, ac=F))
@@ -137,6 +138,7 @@ def test_append_refusals(lib):
     refused(lib, INV, "overlaps", call(cache(vs=F)))
     refused(lib, UNS, "4-byte", call(start=T3 + 2))
     refused(lib, INV, "overlaps", call(start=I))
+    refused(lib, UNS, "a capacity of", call(cache(cap=(1 << 30) + 1)))
     refused(lib, INV, "cache is NULL", lib.regenvc_mx_cache_append(None, k, v, 5, None, None, None))
     assert call(S=0) == 0 and call(cache(B=0, k=None, ks=None, v=None, vs=None)) == 0
     refused(lib, INV, "overlap", lib.regenvc_mx_cache_values(cache(), T1, T1, 1, None))
@@ -189,7 +191,9 @@ def test_attention_plans(lib):
     refused(lib, INV, "n_cu", lib.regenvc_mx_attn_cache_plan_query(1, 1, 1, 1, 1, 64, 0, ctypes.byref(p)))
     refused(lib, INV, "NULL", lib.regenvc_mx_attn_cache_plan_query(1, 1, 1, 1, 1, 64, 256, None))
     refused(lib, INV, "multiple", lib.regenvc_mx_attn_cache_workspace(1, 3, 2, 1, 1, 64, 256, ctypes.byref(b)))
-    refused(lib, UNS, "2^30", lib.regenvc_mx_attn_cache_workspace(1 << 12, 1 << 10, 1, 1 << 10, 1, 64, 256, ctypes.byref(b)))
+    refused(lib, UNS, "2^29", lib.regenvc_mx_attn_cache_workspace(1 << 12, 1 << 10, 1, 1 << 10, 1, 64, 256, ctypes.byref(b)))
+    refused(lib, UNS, "2^22", lib.regenvc_mx_attn_cache_workspace(1 << 20, 4, 4, 1, 1, 64, 256, ctypes.byref(b)))
+    refused(lib, UNS, "max_len", lib.regenvc_mx_attn_cache_workspace(1, 1, 1, 1, (1 << 30) + 1, 64, 256, ctypes.byref(b)))
 
 
 def test_linear_plans(lib):
@@ -217,6 +221,8 @@ def test_residual_norm_refusals(lib):
         return lib.regenvc_residual_norm_fwd(a["x"], a["ldx"], a["y"], a["ldy"], a["t"], a["post"], a["pre"], a["v"],
                                              a["alpha"], a["xo"], a["ldxo"], a["h"], a["ldh"], a["rows"], a["C"], None)
     refused(lib, INV, "rows=-1", fwd(rows=-1))
+    refused(lib, UNS, "must be below", fwd(rows=1 << 26))
+    refused(lib, UNS, "must be below", fwd(rows=1 << 24, C=4096))
     for C in (0, 12, 8200):
         refused(lib, UNS, "multiple of 8", fwd(C=C))
     refused(lib, INV, "dtype", fwd(t=9))
