@@ -121,7 +121,7 @@ def check(name, got, ref, tol):
 # each shape, ragged rows and channels, K that ends inside a block, a half step and a step
 SHAPES = [(1, 16, 8), (1, 1536, 1536), (3, 48, 40), (16, 272, 264), (17, 272, 2312), (33, 1536, 1536), (64, 160, 8960),
           (65, 16, 8), (65, 144, 72), (130, 272, 256), (129, 400, 512), (300, 1552, 1544), (577, 1536, 768),
-          (1365, 1536, 8960), (700, 8960, 1536), (2500, 1040, 1000)]
+          (1365, 1536, 8960), (700, 8960, 1536), (2500, 1040, 1000), (5, 4624, 1544), (16, 1536, 2056)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)

@@ -100,6 +100,24 @@ def test_attention(B, S, H, heads, D, cap, lens, f32):
     check(f"{(B, S, H, heads, D, cap, lens)}", o, lse, odit.widen(q), k, v, lens, scale, not f32)
 
 
+@pytest.mark.parametrize("S,cap,ranges", [(200, 1024, 2), (200, 1600, 3), (1, 1030, 4), (2, 1300, 5), (20, 1800, 7), (1, 2100, 8),
+                                          (3, 2400, 9), (30, 5130, 20), (1, 16500, 64)])
+def test_joined_ranges(S, cap, ranges):
+    """Every form of the joining of key ranges, all of them in use and most of them empty."""
+    import ctypes
+    from paper_2607_28144_amd import _lib
+    B, H, D = 2, 1, 64
+    p = _lib.MxAttnPlan()
+    n_cu = torch.cuda.get_device_properties(0).multi_processor_count
+    assert _lib.load().regenvc_mx_attn_cache_plan_query(B, H, H, S, cap, D, n_cu, ctypes.byref(p)) == 0
+    assert p.key_ranges == ranges
+    c, k, v = filled(B, cap, H, D, cap)
+    q = synth.normal_bf16(np.random.default_rng(S), (B, S, H, D))
+    for lens in ([cap, 70], [cap - 1, 0], [129, cap // 2]):
+        o, lse = mx().attn_cache_fwd(bf16(q), c, ints(lens), out_dtype=torch.float32)
+        check(f"S={S} cap={cap} {lens}", o, lse, odit.widen(q), k, v, lens, synth.default_scale(D), False)
+
+
 @pytest.mark.parametrize("S", [1, 40, 200])
 def test_sharp_scores_and_scales(S):
     """Scores of both signs far apart, a scale of 0 (all places alike) and one of 1."""
