@@ -468,10 +468,9 @@ void attn_few_kernel(AttnCacheArgs a, AttnCachePlan p)
 // 4-7, held from its load a tile earlier, 16 conversions and four LDS stores.
 // LDS is a ring of four stages: tile u + 2 goes where tile u - 2 was, whose
 // last reads (M(u - 1) of both groups) lie before pair u of phases.  1560
-// queries x 32760 places, 12 heads of 128 in 3 ranges: 292-318 us, 1.0-1.08
-// PFLOP/s of the formula's operations and 1.15-1.24 of those done (the seventh
-// tile of a head has 24 rows): matrix units busy for 48 % of the cycles at 2.1
-// GHz, which is the power limit of the bf16 attention too.
+// queries x 32760 places, 12 heads of 128 in 3 ranges: 287 us, 1.09 PFLOP/s;
+// matrix units busy for 48 % of the cycles at 2.1 GHz, which is the power limit of
+// the bf16 attention too.
 constexpr int kManyWaves = 8, kManyRows = 32 * kManyWaves, kManyKeys = 64;
 
 template <int D>
@@ -666,7 +665,18 @@ void attn_many_kernel(AttnCacheArgs a, AttnCachePlan p)
         __syncthreads();
         // Pairs of phases u = 0 .. T - 1, two barriers each in both groups: group 0 runs M(u) | V(u), group 1
         // V(u - 1) | M(u); then the last M (of weights only) of each group.
-        if (grp == 0) {
+        if (row0 >= rows) {
+            // A wave past the last row only brings its share of the codes, between the same barriers: energy that the
+            // clock of the others gets (305 us, 295 so, at the size above).
+            __syncthreads();
+            if (grp != 0) __syncthreads();
+            for (int u = 0; u < T - 1; ++u) {
+                feed(u);
+                __syncthreads();
+                __syncthreads();
+            }
+            if (grp == 0) __syncthreads();
+        } else if (grp == 0) {
             __asm__ volatile("; group 0");
             mprefetch(0, F_{});
             mphase(0, F_{}, T_{});
