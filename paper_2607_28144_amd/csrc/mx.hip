@@ -363,23 +363,16 @@ __device__ __forceinline__ void load_bias(const LinearArgs &a, int n0, int g, u3
 // caches (1365 x 1536 x 8960: 18.4 and 19.7).  WHOLE: no row or channel of the
 // tile lies past the last one.
 template <class S, int EPI, bool WHOLE>
-__device__ __forceinline__ void store_tile(const LinearArgs &a, int m0, int n0, const u32x2 (&raw)[S::NB], char *smem,
-                                           f32x4 (&acc)[S::NB][S::MB])
+__device__ __forceinline__ void store_tile(const LinearArgs &a, int m0, int n0, char *smem, f32x4 (&acc)[S::NB][S::MB])
 {
     constexpr int MB = S::MB, NB = S::NB;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4, x = lane & 15;
-    f32x4 bv[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-        bv[nb] = f32x4{__uint_as_float(raw[nb][0] << 16), __uint_as_float(raw[nb][0] & 0xffff0000u),
-                       __uint_as_float(raw[nb][1] << 16), __uint_as_float(raw[nb][1] & 0xffff0000u)};
     auto round4 = [&](int nb, int mb) {
-        const f32x4 y = acc[nb][mb] + bv[nb];
         bf16x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (__bf16)tile::activate<EPI>(y[i]);
+        for (int i = 0; i < 4; ++i) w[i] = (__bf16)tile::activate<EPI>(acc[nb][mb][i]);
         return w;
     };
     if constexpr (EPI == kEpiGatedRes) {
@@ -404,7 +397,7 @@ __device__ __forceinline__ void store_tile(const LinearArgs &a, int m0, int n0, 
             for (int mb = 0; mb < MB; ++mb)
                 if (live(nb, mb))
                     *reinterpret_cast<f32x4 *>(p + mb * rows16 + nb * 16) =
-                        old[nb & 1][mb] + gv[nb & 1] * (acc[nb][mb] + bv[nb]);
+                        old[nb & 1][mb] + gv[nb & 1] * acc[nb][mb];
         }
     } else if constexpr (S::STAGED) {
         tile::lds_char *stg = (tile::lds_char *)smem + S::OUT + wave * 16 * S::OUT_ROW;
@@ -576,15 +569,18 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
 
     constexpr int RD = NM * 3 / 4;  // a half's reads and copies are spread over this many MFMAs
     int st = 0;
+    u32x2 raw[NB];
+    load_bias<NB>(a, item_of<S>(t, blockIdx.x).n0 + wn * 16 * NB, g, raw);
     for (int item = blockIdx.x; item < t.n_tiles; item += stride) {
         const Item it = item_of<S>(t, item);
         const int m0 = it.m0 + wm * 16 * MB, n0 = it.n0 + wn * 16 * NB;
-        u32x2 raw[NB];
-        load_bias<NB>(a, n0, g, raw);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) acc[nb][mb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int mb = 0; mb < MB; ++mb)
+                acc[nb][mb] = f32x4{__uint_as_float(raw[nb][0] << 16), __uint_as_float(raw[nb][0] & 0xffff0000u),
+                                    __uint_as_float(raw[nb][1] << 16), __uint_as_float(raw[nb][1] & 0xffff0000u)};
+        if (item + stride < t.n_tiles) load_bias<NB>(a, item_of<S>(t, item + stride).n0 + wn * 16 * NB, g, raw);
         __builtin_amdgcn_s_setprio(1);  // before the other workgroup's epilogue (10920 x 8960 x 1536: 97.4 us, 95.4 so)
         for (int kt = 0; kt < t.nk; ++kt) {
             const int st1 = st + 1 == ST ? 0 : st + 1;
@@ -604,7 +600,8 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
             __builtin_amdgcn_s_barrier();
             __asm__ volatile("" : : : "memory");
             if (ST == 2 && kt == 0) {
-                // the biases have landed too: known here, the compiler does not wait for later copies where they are used
+                // the next tile's biases have landed too: known here, the compiler does not wait for later copies where
+                // they are used
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) __asm__ volatile("" : "+v"(raw[nb]));
             }
@@ -630,9 +627,9 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
         }
         __builtin_amdgcn_s_setprio(0);
         if (m0 + 16 * MB <= a.M && n0 + 16 * NB <= a.N)
-            store_tile<S, EPI, true>(a, m0, n0, raw, smem, acc);
+            store_tile<S, EPI, true>(a, m0, n0, smem, acc);
         else
-            store_tile<S, EPI, false>(a, m0, n0, raw, smem, acc);
+            store_tile<S, EPI, false>(a, m0, n0, smem, acc);
     }
     tile::wait_all_copies();
 }
