@@ -256,9 +256,9 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
 // 64 KB of fragment reads at 128); two workgroups per compute unit take about
 // 1000.  8192 x 8192 x 8192: 273-292 us, 3.8-4.0 PFLOP/s, with the matrix units
 // busy for 52 % of the cycles and the clock down to 1.79 GHz: the power limit.
-// 10920 x 8960 x 1536: 95 us, with GELU 109 (2.75 PFLOP/s), of which the epilogue
+// 10920 x 8960 x 1536: 94 us, with GELU 108 (2.8 PFLOP/s), of which the epilogue
 // (196 MB of output; an exponential and a reciprocal for each of 98 million
-// values) takes 15 and 29: without it 80.  1365 x 1536 x 8960: 17.4 us (2.2
+// values) takes 14 and 28: without it 80.  1365 x 1536 x 8960: 17.4 us (2.2
 // PFLOP/s).
 // Larger tiles do less LDS work per MFMA, but 256 x 256 leaves a wave alone on
 // its SIMD with 256 accumulators: 310-338 us for the same product, and no

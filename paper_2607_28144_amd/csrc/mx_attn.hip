@@ -469,8 +469,8 @@ void attn_few_kernel(AttnCacheArgs a, AttnCachePlan p)
 // LDS is a ring of four stages: tile u + 2 goes where tile u - 2 was, whose
 // last reads (M(u - 1) of both groups) lie before pair u of phases.  1560
 // queries x 32760 places, 12 heads of 128 in 3 ranges: 287 us, 1.09 PFLOP/s;
-// matrix units busy for 48 % of the cycles at 2.1 GHz, which is the power limit of
-// the bf16 attention too.
+// matrix units busy for 42 % of the cycles (48 before waves without a row were
+// spared) at 2.1 GHz, which is the power limit of the bf16 attention too.
 constexpr int kManyWaves = 8, kManyRows = 32 * kManyWaves, kManyKeys = 64;
 
 template <int D>
