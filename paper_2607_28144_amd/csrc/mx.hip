@@ -263,10 +263,12 @@ __global__ __launch_bounds__(64 * W) void linear_rows_kernel(LinearArgs a, int n
 // Larger tiles do less LDS work per MFMA, but 256 x 256 leaves a wave alone on
 // its SIMD with 256 accumulators: 310-338 us for the same product, and no
 // second workgroup beside its epilogue.  Where there are few tiles, their
-// steps wait for memory, all workgroups being at the same place in K: four or
-// five stages then pay (1365 x 1536 x 8960, 132 tiles: 29.8 us with two
-// stages, 22.7 with four; 240 tiles of 96 x 96: 20).  K is not split: over
-// 216 shapes the best split of each was 0.07 % faster than the best whole one.
+// steps wait for memory, all workgroups being at the same place in K: four
+// stages then pay (1365 x 1536 x 8960, 132 tiles: 29.8 us with two stages, 22.7
+// with four; 240 tiles of 96 x 96: 17.4, with five or six 17.8).  All of a step's
+// fragments read a step ahead, into a second set of registers: 18.6.  K is not
+// split: over 216 shapes the best split of each was 0.07 % faster than the best
+// whole one.
 template <int MB_, int NB_, int WPE_, int ST_>
 struct Shape {
     static constexpr int MB = MB_, NB = NB_, WPE = WPE_, ST = ST_;
@@ -636,7 +638,7 @@ void linear_tile_kernel(LinearArgs a, Tiles t)
 
 typedef Shape<4, 4, 2, 2> Tile128x128;
 typedef Shape<4, 4, 1, 4> Tile128x128Deep;  // four stages: for few tiles, one workgroup per compute unit
-typedef Shape<3, 3, 1, 5> Tile96x96;
+typedef Shape<3, 3, 1, 4> Tile96x96;
 typedef Shape<2, 4, 2, 3> Tile64x128;
 typedef Shape<2, 2, 2, 4> Tile64x64;
 enum TileId : int32_t { kRows, kTile128x128, kTile128x128Deep, kTile96x96, kTile64x128, kTile64x64 };
