@@ -212,13 +212,20 @@ class _Nothing:
 
 
 _NOTHING = _Nothing()
+_current_device = None
 
 
 def on_device(device):
     """Context with a torch device (or the device of an index) current; nothing to do where it is already."""
+    global _current_device
+    if _current_device is None:
+        import torch
+        torch.cuda.current_device()  # initializes
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if _current_device() == (device if type(device) is int else device.index):
+        return _NOTHING
     import torch
-    idx = device if isinstance(device, int) else device.index
-    return _NOTHING if torch.cuda.current_device() == idx else torch.cuda.device(device)
+    return torch.cuda.device(device)
 
 
 def index_of(t, name: str) -> int:

@@ -140,14 +140,15 @@ def _norm(kind: Optional[str], eps: float, w, b, C: int, name: str, idx: int) ->
 
 def _row_vectors(groups: int, C: int, group_rows: int, idx: int, gate, scale, shift) -> _lib.RowVectors:
     """gate, scale, shift (or None): float32 [C], or [groups, C] with one row stride."""
+    if groups == 1:  # [C] or [1, C]
+        f32, vector = torch.float32, _lib.vector
+        return _lib.RowVectors(vector(gate, "gate", f32, C, idx), vector(scale, "scale", f32, C, idx),
+                               vector(shift, "shift", f32, C, idx), C, group_rows)
     ld = None
     ptrs = []
     for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
         if t is None:
             ptrs.append(None)
-            continue
-        if groups == 1:  # [C] or [1, C]
-            ptrs.append(_lib.vector(t, name, torch.float32, C, idx))
             continue
         step = _lib.matrix(t, name, torch.float32, groups, C, idx)
         if ld is not None and step != ld:
