@@ -75,9 +75,10 @@ regenvc_status check_ld(const char *fn, const char *name, int64_t ld, int32_t C)
 }
 
 // Alignment of every buffer that is there, and no output over another one, but
-// for the pair (same_out, same_in), which may be one buffer.
+// for the first over the second where the call is in place: these two by their
+// places in the list, for another buffer at the same address is refused.
 template <size_t N>
-regenvc_status check_buffers(const char *fn, const Buffer (&b)[N], const void *same_out, const void *same_in)
+regenvc_status check_buffers(const char *fn, const Buffer (&b)[N], bool in_place)
 {
     for (const Buffer &x : b)
         if (x.ptr != nullptr && !aligned(x.ptr, 16))
@@ -86,7 +87,7 @@ regenvc_status check_buffers(const char *fn, const Buffer (&b)[N], const void *s
         if (!b[i].out || b[i].ptr == nullptr) continue;
         for (size_t j = 0; j < N; ++j) {
             if (i == j || b[j].ptr == nullptr || (b[j].out && j < i)) continue;
-            if (b[i].ptr == same_out && b[j].ptr == same_in && same_out == same_in) continue;
+            if (i == 0 && j == 1 && in_place) continue;
             if (overlaps(range_of(b[i].ptr, b[i].bytes), range_of(b[j].ptr, b[j].bytes)))
                 return failf(REGENVC_ERR_INVALID_ARG, "%s: %s overlaps %s", fn, b[i].name, b[j].name);
         }
@@ -143,8 +144,8 @@ regenvc_status regenvc_residual_norm_fwd(const float *x, int64_t ldx, const void
     const int64_t e = a.f32 ? 4 : 2, groups = (rows + a.group_rows - 1) / a.group_rows;
     const int64_t vec = span(groups, a.ldv, C, 4);
     const Buffer bufs[] = {{"x_out", x_out, span(rows, ldxo, C, 4), true},
-                           {"h", h, span(rows, ldh, C, e), true},
                            {"x", x, span(rows, ldx, C, 4), false},
+                           {"h", h, span(rows, ldh, C, e), true},
                            {"y", y, span(rows, ldy, C, e), false},
                            {"gate", a.gate, vec, false},
                            {"scale", a.scale, vec, false},
@@ -153,7 +154,7 @@ regenvc_status regenvc_residual_norm_fwd(const float *x, int64_t ldx, const void
                            {"pre b", pre->b, (int64_t)C * 2, false},
                            {"post w", post->w, (int64_t)C * 2, false},
                            {"post b", post->b, (int64_t)C * 2, false}};
-    if ((st = check_buffers(fn, bufs, x_out, ldx == ldxo ? x : nullptr)) != REGENVC_OK) return st;
+    if ((st = check_buffers(fn, bufs, x_out == x && ldxo == ldx)) != REGENVC_OK) return st;
     if ((st = regenvc::abi::device_ok()) != REGENVC_OK) return st;
     a.x = x, a.ldx = ldx;
     a.x_out = x_out, a.ldxo = ldxo, a.h = h, a.ldh = ldh;
@@ -215,6 +216,7 @@ regenvc_status regenvc_residual_norm_bwd(const float *x_out, int64_t ldx, const 
     const int row_sums = (grads->dw != nullptr) + (grads->db != nullptr) + (grads->dpost_w != nullptr) +
                          (grads->dpost_b != nullptr);
     const Buffer bufs[] = {{"dx", dx, span(rows, lddx, C, 4), true},
+                           {"gx", gx, span(rows, ldgx, C, 4), false},
                            {"dy", dy, span(rows, lddy, C, e), true},
                            {"dgate", grads->dgate, gvec, true},
                            {"dscale", grads->dscale, gvec, true},
@@ -227,14 +229,13 @@ regenvc_status regenvc_residual_norm_bwd(const float *x_out, int64_t ldx, const 
                            {"x_out", x_out, span(rows, ldx, C, 4), false},
                            {"y", y, span(rows, ldy, C, e), false},
                            {"gh", gh, span(rows, ldgh, C, e), false},
-                           {"gx", gx, span(rows, ldgx, C, 4), false},
                            {"gate", a.gate, vec, false},
                            {"scale", a.scale, vec, false},
                            {"pre w", pre->w, (int64_t)C * 2, false},
                            {"pre b", pre->b, (int64_t)C * 2, false},
                            {"post w", post->w, (int64_t)C * 2, false},
                            {"post b", post->b, (int64_t)C * 2, false}};
-    if ((st = check_buffers(fn, bufs, dx, ldgx == lddx ? gx : nullptr)) != REGENVC_OK) return st;
+    if ((st = check_buffers(fn, bufs, dx == gx && lddx == ldgx)) != REGENVC_OK) return st;
     if (workspace != nullptr && !aligned(workspace, 256))
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: workspace must be 256-byte aligned", fn);
     if ((st = regenvc::abi::device_ok()) != REGENVC_OK) return st;

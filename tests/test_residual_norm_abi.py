@@ -1,0 +1,63 @@
+"""Argument checks of the residual-norm entry points (include/regenvc_dit.h) at
+their borders, on the CPU: calls in place, and sizes at and beyond what a call
+can do.  Every call here is refused before any HIP call, so the fake addresses are
+never dereferenced."""
+import pytest
+
+from paper_2607_28144_amd import _lib
+
+A, B, C, D, E = (0x10000000 + (i << 33) for i in range(5))  # 256-byte aligned, far apart
+LN, NONE = _lib.Norm(1, 1e-6, None, None), _lib.Norm(0, 1e-6, None, None)
+BF16, F32 = _lib.BF16, _lib.F32
+INV = _lib.ERR_INVALID_ARG
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return _lib.load()
+
+
+def refused(lib, status, word, st):
+    assert st == status, (st, lib.regenvc_last_error())
+    assert word in lib.regenvc_last_error().decode(), lib.regenvc_last_error()
+
+
+def forward(lib, **kw):
+    a = dict(dict(x=A, ldx=64, y=B, ldy=64, t=F32, gate=None, xo=A, ldxo=64, h=C, ldh=64, rows=10, C=64), **kw)
+    v = _lib.RowVectors(a["gate"], None, None, 64, 0)
+    return lib.regenvc_residual_norm_fwd(a["x"], a["ldx"], a["y"], a["ldy"], a["t"], NONE, LN, v, 1.0, a["xo"], a["ldxo"],
+                                         a["h"], a["ldh"], a["rows"], a["C"], None)
+
+
+@pytest.mark.parametrize("t", [BF16, F32])
+def test_forward_in_place_exempts_the_stream_alone(lib, t):
+    """x_out over x; at that address lies nothing else, in any row stride."""
+    for ld in (64, 72):
+        refused(lib, INV, "x_out overlaps h", forward(lib, t=t, h=A, ldh=ld))
+        refused(lib, INV, "x_out overlaps y", forward(lib, t=t, y=A, ldy=ld))
+    refused(lib, INV, "x_out overlaps gate", forward(lib, t=t, gate=A))
+    refused(lib, INV, "x_out overlaps h", forward(lib, t=t, h=A + 256))
+    refused(lib, INV, "x_out overlaps x", forward(lib, t=t, ldxo=72))
+    # in place alone is let through: it is a later pair that speaks
+    refused(lib, INV, "h overlaps y", forward(lib, t=t, h=B))
+
+
+def backward(lib, **kw):
+    a = dict(dict(x=A, y=B, gh=C, ldgh=64, gx=D, ldgx=64, dx=D, lddx=64, dy=E, lddy=64, t=F32, dgate=None, rows=10), **kw)
+    v = _lib.RowVectors(E + (1 << 32), None, None, 64, 0)
+    return lib.regenvc_residual_norm_bwd(a["x"], 64, a["y"], 64, a["t"], NONE, LN, v, 1.0, a["gh"], a["ldgh"], a["gx"],
+                                         a["ldgx"], a["dx"], a["lddx"], a["dy"], a["lddy"], _lib.NormGrads(dgate=a["dgate"]),
+                                         a["rows"], 64, None, 0, None)
+
+
+@pytest.mark.parametrize("t", [BF16, F32])
+def test_backward_in_place_exempts_the_stream_gradient_alone(lib, t):
+    """dx over gx; at that address lies nothing else."""
+    for ld in (64, 72):
+        refused(lib, INV, "dx overlaps dy", backward(lib, t=t, dy=D, lddy=ld))
+        refused(lib, INV, "dx overlaps gh", backward(lib, t=t, gh=D, ldgh=ld))
+    refused(lib, INV, "dx overlaps dgate", backward(lib, t=t, dgate=D))
+    refused(lib, INV, "dx overlaps x_out", backward(lib, t=t, x=D))
+    refused(lib, INV, "dx overlaps y", backward(lib, t=t, y=D))
+    refused(lib, INV, "dx overlaps gx", backward(lib, t=t, lddx=72))
+    refused(lib, INV, "dy overlaps gh", backward(lib, t=t, dy=C))
