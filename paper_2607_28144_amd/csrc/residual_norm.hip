@@ -583,17 +583,17 @@ hipError_t launch_residual_norm_fwd(const ResidualNormArgs &a, hipStream_t strea
 ResidualNormPlan residual_norm_plan(int rows, int C, int group_rows, int n_cu)
 {
     ResidualNormPlan p{};
-    p.groups = (rows + group_rows - 1) / group_rows;
+    p.groups = (int)(((int64_t)rows + group_rows - 1) / group_rows);
     p.row_waves = (C + 511) / 512;
     p.rows_at_once = std::max(1, 4 / p.row_waves);
     // Workgroups per compute unit: as many as its registers hold, for the more rows are under way the better memory
     // latency passes, but each costs a row per sum in the workspace: a third one pays from 8 rows per workgroup on
     // (10920 rows of 1536 channels: 106, 65 and 63 us with one, two and three; 1560 of 2048: 23, 18 and 20).  Never
     // more workgroups than run at once: a second round costs as much as the first.
-    const int per_cu = p.row_waves > 4 ? 1 : p.row_waves <= 3 && rows >= 24 * n_cu ? 3 : 2;
-    const int want = per_cu * n_cu;
-    p.per_group = std::max(1, std::min(want / p.groups, group_rows / p.rows_at_once));
-    p.blocks = (int)std::min<int64_t>(p.segments(), want);
+    const int64_t per_cu = p.row_waves > 4 ? 1 : p.row_waves <= 3 && rows >= 24 * (int64_t)n_cu ? 3 : 2;
+    const int64_t want = per_cu * n_cu;
+    p.per_group = (int)std::max<int64_t>(1, std::min<int64_t>(want / p.groups, group_rows / p.rows_at_once));
+    p.blocks = (int)std::min(p.segments(), want);
     return p;
 }
 

@@ -40,8 +40,8 @@ regenvc_status check_norm(const char *fn, const char *name, const regenvc_norm *
     return REGENVC_OK;
 }
 
-regenvc_status check_common(const char *fn, regenvc_dtype dtype, const regenvc_norm *post, const regenvc_norm *pre,
-                            const regenvc_row_vectors *v, float alpha, int32_t rows, int32_t C, bool backward)
+// Rows and channels of a call, and of the query of its workspace.
+regenvc_status check_size(const char *fn, int32_t rows, int32_t C)
 {
     if (rows < 0) return failf(REGENVC_ERR_INVALID_ARG, "%s: rows=%d < 0", fn, rows);
     // a launch has less than 2^32 threads: a wave per row, or four
@@ -49,8 +49,16 @@ regenvc_status check_common(const char *fn, regenvc_dtype dtype, const regenvc_n
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d rows, must be below 2^26 (2^24 with more than 2048 channels)", fn, rows);
     if (C < 8 || C % 8 != 0 || C > 8192)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: C=%d is not a multiple of 8 in [8, 8192]", fn, C);
+    return REGENVC_OK;
+}
+
+regenvc_status check_common(const char *fn, regenvc_dtype dtype, const regenvc_norm *post, const regenvc_norm *pre,
+                            const regenvc_row_vectors *v, float alpha, int32_t rows, int32_t C, bool backward)
+{
+    regenvc_status st = check_size(fn, rows, C);
+    if (st != REGENVC_OK) return st;
     if (dtype != REGENVC_BF16 && dtype != REGENVC_F32) return failf(REGENVC_ERR_INVALID_ARG, "%s: dtype %d", fn, dtype);
-    regenvc_status st = check_norm(fn, "post", post, true);
+    st = check_norm(fn, "post", post, true);
     if (st == REGENVC_OK) st = check_norm(fn, "pre", pre, false);
     if (st != REGENVC_OK) return st;
     if (!std::isfinite(alpha)) return failf(REGENVC_ERR_INVALID_ARG, "%s: alpha is not finite", fn);
@@ -169,8 +177,8 @@ regenvc_status regenvc_residual_norm_bwd_workspace(int32_t rows, int32_t C, int3
     if (rows < 0 || group_rows < 0 || n_cu < 1 || group_sums < 0 || group_sums > 3 || row_sums < 0 || row_sums > 4)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: bad size (rows=%d group_rows=%d sums=%d, %d n_cu=%d)", fn, rows,
                      group_rows, group_sums, row_sums, n_cu);
-    if (C < 8 || C % 8 != 0 || C > 8192)
-        return failf(REGENVC_ERR_UNSUPPORTED, "%s: C=%d is not a multiple of 8 in [8, 8192]", fn, C);
+    const regenvc_status st = check_size(fn, rows, C);
+    if (st != REGENVC_OK) return st;
     *bytes = 0;
     if (rows > 0)
         *bytes = regenvc::residual_norm_workspace(

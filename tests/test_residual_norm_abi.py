@@ -2,6 +2,8 @@
 their borders, on the CPU: calls in place, and sizes at and beyond what a call
 can do.  Every call here is refused before any HIP call, so the fake addresses are
 never dereferenced."""
+import ctypes
+
 import pytest
 
 from paper_2607_28144_amd import _lib
@@ -9,7 +11,7 @@ from paper_2607_28144_amd import _lib
 A, B, C, D, E = (0x10000000 + (i << 33) for i in range(5))  # 256-byte aligned, far apart
 LN, NONE = _lib.Norm(1, 1e-6, None, None), _lib.Norm(0, 1e-6, None, None)
 BF16, F32 = _lib.BF16, _lib.F32
-INV = _lib.ERR_INVALID_ARG
+INV, UNS = _lib.ERR_INVALID_ARG, _lib.ERR_UNSUPPORTED
 
 
 @pytest.fixture(scope="module")
@@ -61,3 +63,26 @@ def test_backward_in_place_exempts_the_stream_gradient_alone(lib, t):
     refused(lib, INV, "dx overlaps y", backward(lib, t=t, y=D))
     refused(lib, INV, "dx overlaps gx", backward(lib, t=t, lddx=72))
     refused(lib, INV, "dy overlaps gh", backward(lib, t=t, dy=C))
+
+
+def workspace(lib, rows, C=64, group_rows=0, sums=(3, 2), n_cu=256):
+    n = ctypes.c_int64(-7)
+    return lib.regenvc_residual_norm_bwd_workspace(rows, C, group_rows, *sums, n_cu, ctypes.byref(n)), n.value
+
+
+@pytest.mark.parametrize("C,limit", [(64, 1 << 26), (2048, 1 << 26), (2056, 1 << 24), (8192, 1 << 24)])
+def test_workspace_query_refuses_the_rows_that_the_call_refuses(lib, C, limit):
+    """... and gives no size for them; sums of sizes that pass 32 bits neither end the process nor come out as 0."""
+    for rows in (limit, (1 << 30) + 8, 1500000000, (1 << 31) - 1):
+        for group_rows in (0, 1, rows - 1, (1 << 31) - 1):
+            st, n = workspace(lib, rows, C, group_rows)
+            refused(lib, UNS, "must be below", st)
+            assert n == -7
+
+
+def test_workspace_query_for_any_number_of_compute_units(lib):
+    """At least a row of C for each sum over all rows, and no more than a plan of one row per workgroup writes."""
+    for rows, C, group_rows in ((10920, 1536, 1560), (100, 64, 0), (5000, 8192, 7), (1 << 20, 64, 1)):
+        for n_cu in (1, 304, 1 << 20, 2000000000, (1 << 31) - 1):
+            st, n = workspace(lib, rows, C, group_rows, n_cu=n_cu)
+            assert st == _lib.OK and 2 * C * 4 <= n <= 5 * rows * C * 4, (rows, C, group_rows, n_cu, n)
