@@ -81,8 +81,10 @@ def test_workspace_query_refuses_the_rows_that_the_call_refuses(lib, C, limit):
 
 
 def test_workspace_query_for_any_number_of_compute_units(lib):
-    """At least a row of C for each sum over all rows, and no more than a plan of one row per workgroup writes."""
+    """At least a row of C for each sum over all rows, and no more than one for every sum and row: a group has at most
+    group_rows segments, so there are at most ceil(rows / group_rows) group_rows < rows + group_rows of them (the last
+    group's may be empty)."""
     for rows, C, group_rows in ((10920, 1536, 1560), (100, 64, 0), (5000, 8192, 7), (1 << 20, 64, 1)):
         for n_cu in (1, 304, 1 << 20, 2000000000, (1 << 31) - 1):
             st, n = workspace(lib, rows, C, group_rows, n_cu=n_cu)
-            assert st == _lib.OK and 2 * C * 4 <= n <= 5 * rows * C * 4, (rows, C, group_rows, n_cu, n)
+            assert st == _lib.OK and 2 * C * 4 <= n < 5 * (rows + group_rows + 1) * C * 4, (rows, C, group_rows, n_cu, n)
