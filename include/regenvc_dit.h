@@ -144,7 +144,8 @@ typedef struct {
    x, x_out: f32 [rows, C]; y, h: [rows, C] in dtype (bf16, rounded to nearest
    even, or f32); row strides ld* multiples of 8.  x_out may be x itself (same
    pointer and stride); outputs overlap nothing else.  C a multiple of 8, at
-   most 8192; rows below 2^26 (2^24 with more than 2048 channels); pointers 16-byte aligned; alpha finite. */
+   most 8192; rows at most 2^26 - 4 (below 2^24 with more than 2048 channels);
+   pointers 16-byte aligned; alpha finite. */
 regenvc_status regenvc_residual_norm_fwd(const float *x, int64_t ldx, const void *y, int64_t ldy, regenvc_dtype dtype,
                                          const regenvc_norm *post, const regenvc_norm *pre,
                                          const regenvc_row_vectors *vectors, float alpha, float *x_out, int64_t ldxo,

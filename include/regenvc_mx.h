@@ -49,7 +49,7 @@ regenvc_status regenvc_mx_quantize(const void *x, regenvc_dtype x_dtype, int64_t
 
 /* The values of a matrix in MXFP4: out bf16 (rounded to nearest even, which
    only values below 2^-126 and above the bf16 range need) or f32 [rows, K],
-   row stride ldo, a multiple of 8. */
+   row stride ldo, a multiple of 8; rows at most 2^26 - 4. */
 regenvc_status regenvc_mx_dequantize(const void *codes, const void *scales, void *out, regenvc_dtype out_dtype,
                                      int64_t ldo, int32_t rows, int32_t K, void *stream);
 

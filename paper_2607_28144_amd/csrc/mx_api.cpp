@@ -22,7 +22,8 @@ namespace {
 constexpr int32_t kMaxK = 1 << 20;
 constexpr int32_t kMaxN = 65535 * 16;               // 16 channels per workgroup, in the grid's second dimension
 constexpr int64_t kMaxOut = (int64_t)1 << 42;        // 2^30 tiles of 64 x 64
-constexpr int32_t kMaxRows = 1 << 26;                // 2^32 threads at a wave per row
+constexpr int32_t kMaxRows = 1 << 26;                // codes and scales of 2^20 columns stay far within int64
+constexpr int32_t kMaxDequantize = kMaxRows - 4;     // workgroups of 256 for four rows each: less than 2^32 threads
 constexpr int32_t kMaxPlaces = 1 << 30;              // a tile past the last place stays within int32
 
 regenvc_status done()
@@ -168,6 +169,8 @@ regenvc_status regenvc_mx_dequantize(const void *codes, const void *scales, void
     regenvc_status st = check_matrix(fn, rows, K);
     if (st == REGENVC_OK) st = check_dtype(fn, out_dtype);
     if (st != REGENVC_OK) return st;
+    if (rows > kMaxDequantize)
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d rows, at most %d", fn, rows, kMaxDequantize);
     if (rows == 0 || K == 0) return done();
     if (ldo < K || ldo % 8 != 0)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: row stride ldo=%lld (a multiple of 8, >= K)", fn, (long long)ldo);

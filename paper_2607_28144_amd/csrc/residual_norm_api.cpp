@@ -44,9 +44,10 @@ regenvc_status check_norm(const char *fn, const char *name, const regenvc_norm *
 regenvc_status check_size(const char *fn, int32_t rows, int32_t C)
 {
     if (rows < 0) return failf(REGENVC_ERR_INVALID_ARG, "%s: rows=%d < 0", fn, rows);
-    // a launch has less than 2^32 threads: a wave per row, or four
-    if (rows >= 1 << (C <= 2048 ? 26 : 24))
-        return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d rows, must be below 2^26 (2^24 with more than 2048 channels)", fn, rows);
+    // a launch has less than 2^32 threads: workgroups of 256 for four rows each, or for one
+    if (rows > (C <= 2048 ? (1 << 26) - 4 : (1 << 24) - 1))
+        return failf(REGENVC_ERR_UNSUPPORTED,
+                     "%s: %d rows, must be below 2^26 - 3 (2^24 with more than 2048 channels)", fn, rows);
     if (C < 8 || C % 8 != 0 || C > 8192)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: C=%d is not a multiple of 8 in [8, 8192]", fn, C);
     return REGENVC_OK;

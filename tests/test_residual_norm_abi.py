@@ -88,3 +88,15 @@ def test_workspace_query_for_any_number_of_compute_units(lib):
         for n_cu in (1, 304, 1 << 20, 2000000000, (1 << 31) - 1):
             st, n = workspace(lib, rows, C, group_rows, n_cu=n_cu)
             assert st == _lib.OK and 2 * C * 4 <= n < 5 * (rows + group_rows + 1) * C * 4, (rows, C, group_rows, n_cu, n)
+
+
+@pytest.mark.parametrize("C,most", [(8, (1 << 26) - 4), (2048, (1 << 26) - 4), (2056, (1 << 24) - 1), (8192, (1 << 24) - 1)])
+def test_most_rows_are_those_of_one_launch(lib, C, most):
+    """A launch has less than 2^32 threads: four rows to a workgroup of 256, or one beyond 2048 channels."""
+    per = 4 if C <= 2048 else 1
+    assert -(-most // per) * 256 < 1 << 32 <= -(-(most + 1) // per) * 256
+    ld = dict(ldx=C, ldxo=C, ldy=C, ldh=C, C=C, xo=None)
+    refused(lib, INV, "a NULL data pointer", forward(lib, rows=most, **ld))  # the sizes are in order
+    refused(lib, UNS, "must be below", forward(lib, rows=most + 1, **ld))
+    assert workspace(lib, most, C)[0] == _lib.OK
+    refused(lib, UNS, "must be below", workspace(lib, most + 1, C)[0])
