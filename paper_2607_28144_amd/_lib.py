@@ -236,6 +236,13 @@ def index_of(t, name: str) -> int:
     return idx
 
 
+def int32(**sizes: int) -> None:
+    """Refuses sizes that do not fit the int32 arguments of the C ABI: ctypes would hand on their low 32 bits."""
+    for name, v in sizes.items():
+        if not -(1 << 31) <= v < 1 << 31:
+            raise ValueError(f"{name}={v} does not fit 32 bits")
+
+
 def matrix(t, name: str, dtype, rows: int, cols: int, idx: int) -> int:
     """The row stride of a [rows, cols] tensor of this type on device idx; refuses any other.  (Of a single row, whose
     stride torch leaves to chance: cols.)"""

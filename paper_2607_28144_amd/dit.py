@@ -158,8 +158,13 @@ def _row_vectors(groups: int, C: int, group_rows: int, idx: int, gate, scale, sh
     return _lib.RowVectors(ptrs[0], ptrs[1], ptrs[2], C if ld is None else ld, group_rows)
 
 
-def _groups(rows: int, group_rows: int) -> int:
-    return -(-rows // group_rows) if 0 < group_rows < rows else 1
+def _groups(rows: int, group_rows: int) -> Tuple[int, int]:
+    """The sets of vectors of a call, and group_rows as the library gets it: any number from the rows on is one set."""
+    if rows >= 1 << 31 or group_rows < -1:
+        _lib.int32(rows=rows, group_rows=min(group_rows, rows))
+    if group_rows >= rows:
+        return 1, rows
+    return -(-rows // group_rows) if group_rows > 0 else 1, group_rows
 
 
 def residual_norm_fwd(x: torch.Tensor, y: torch.Tensor, norm: str = "layer", post: Optional[str] = None,
@@ -189,7 +194,8 @@ def residual_norm_fwd(x: torch.Tensor, y: torch.Tensor, norm: str = "layer", pos
         h, ldh = torch.empty(rows, C, dtype=act, device=dev), C
     else:
         ldh = _lib.matrix(h, "h", act, rows, C, idx)
-    v = _row_vectors(_groups(rows, group_rows), C, group_rows, idx, gate, scale, shift)
+    groups, group_rows = _groups(rows, group_rows)
+    v = _row_vectors(groups, C, group_rows, idx, gate, scale, shift)
     np, nq = _norm(post, eps, post_w, post_b, C, "post", idx), _norm(norm, eps, w, b, C, "norm", idx)
     with _lib.on_device(idx):
         st = _lib.load().regenvc_residual_norm_fwd(
@@ -258,7 +264,7 @@ def residual_norm_bwd(x_out: torch.Tensor, y: torch.Tensor, gh: torch.Tensor, gx
         dy, lddy = torch.empty(rows, C, dtype=act, device=dev), C
     else:
         lddy = _lib.matrix(dy, "dy", act, rows, C, idx)
-    groups = _groups(rows, group_rows)
+    groups, group_rows = _groups(rows, group_rows)
     v = _row_vectors(groups, C, group_rows, idx, gate, scale, None)
     np, nq = _norm(post, eps, post_w, post_b, C, "post", idx), _norm(norm, eps, w, b, C, "norm", idx)
 

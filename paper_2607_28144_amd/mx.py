@@ -43,6 +43,7 @@ class MxTensor:
 
 def mx_bytes(rows: int, cols: int) -> Tuple[int, int]:
     """Bytes of the codes and of the scales of a [rows, cols] matrix (regenvc_mx_bytes)."""
+    _lib.int32(rows=rows, cols=cols)
     nc, ns = ctypes.c_int64(), ctypes.c_int64()
     _lib.check(_lib.load().regenvc_mx_bytes(rows, cols, ctypes.byref(nc), ctypes.byref(ns)), "regenvc_mx_bytes")
     return nc.value, ns.value
@@ -95,6 +96,7 @@ def linear_workspace_bytes(M: int, N: int, K: int, quantized: bool) -> int:
     key = (M, N, K, quantized)
     need = _NEED.get(key)
     if need is None:
+        _lib.int32(M=M, N=N, K=K)
         out = ctypes.c_int64()
         st = _lib.load().regenvc_mx_linear_workspace(M, N, K, int(quantized), ctypes.byref(out))
         need = out.value if st == _lib.OK else 0  # a shape the call itself refuses: let it say so
@@ -151,6 +153,7 @@ class KvCache:
     def __init__(self, batch: int, capacity: int, heads: int, D: int, device="cuda"):
         if D not in (64, 128):
             raise ValueError(f"D={D} (64 or 128)")
+        _lib.int32(batch=batch, capacity=capacity, heads=heads)
         self.batch, self.capacity, self.heads, self.D = int(batch), int(capacity), int(heads), int(D)
         self.device = torch.device(device)
         if self.device.type != "cuda":
@@ -177,6 +180,8 @@ class KvCache:
                 or k.shape[3] != self.D:
             raise ValueError(f"k, v must be [{self.batch}, S, {self.heads}, {self.D}], got {tuple(k.shape)}, {tuple(v.shape)}")
         S = k.shape[1]
+        if S >= 1 << 31:
+            _lib.int32(S=S)
         idx = self.device.index
         kd, vd = _desc(k, "k", torch.bfloat16), _desc(v, "v", torch.bfloat16)
         if k.get_device() != idx or v.get_device() != idx:
@@ -209,6 +214,7 @@ def _attn_need(B: int, H: int, heads: int, Sq: int, max_len: int, D: int, idx: i
     key = (idx, B, H, heads, Sq, max_len, D)
     need = _ATTN_NEED.get(key)
     if need is None:
+        _lib.int32(B=B, H=H, Sq=Sq, max_len=max_len)
         out = ctypes.c_int64()
         st = _lib.load().regenvc_mx_attn_cache_workspace(B, H, heads, Sq, max_len, D, _lib.compute_units(idx),
                                                          ctypes.byref(out))
