@@ -31,3 +31,14 @@ def test_most_rows_of_a_dequantisation_are_those_of_one_launch(lib):
     n, m = ctypes.c_int64(), ctypes.c_int64()
     assert lib.regenvc_mx_bytes((1 << 26) - 1, 8, ctypes.byref(n), ctypes.byref(m)) == _lib.OK
     refused(lib, INV, "a NULL data pointer", lib.regenvc_mx_quantize(None, _lib.BF16, 8, A, B, (1 << 26) - 1, 8, None))
+
+
+def test_linear_workspace_holds_the_activations():
+    """What a bf16 operand needs is never less than its codes and scales, but for the rows that the few-row kernel
+    brings to MXFP4 itself."""
+    pytest.importorskip("torch")
+    from paper_2607_28144_amd import mx
+    for M, N, K in [(17, 16, 8), (65, 16, 8), (1365, 1536, 8960), (10920, 8960, 1536), (200, 8960, 8960), (16, 1536, 2056)]:
+        assert mx.linear_workspace_bytes(M, N, K, False) >= sum(mx.mx_bytes(M, K))
+        assert mx.linear_workspace_bytes(M, N, K, True) == 0
+    assert mx.linear_workspace_bytes(16, 1536, 2048, False) == 0
