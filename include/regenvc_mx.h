@@ -92,17 +92,22 @@ typedef struct {
    i < count[b], goes to place (start[b] + i) mod capacity; of more than
    `capacity` tokens only the last ones are kept.  start, count: int32 [B] in
    device memory, or NULL (0 and S); counts are held to [0, S], a sequence with
-   a negative start is left as it is.  No place but those is written. */
+   a negative start is left as it is.  No place but those is written.  B is at
+   most 65535, S heads D / 8 below 2^31. */
 regenvc_status regenvc_mx_cache_append(const regenvc_mx_cache *cache, const regenvc_tensor *k, const regenvc_tensor *v,
                                        int32_t S, const int32_t *start, const int32_t *count, void *stream);
 
-/* The cache's values: k, v bf16 or f32 [B, capacity, heads, D] contiguous. */
+/* The cache's values: k, v bf16 or f32 [B, capacity, heads, D] contiguous.  B is
+   at most 65535, capacity heads D / 8 below 2^31. */
 regenvc_status regenvc_mx_cache_values(const regenvc_mx_cache *cache, void *k, void *v, regenvc_dtype dtype,
                                        void *stream);
 
-/* Exact attention of q (bf16 [B, Sq, H, D], H a multiple of the cache's heads;
-   query head h reads key head h / (H / heads)) over the first lens[b] places of
-   each sequence:
+/* Attention of q (bf16 [B, Sq, H, D], H a multiple of the cache's heads; query
+   head h reads key head h / (H / heads)) over all of the first lens[b] places of
+   each sequence.  Scores and sums are fp32; a softmax weight is rounded to bf16
+   before it multiplies a value, whatever o_dtype is.  O, normalized by the sum of
+   the rounded weights, is within 2^-8 (sum of weight |v| + |O|) of the softmax's,
+   besides fp32 roundings; LSE takes the weights unrounded.
      o:    [B, Sq, H, D] in o_dtype; lse: f32 [B, H, Sq] or NULL
      lens: int32 [B] in device memory, held to [0, capacity], or NULL: max_len
            for all.  A sequence without a place gives O = 0, LSE = -inf.

@@ -194,8 +194,9 @@ __device__ __forceinline__ void row_stats(const Val &val, const bool (&on)[NV], 
 
 // Forward: WPR waves per row, NV eight-channel chunks per lane.  10920 x 1536,
 // norms on both sides, a modulation per 1560 rows, 201 MB: 35 us where two sets of
-// rows take turns, 41 with three (5.7 and 4.9 TB/s; a 2 GiB copy: 4.9); one row:
-// 3.6 us.
+// rows take turns, 41 with three (5.7 and 4.9 TB/s; a 2 GiB copy: 4.9, so that two
+// sets are partly read from the last-level cache); in f32 with three, 268 MB: 60 us
+// in a graph of such calls, where bf16 takes 45; one row: 3.6 us.
 template <int NV, int WPR, bool F32>
 __global__ __launch_bounds__(kThreads) void residual_norm_fwd_kernel(ResidualNormArgs a)
 {
@@ -296,18 +297,25 @@ __device__ __forceinline__ void join_stats(const Share *sh, int waves, int C, in
 //     dpost_w = sum du p           dpost_b = sum du
 // (without m(g), m(q) for RMS norms; dy = du without a post-norm).
 //
-// A row is worked on by W = ceil(C / 512) waves, eight channels per lane, so
-// that the sums over rows, a row's values and the next row's, already requested,
-// fit 128 registers a lane; a workgroup works on R rows at a time.  The waves
+// A row is worked on by W = ceil(C / 512) waves, eight channels per lane, which
+// hold the sums over rows, a row's values and the next row's, already requested,
+// in 130 to 185 registers a lane: three waves per SIMD with 3 sums or, in bf16,
+// 4, otherwise two; a workgroup works on R rows at a time.  The waves
 // of a row exchange their shares of its statistics through LDS: of both norms
 // in one step, then m(g), m(g n), then m(q), m(q p).  The sums over rows stay
 // in registers until a segment ends and are then added over the R rows through
 // LDS, in a fixed order: no atomics.  NS: sums held (3, 4 with a post-norm, 5
 // with its bias).
-// WIDE: more than eight waves.
+// WIDE: more than eight waves, so at most 128 registers a lane.  In bf16 3 sums
+// need two more; the others spill, 24 of them (3 sums in f32) to 110 (5), which
+// goes through memory beside the rows: 2000 x 8192 with 3, 4 and 5 sums 86, 136
+// and 182 us in bf16 (295 MB of rows), 114, 179 and 200 in f32 (393 MB).
 // 10920 x 1536 without a post-norm: 59 us, 302 MB, 5.1 TB/s; 1560 x 2048 with
 // one: 18.4 us, 57 MB, 3.1: 512 workgroups of three rows, whose sums (12.6 MB)
-// come on top.
+// come on top.  With the joining launch, three sets of tensors in turn, 10920 x
+// 1536 with 3, 4 and 5 sums: 72, 80 and 100 us in bf16, 97, 111 and 114 in f32;
+// with a modulation for every row, each of which is then a segment of its own
+// with nothing requested ahead of it, 123 and 146 with 3 sums.
 template <bool F32, int NS, bool WIDE>
 __global__ __launch_bounds__(WIDE ? 1024 : 512) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : NS == 3 ? 3 : 2)))
 void residual_norm_bwd_kernel(ResidualNormArgs a, ResidualNormPlan p, float *group_ws,
@@ -588,8 +596,9 @@ ResidualNormPlan residual_norm_plan(int rows, int C, int group_rows, int n_cu)
     p.rows_at_once = std::max(1, 4 / p.row_waves);
     // Workgroups per compute unit: as many as its registers hold, for the more rows are under way the better memory
     // latency passes, but each costs a row per sum in the workspace: a third one pays from 8 rows per workgroup on
-    // (10920 rows of 1536 channels: 106, 65 and 63 us with one, two and three; 1560 of 2048: 23, 18 and 20).  Never
-    // more workgroups than run at once: a second round costs as much as the first.
+    // (10920 rows of 1536 channels: 106, 65 and 63 us with one, two and three; 1560 of 2048: 23, 18 and 20).  Measured
+    // with 3 sums in bf16; the forms with 5 sums, and those in f32 with a post-norm, have registers for two, and the
+    // third's rows come in a second round (the times at the kernel), for what a plan goes by is rows and channels only.
     const int64_t per_cu = p.row_waves > 4 ? 1 : p.row_waves <= 3 && rows >= 24 * (int64_t)n_cu ? 3 : 2;
     const int64_t want = per_cu * n_cu;
     p.per_group = (int)std::max<int64_t>(1, std::min<int64_t>(want / p.groups, group_rows / p.rows_at_once));

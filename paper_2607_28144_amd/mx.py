@@ -229,9 +229,10 @@ def attn_cache_fwd(q: torch.Tensor, cache: KvCache, lens: Optional[torch.Tensor]
                    max_len: Optional[int] = None, out_dtype: torch.dtype = torch.bfloat16,
                    out: Optional[torch.Tensor] = None, return_lse: bool = True, lse_out: Optional[torch.Tensor] = None
                    ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
-    """Exact attention of q (bf16 [batch, Sq, H, D]; H a multiple of the
-    cache's heads) over the first lens[b] places of each sequence (int32 device
-    tensor; default max_len for all) (regenvc_mx_attn_cache_fwd).  max_len
+    """Attention of q (bf16 [batch, Sq, H, D]; H a multiple of the cache's
+    heads) over all of the first lens[b] places of each sequence (int32 device
+    tensor; default max_len for all) (regenvc_mx_attn_cache_fwd).  Softmax
+    weights multiply the values in bf16, whatever out_dtype is.  max_len
     (default: the capacity) is the length that the work is planned for.
     Returns (O, LSE or None); a sequence without a place gives 0 and -inf."""
     if q.dim() != 4:
