@@ -57,6 +57,35 @@ class MxAttnPlan(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tile_rows", "row_tiles", "key_ranges")]
 
 
+class PagePool(ctypes.Structure):
+    """regenvc_page_pool: device pointers and sizes of a bf16 key/value cache in pages."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "means")] + \
+               [(n, ctypes.c_int32) for n in ("pages", "page", "heads", "D")]
+
+
+class PageBatch(ctypes.Structure):
+    """regenvc_page_batch: the sequences of a call."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("table", "first", "lens")] + [("table_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("B", "columns", "T")]
+
+
+class RotaryTable(ctypes.Structure):
+    """regenvc_rotary: turns per position of the rotated pairs of a head."""
+    _fields_ = [("turns", ctypes.c_void_p), ("pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("amplitude", ctypes.c_float)]
+
+
+class PagedAttnShape(ctypes.Structure):
+    """regenvc_paged_attn_shape: what the plan of an attention call over pages goes by."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "H", "heads", "D", "page", "q_block", "count", "max_rows",
+                                              "max_len")]
+
+
+class PagedAttnPlan(ctypes.Structure):
+    """regenvc_paged_attn_plan: the decomposition of attention over pages."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("tile_rows", "key_ranges")]
+
+
 class Norm(ctypes.Structure):
     """regenvc_norm: a norm over a row, with its bf16 weights."""
     _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p)]
@@ -90,6 +119,8 @@ _i64 = ctypes.c_int64
 _PI64 = ctypes.POINTER(ctypes.c_int64)
 _PC = ctypes.POINTER(MxCache)
 _PN = ctypes.POINTER(Norm)
+_PP, _PB, _PR = ctypes.POINTER(PagePool), ctypes.POINTER(PageBatch), ctypes.POINTER(RotaryTable)
+_PS = ctypes.POINTER(PagedAttnShape)
 _SIGNATURES = {
     "regenvc_attn_fwd": [_PT, _PT, _PT, _PT, ctypes.c_int, ctypes.c_void_p,
                          _i32, _i32, _i32, _i32, _i32, ctypes.c_float, ctypes.c_void_p],
@@ -162,6 +193,12 @@ _SIGNATURES = {
                                   _p],
     "regenvc_mx_attn_cache_workspace": [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _PI64],
     "regenvc_mx_attn_cache_plan_query": [_i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(MxAttnPlan)],
+    "regenvc_paged_append": [_PP, _PB, _PT, _PT, _PT, _p, _p, ctypes.c_float, _PR, _PT, _i32, _p],
+    "regenvc_paged_select": [_PT, _PP, _PB, _i32, _i32, _i32, _i32, _i32, _i32, _p, _p],
+    "regenvc_paged_attn_fwd": [_PT, _PP, _PB, _p, _i32, _i32, _i32, _i32, _i32, _PT, ctypes.c_int, _p, _i32,
+                               ctypes.c_float, _p, _i64, _p],
+    "regenvc_paged_attn_workspace": [_PS, _i32, _PI64],
+    "regenvc_paged_attn_plan_query": [_PS, _i32, ctypes.POINTER(PagedAttnPlan)],
 }
 
 _lib = None

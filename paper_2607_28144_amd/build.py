@@ -16,13 +16,14 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_NAME = "libregenvc_attn.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 SOURCES = ["api.cpp", "attn_fwd.hip", "lse_merge.hip", "norm_rope.hip", "dit_api.cpp", "dit.hip", "vae_api.cpp",
-           "vae.hip", "residual_norm_api.cpp", "residual_norm.hip", "mx_api.cpp", "mx.hip", "mx_attn.hip"]
+           "vae.hip", "residual_norm_api.cpp", "residual_norm.hip", "mx_api.cpp", "mx.hip", "mx_attn.hip",
+           "paged_api.cpp", "paged.hip", "paged_attn.hip"]
 ARCH = "gfx950"
 # MFMA results in VGPRs: the score tiles feed VALU softmax code directly, and
 # read-only operands may then live in AGPRs; the MXFP4 tiles, whose accumulators
 # leave room beside them, are spared the moves between the two files.  Not for
 # the bf16 tile kernels, whose accumulators fill the AGPRs.
-VGPR_FORM = {"attn_fwd.hip", "mx.hip", "mx_attn.hip"}
+VGPR_FORM = {"attn_fwd.hip", "mx.hip", "mx_attn.hip", "paged_attn.hip"}
 # Sources with tiles whose MFMAs are instructions of their own (inline
 # assembly, around which the compiler places no wait states): their assembly is
 # checked (check_tile_kernels).

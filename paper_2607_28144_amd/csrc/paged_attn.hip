@@ -1,0 +1,483 @@
+// gfx950 attention of new tokens to a bf16 key/value cache in pages: to all
+// places of their sequence, or to the pages that a list selects.
+//
+// Scores are computed transposed, S^T = K Q^T, on v_mfma_f32_16x16x32_bf16: a
+// lane's accumulator holds, for one query row, keys 4 g .. 4 g + 3 of 16 (g =
+// lane / 16); rounded to bf16, two of them are the B operand of O^T = V^T P^T in
+// the key order {4 g + i, 16 + 4 g + i}, which the transposing LDS reads of V
+// follow.  The sum over d of K Q^T is taken in the order in which lane group g
+// has the D / 4 channels from D / 4 g on.
+//
+// Query heads that share a key head are rows of one tile: row r is query r / G
+// of head G hk + r % G.  Two running sums per row: O is divided by the sum of
+// the weights as rounded to bf16, LSE takes that of the unrounded ones.
+//
+// Keys go by units of 16 places, which always lie in one page.  A wave reads a
+// unit's rows through a buffer descriptor that ends with the last place that its
+// tile sees: what lies behind it comes back as zeros, whatever memory holds, as
+// do pages that do not exist.  The page numbers of a wave's next units are held
+// a lane each.
+#include "paged_kernels.hpp"
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "attn_device.hpp"
+#include "paged_device.hpp"
+
+namespace regenvc {
+namespace paged {
+namespace {
+
+using namespace cache_attn;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kUnit = 16;
+constexpr int kNowhere = 0x3fffffff;  // the place of a unit that does not exist: past every limit
+constexpr int kKeyAlign = 64;         // ranges of keys begin at multiples of it
+
+// What a workgroup works on: `rows` rows (query, head) of a block of queries, from
+// its row `row0` on, and keys [k0, k1) in units of 16.  Key i is place i, or with
+// selected pages place i % page of the page that entry i / page names.
+struct Work {
+    Block blk;
+    int hk, row0, rows, range;
+    int k0, k1;
+    int see, least;         // places that its last, its first row sees
+    const int32_t *pages;   // the sequence's row of the table
+    const int32_t *chosen;  // of the block and key head
+};
+
+template <bool SPARSE>
+__device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
+{
+    Work w;
+    uint32_t id = blockIdx.x;  // range, then key head, then tile, then block
+    const uint32_t ranges = p.key_ranges, heads = a.c.heads, tiles = p.tiles;
+    uint32_t q = id / ranges;
+    w.range = (int)(id - q * ranges);
+    uint32_t q2 = q / heads;
+    w.hk = (int)(q - q2 * heads);
+    const uint32_t j = q2 / tiles;
+    w.row0 = (int)(q2 - j * tiles) * p.tile_rows;
+    w.blk = block_of(a.n, a.c.shift, p.block, j);
+    const int G = a.H / a.c.heads, all = w.blk.rows * G;
+    w.rows = min(p.tile_rows, all - w.row0);
+    w.pages = a.n.table + w.blk.b * a.n.table_stride;
+    w.chosen = nullptr;
+    w.k0 = w.k1 = w.see = w.least = 0;
+    if (w.rows <= 0) return w;
+    const int first = w.blk.pos + w.row0 / G, last = w.blk.pos + (w.row0 + w.rows - 1) / G;
+    w.see = a.causal ? max(0, last + 1) : w.blk.len;
+    w.least = a.causal ? max(0, first + 1) : w.blk.len;
+    int keys = w.see;
+    if constexpr (SPARSE) {
+        w.chosen = a.selected + ((int64_t)j * a.c.heads + w.hk) * a.count;
+        // entries behind the last that is none
+        int n = 0;
+        for (int i = threadIdx.x & 63; i < a.count; i += 64)
+            if (w.chosen[i] >= 0) n = i + 1;
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) n = max(n, __shfl_xor(n, m, 64));
+        keys = __builtin_amdgcn_readfirstlane(n) << a.c.shift;
+    }
+    const uint32_t units = ((uint32_t)keys + kKeyAlign - 1) / kKeyAlign;  // < 2^26
+    w.k0 = (int)((uint64_t)units * w.range / ranges) * kKeyAlign;
+    w.k1 = min(keys, (int)((uint64_t)units * (w.range + 1) / ranges) * kKeyAlign);
+    return w;
+}
+
+// Where the unit from key i on lies: its page in the pool (-1: nowhere) and its first place.
+struct Unit {
+    int page, place;
+};
+template <bool SPARSE>
+__device__ __forceinline__ Unit unit_at(const AttnArgs &a, const Work &w, int i)
+{
+    Unit u{-1, kNowhere};
+    if (i >= w.k1) return u;
+    int col = i >> a.c.shift, place = i;
+    if constexpr (SPARSE) {
+        col = w.chosen[col];
+        if (col < 0 || col >= a.n.columns) return u;
+        place = (col << a.c.shift) + (i & ((1 << a.c.shift) - 1));
+    }
+    if (place >= w.see) return u;
+    const int page = w.pages[col];
+    if (page < 0 || page >= a.c.pages) return u;
+    u.page = page;
+    u.place = place;
+    return u;
+}
+
+// A descriptor of the unit's rows of one head, as many as its tile sees.
+template <int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const AttnArgs &a, const Work &w, uint16_t *base, int page, int place)
+{
+    const int n = max(0, min(kUnit, w.see - place));
+    const int64_t row = (((int64_t)max(page, 0) * a.c.heads + w.hk) << a.c.shift) + (place & ((1 << a.c.shift) - 1));
+    return __builtin_amdgcn_make_buffer_rsrc(base + row * D, 0, n * D * 2, 0x00027000);
+}
+__device__ __forceinline__ u32x4 load_rows(__amdgpu_buffer_rsrc_t r, int at, int imm)
+{
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + imm, 0, 0));
+}
+
+// Partial results of the key ranges in the workspace: O (f32, normalized over
+// the range) [range][row][head][D], then LSE in log2 units [range][row][head]
+// (-inf: no key).
+__device__ __forceinline__ float *part_o(const AttnArgs &a, int64_t range, int64_t t, int64_t h)
+{
+    return reinterpret_cast<float *>(a.ws) + ((range * a.n.T + t) * a.H + h) * a.c.D;
+}
+__device__ __forceinline__ float *part_lse(const AttnArgs &a, int64_t ranges, int64_t range, int64_t t, int64_t h)
+{
+    return reinterpret_cast<float *>(a.ws) + ranges * a.n.T * a.H * a.c.D + (range * a.n.T + t) * a.H + h;
+}
+__device__ __forceinline__ void store_out4(const AttnArgs &a, int64_t t, int64_t h, int d, f32x4 v)
+{
+    const int64_t at = t * a.o_ss + h * a.o_sh + d;
+    if (a.f32) {
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.o) + at) = v;
+    } else {
+        const bf16x4 o = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+        *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.o) + at) = o;
+    }
+}
+
+// Row r of the tile: the channels D / 4 g + 8 s + 0..7 of it for s < D / 32, and the places that it sees.
+template <int D>
+__device__ __forceinline__ int load_q(const AttnArgs &a, const Work &w, int r, int G, bf16x8 (&q)[D / 32])
+{
+    const int g = (threadIdx.x & 63) >> 4, at = w.row0 + max(0, min(r, w.rows - 1));
+    const int query = at / G;
+    const uint16_t *p = a.q + (int64_t)(w.blk.row + query) * a.q_ss + (int64_t)(w.hk * G + at - query * G) * a.q_sh + D / 4 * g;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(p + 8 * s);
+    return a.causal ? max(0, w.blk.pos + query + 1) : w.blk.len;
+}
+
+// Few rows (tiles of 16 MB): memory-bound.  Every wave walks key tiles of its
+// own, 32 keys at a time, with nothing shared: K goes from memory to registers
+// and the matrix unit; V through 2 D x 32 bytes of wave-private LDS, for the
+// transposition.  The waves' results meet in LDS.
+constexpr int kFewWaves = 4;
+
+template <int D, int MB, bool SPARSE>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void attn_few_kernel(AttnArgs a, AttnPlan p)
+{
+    constexpr int KS = D / 32, DB = D / 16, CH = D / 8;  // CH: 16-byte chunks of a row
+    constexpr int VR = 64 / CH, NVJ = 32 / VR;           // rows of V that a load of the wave takes, and the loads
+    constexpr int V_BYTES = 32 * D * 2;
+    constexpr int RED = kFewWaves * 16 * MB * D * 4;
+    constexpr int LDS = kFewWaves * V_BYTES > RED ? kFewWaves * V_BYTES : RED;
+    __shared__ __attribute__((aligned(1024))) char smem[LDS];
+    __shared__ float stat[kFewWaves][3][16 * MB];
+    const int lane = threadIdx.x & 63, g = lane >> 4, x = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Work w = work_of<SPARSE>(a, p);
+    if (w.rows <= 0) return;
+    const int G = a.H / a.c.heads;
+    const float c = log2_scale(a.scale);
+
+    bf16x8 q[MB][KS];
+    int lim[MB];  // places that this lane's rows see
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) lim[mb] = load_q<D>(a, w, mb * 16 + x, G, q[mb]);
+    f32x4 o[MB][DB];
+    float m[MB], l[MB], r[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        m[mb] = kNone, l[mb] = r[mb] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[mb][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // Units of this wave's tiles i = 0, 1, ... (keys key_of(i) .. + 31), two each: lane 32 h + i % 32 holds half h of tile
+    // i of 32, and those of the 32 tiles after them.
+    const int step = 32 * kFewWaves, begin = w.k0 + 32 * wave;
+    const int tiles = max(0, (w.k1 - begin + step - 1) / step);
+    auto units = [&](int i0) { return unit_at<SPARSE>(a, w, begin + (i0 + (lane & 31)) * step + (lane >> 5) * kUnit); };
+    Unit now = units(0), later = units(32);
+    struct Piece {
+        u32x4 k[2][KS], v[NVJ];
+        int place[2];
+    };
+    auto load = [&](Piece &t, int i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int page = __builtin_amdgcn_readlane(now.page, (i & 31) + 32 * h);
+            const int place = __builtin_amdgcn_readlane(now.place, (i & 31) + 32 * h);
+            t.place[h] = place;
+            const __amdgpu_buffer_rsrc_t rk = rows_of<D>(a, w, a.c.k, page, place), rv = rows_of<D>(a, w, a.c.v, page, place);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) t.k[h][s] = load_rows(rk, x * D * 2 + g * D / 2, s * 16);
+#pragma unroll
+            for (int j = 0; j < NVJ / 2; ++j) t.v[h * (NVJ / 2) + j] = load_rows(rv, lane * 16, j * 1024);
+        }
+    };
+    lds_char *vl = (lds_char *)smem + wave * V_BYTES;
+    Piece cur, nxt;
+    if (tiles > 0) load(cur, 0);
+    for (int i = 0; i < tiles; ++i) {
+        if (((i + 1) & 31) == 0) {
+            now = later;
+            later = units(i + 1 + 32);
+        }
+        if (i + 1 < tiles) load(nxt, i + 1);  // in flight beside this tile
+#pragma unroll
+        for (int j = 0; j < NVJ; ++j) {
+            const int row = lane / CH + VR * j;
+            *(__attribute__((address_space(3))) u32x4 *)(vl + row * D * 2 + v_slot<D>(row, lane % CH) * 16) = cur.v[j];
+        }
+        f32x4 s[MB][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                s[mb][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < KS; ++t)
+                    s[mb][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, cur.k[h][t]), q[mb][t],
+                                                                       s[mb][h], 0, 0, 0);
+            }
+        if (max(cur.place[0], cur.place[1]) + kUnit > w.least) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (cur.place[e >> 2] + 4 * g + (e & 3) >= lim[mb]) s[mb][e >> 2][e & 3] = -INFINITY;
+        }
+        bf16x8 pw[MB];
+        float le[MB], re[MB];
+        bool over = false;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            weights32(s[mb], c, m[mb], le[mb], re[mb], pw[mb]);
+            over |= !(le[mb] <= kSpecLimit);
+        }
+        if (__builtin_amdgcn_ballot_w64(over) != 0) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                float t = s[mb][0][0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) t = fmaxf(t, s[mb][e >> 2][e & 3]);
+                const float mn = fmaxf(m[mb], quad_max(t) * c);
+                const float alpha = __builtin_amdgcn_exp2f(m[mb] - mn);
+                m[mb] = mn;
+                l[mb] *= alpha, r[mb] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[mb][d] *= alpha;
+                weights32(s[mb], c, mn, le[mb], re[mb], pw[mb]);
+            }
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) l[mb] += le[mb], r[mb] += re[mb];
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            const int row = 4 * g + (x >> 2), col = d * 16 + 4 * (x & 3);
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lds_bf16x4 *)(vl + row * D * 2 + v_slot<D>(row, col >> 3) * 16 + (col & 7) * 2));
+            const bf16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (lds_bf16x4 *)(vl + (row + 16) * D * 2 + v_slot<D>(row + 16, col >> 3) * 16 + (col & 7) * 2));
+            const bf16x8 vf = {lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) o[mb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pw[mb], o[mb][d], 0, 0, 0);
+        }
+        cur = nxt;
+    }
+    // the four waves' results, in a fixed order
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        l[mb] = quad_sum(l[mb]);
+        r[mb] = quad_sum(r[mb]);
+        if (g == 0) stat[wave][0][mb * 16 + x] = m[mb], stat[wave][1][mb * 16 + x] = l[mb], stat[wave][2][mb * 16 + x] = r[mb];
+    }
+    __syncthreads();  // also: no wave reads V from LDS any more
+    float *sum = reinterpret_cast<float *>(smem) + wave * 16 * MB * D;  // [wave][row][D]
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const int row = mb * 16 + x;
+        float mm = stat[0][0][row];
+#pragma unroll
+        for (int t = 1; t < kFewWaves; ++t) mm = fmaxf(mm, stat[t][0][row]);
+        const float f = __builtin_amdgcn_exp2f(m[mb] - mm);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+            *reinterpret_cast<f32x4 *>(sum + row * D + (((d * 4 + g) ^ (x & 7)) * 4)) = o[mb][d] * f;
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < w.rows * (D / 4); t += 64 * kFewWaves) {
+        const int row = t / (D / 4), d4 = t % (D / 4);
+        float mm = stat[0][0][row];
+#pragma unroll
+        for (int k = 1; k < kFewWaves; ++k) mm = fmaxf(mm, stat[k][0][row]);
+        float ll = 0.f, rr = 0.f;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k) {
+            const float f = __builtin_amdgcn_exp2f(stat[k][0][row] - mm);
+            ll = fmaf(stat[k][1][row], f, ll);
+            rr = fmaf(stat[k][2][row], f, rr);
+        }
+        const bool none = ll == 0.f;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k)
+            v += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(smem) + (k * 16 * MB + row) * D +
+                                                  ((d4 ^ (row & 7)) * 4));
+        v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : v * (1.0f / rr);
+        const float lse2 = none ? -INFINITY : mm + __builtin_amdgcn_logf(ll);
+        const int64_t at = w.row0 + row, tok = w.blk.row + at / G, h = w.hk * G + at % G;
+        if (p.key_ranges == 1) {
+            store_out4(a, tok, h, d4 * 4, v);
+            if (d4 == 0 && a.lse != nullptr) a.lse[h * a.n.T + tok] = lse2 * kLn2;
+        } else {
+            *reinterpret_cast<f32x4 *>(part_o(a, w.range, tok, h) + d4 * 4) = v;
+            if (d4 == 0) *part_lse(a, p.key_ranges, w.range, tok, h) = lse2;
+        }
+    }
+}
+
+// Whether row t belongs to a sequence: no other is written.
+__device__ __forceinline__ bool covered(const Batch &n, int64_t t)
+{
+    return t >= n.first[0] && t < n.first[n.B];
+}
+
+// The key ranges' partial results joined, in order.  Up to kFewRanges of them:
+// D / 4 lanes per (row, head), R >= ranges of them read at once.
+constexpr int kFewRanges = 8;
+template <int D, int R>
+__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, int ranges)
+{
+    constexpr int LPR = D / 4;
+    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
+    if (id >= (int64_t)a.n.T * a.H) return;
+    const int d = threadIdx.x % LPR * 4;
+    const int64_t h = id % a.H, t = id / a.H;
+    if (!covered(a.n, t)) return;
+    float lse[R];
+    f32x4 part[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {  // past the last range that again, with no weight
+        lse[k] = *part_lse(a, ranges, min(k, ranges - 1), t, h);
+        part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, min(k, ranges - 1), t, h) + d);
+    }
+    float m = lse[0];
+#pragma unroll
+    for (int k = 1; k < R; ++k) m = fmaxf(m, lse[k]);
+    m = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const float f = k < ranges ? __builtin_amdgcn_exp2f(lse[k] - m) : 0.f;
+        l += f;
+        o += part[k] * f;
+    }
+    store_out4(a, t, h, d, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.0f / l));
+    if (d == 0 && a.lse != nullptr) a.lse[h * a.n.T + t] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// More: a workgroup per (row, head), D / 4 lanes along the channels and 1024 /
+// D along the ranges, whose sums meet in LDS.
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int ranges)
+{
+    constexpr int LPR = D / 4, SL = 256 / LPR;
+    __shared__ float weight[64], total;
+    __shared__ f32x4 sum[SL][LPR];
+    const int i = threadIdx.x, d = i % LPR, slice = i / LPR;
+    const int64_t id = blockIdx.x, h = id % a.H, t = id / a.H;
+    if (!covered(a.n, t)) return;
+    constexpr int KEEP = 64 / SL;  // requested before the weights are known
+    f32x4 part[KEEP];
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+        part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, min(k * SL + slice, ranges - 1), t, h) + d * 4);
+    if (i < 64) {
+        const float e = i < ranges ? *part_lse(a, ranges, i, t, h) : -INFINITY;
+        float m = e;
+#pragma unroll
+        for (int s = 32; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+        m = m == -INFINITY ? 0.f : m;
+        const float f = __builtin_amdgcn_exp2f(e - m);
+        weight[i] = f;
+        float l = f;
+#pragma unroll
+        for (int s = 32; s >= 1; s >>= 1) l += __shfl_xor(l, s, 64);
+        if (i == 0) {
+            total = l;
+            if (a.lse != nullptr) a.lse[h * a.n.T + t] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        }
+    }
+    __syncthreads();
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+        if (k * SL + slice < ranges) o += part[k] * weight[k * SL + slice];
+    sum[slice][d] = o;
+    __syncthreads();
+    if (slice != 0) return;
+#pragma unroll
+    for (int k = 1; k < SL; ++k) o += sum[k][d];
+    store_out4(a, t, h, d * 4, total == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.0f / total));
+}
+
+template <int D, bool SPARSE>
+hipError_t launch_tiles(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(((int64_t)a.n.T / p.block + a.n.B) * p.tiles * a.c.heads * p.key_ranges));
+    switch (p.tile_rows) {
+    case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
+    case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
+    default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_d(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    const hipError_t e = a.selected != nullptr ? launch_tiles<D, true>(a, p, stream) : launch_tiles<D, false>(a, p, stream);
+    if (e != hipSuccess || p.key_ranges == 1) return e;
+    const int64_t rows = (int64_t)a.n.T * a.H;
+    const dim3 few((unsigned)((rows * (D / 4) + 255) / 256));
+    if (p.key_ranges <= 2)
+        hipLaunchKernelGGL((attn_join_few_kernel<D, 2>), few, dim3(256), 0, stream, a, p.key_ranges);
+    else if (p.key_ranges <= 4)
+        hipLaunchKernelGGL((attn_join_few_kernel<D, 4>), few, dim3(256), 0, stream, a, p.key_ranges);
+    else if (p.key_ranges <= kFewRanges)
+        hipLaunchKernelGGL((attn_join_few_kernel<D, kFewRanges>), few, dim3(256), 0, stream, a, p.key_ranges);
+    else
+        hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)rows), dim3(256), 0, stream, a, p.key_ranges);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AttnPlan attn_plan(const AttnShape &s, int n_cu)
+{
+    AttnPlan p{};
+    const int64_t G = s.H / s.heads, queries = s.count > 0 ? std::min(s.q_block, s.max_rows) : s.max_rows;
+    p.tile_rows = queries * G <= 16 ? 16 : 32;
+    p.block = s.count > 0 ? s.q_block : (int)std::max<int64_t>(1, p.tile_rows / G);
+    p.tiles = (int)((std::min(p.block, s.T) * G + p.tile_rows - 1) / p.tile_rows);
+    // As many ranges as fill the compute units with two workgroups each, of at least two rounds of a workgroup's waves.
+    const int64_t units = ((int64_t)s.T / p.block + std::min(s.B, s.T)) * p.tiles * s.heads;
+    const int64_t keys = s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len;
+    const int64_t slots = 2 * (int64_t)n_cu;
+    p.key_ranges = (int32_t)std::max<int64_t>(1, std::min({slots / std::max<int64_t>(1, units), keys / 256, (int64_t)64}));
+    p.ws_bytes = p.key_ranges > 1 ? p.key_ranges * ((int64_t)s.T * s.H * (s.D + 1)) * (int64_t)sizeof(float) : 0;
+    return p;
+}
+
+hipError_t launch_attn(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
+{
+    return a.c.D == 128 ? launch_d<128>(a, p, stream) : launch_d<64>(a, p, stream);
+}
+
+}  // namespace paged
+}  // namespace regenvc

@@ -1,0 +1,63 @@
+// Device helpers of the kernels of a cache in pages: which sequence a piece of
+// a call belongs to.
+#pragma once
+#include "paged_kernels.hpp"
+
+namespace regenvc {
+namespace paged {
+
+__device__ __forceinline__ int first_of(const Batch &n, int b)
+{
+    return max(0, min(n.first[b], n.T));
+}
+__device__ __forceinline__ int places_of(const Batch &n, int b, int shift)
+{
+    return max(0, min(n.lens[b], n.columns << shift));
+}
+
+// The last sequence whose first piece is at most j, or -1; from(b) ascends.
+// Every lane of the wave takes part and gets the answer: 64 sequences are
+// looked at together, so up to 64 cost one load.
+template <typename F>
+__device__ __forceinline__ int last_from(int B, int64_t j, F from)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = B;
+    while (n > 0) {
+        const int step = (n + 63) >> 6, b = lo + lane * step;
+        const bool le = b < lo + n && from(min(b, B - 1)) <= j;
+        const int c = __popcll(__builtin_amdgcn_ballot_w64(le));
+        if (c == 0) return -1;
+        const int at = lo + (c - 1) * step;
+        if (step == 1) return at;
+        n = min(step, lo + n - at);
+        lo = at;
+    }
+    return -1;
+}
+
+// The queries of block j: rows row .. row + rows - 1, of which the first stands
+// at place `pos` of sequence b, which has `len` places.  rows 0: no such block.
+// A sequence's blocks begin at first[b] / size + b, so that T / size + B numbers
+// are enough for any division of T rows into B sequences.
+struct Block {
+    int b, row, rows, pos, len;
+};
+__device__ __forceinline__ Block block_of(const Batch &n, int shift, int size, int64_t j)
+{
+    Block k{0, 0, 0, 0, 0};
+    const int b = last_from(n.B, j, [&](int i) { return (int64_t)(first_of(n, i) / size) + i; });
+    if (b < 0) return k;
+    const int f0 = first_of(n, b), f1 = first_of(n, b + 1);
+    const int64_t at = (j - f0 / size - b) * size;
+    if (at >= f1 - f0) return k;
+    k.b = b;
+    k.row = f0 + (int)at;
+    k.rows = min(size, f1 - k.row);
+    k.len = places_of(n, b, shift);
+    k.pos = k.len - (f1 - k.row);
+    return k;
+}
+
+}  // namespace paged
+}  // namespace regenvc
