@@ -39,11 +39,13 @@ constexpr int kNowhere = 0x3fffffff;  // the place of a unit that does not exist
 constexpr int kKeyAlign = 64;         // ranges of keys begin at multiples of it
 
 // What a workgroup works on: `rows` rows (query, head) of a block of queries, from
-// its row `row0` on, and keys [k0, k1) in units of 16.  Key i is place i, or with
-// selected pages place i % page of the page that entry i / page names.
+// its row `row0` on, and of their keys range `range` of `ranges`, [k0, k1) in units
+// of 16.  Key i is place i, or with selected pages place i % page of the page that
+// entry i / page names.  A tile of many keys is cut into more ranges than one of
+// few: sequences of a call differ, and the longest would be the last to end.
 struct Work {
     Block blk;
-    int hk, row0, rows, range;
+    int hk, row0, rows, range, ranges;
     int k0, k1;
     int see, least;         // places that its last, its first row sees
     const int32_t *pages;   // the sequence's row of the table
@@ -54,11 +56,12 @@ template <bool SPARSE>
 __device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
 {
     Work w;
-    uint32_t id = blockIdx.x;  // range, then key head, then tile, then block
-    const uint32_t ranges = p.key_ranges, heads = a.c.heads, tiles = p.tiles;
-    uint32_t q = id / ranges;
-    w.range = (int)(id - q * ranges);
-    uint32_t q2 = q / heads;
+    // range, then key head, then tile, then block, the last one first: in a causal call it has the most keys
+    const uint32_t id = gridDim.x - 1 - blockIdx.x;
+    const uint32_t heads = a.c.heads, tiles = p.tiles;
+    const uint32_t q = id / (uint32_t)p.key_ranges;
+    w.range = (int)(id - q * p.key_ranges);
+    const uint32_t q2 = q / heads;
     w.hk = (int)(q - q2 * heads);
     const uint32_t j = q2 / tiles;
     w.row0 = (int)(q2 - j * tiles) * p.tile_rows;
@@ -67,6 +70,7 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
     w.rows = min(p.tile_rows, all - w.row0);
     w.pages = a.n.table + w.blk.b * a.n.table_stride;
     w.chosen = nullptr;
+    w.ranges = 1;
     w.k0 = w.k1 = w.see = w.least = 0;
     if (w.rows <= 0) return w;
     const int first = w.blk.pos + w.row0 / G, last = w.blk.pos + (w.row0 + w.rows - 1) / G;
@@ -83,9 +87,15 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
         for (int m = 32; m >= 1; m >>= 1) n = max(n, __shfl_xor(n, m, 64));
         keys = __builtin_amdgcn_readfirstlane(n) << a.c.shift;
     }
-    const uint32_t units = ((uint32_t)keys + kKeyAlign - 1) / kKeyAlign;  // < 2^26
-    w.k0 = (int)((uint64_t)units * w.range / ranges) * kKeyAlign;
-    w.k1 = min(keys, (int)((uint64_t)units * (w.range + 1) / ranges) * kKeyAlign);
+    const uint32_t units = ((uint32_t)keys + kKeyAlign - 1) / kKeyAlign;  // < 2^24, ranges <= 64
+    const uint32_t ranges = max(1u, min((uint32_t)p.key_ranges, (units + p.range_units - 1) / p.range_units));
+    w.ranges = (int)ranges;
+    if (w.range >= w.ranges) {
+        w.rows = 0;
+        return w;
+    }
+    w.k0 = (int)(units * w.range / ranges) * kKeyAlign;
+    w.k1 = min(keys, (int)(units * (w.range + 1) / ranges) * kKeyAlign);
     return w;
 }
 
@@ -112,22 +122,51 @@ __device__ __forceinline__ Unit unit_at(const AttnArgs &a, const Work &w, int i)
     return u;
 }
 
-// A descriptor of the unit's rows of one head, as many as its tile sees.
+// A buffer descriptor of the unit's rows of one head, as many as its tile sees: loads behind them give zeros.
 template <int D>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const AttnArgs &a, const Work &w, uint16_t *base, int page, int place)
+__device__ __forceinline__ u32x4 rows_of(const AttnArgs &a, const Work &w, uint16_t *base, int page, int place)
 {
-    const int n = max(0, min(kUnit, w.see - place));
+    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kUnit, w.see - place)));  // uniform as it is, in a scalar
     const int64_t row = (((int64_t)max(page, 0) * a.c.heads + w.hk) << a.c.shift) + (place & ((1 << a.c.shift) - 1));
-    return __builtin_amdgcn_make_buffer_rsrc(base + row * D, 0, n * D * 2, 0x00027000);
+    const uint64_t at = (uint64_t)(base + row * D);
+    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffff, (uint32_t)(n * D * 2), 0x00027000};
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(u32x4 r)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)r[1] << 32 | r[0]), 0, (int)r[2], (int)r[3]);
 }
 __device__ __forceinline__ u32x4 load_rows(__amdgpu_buffer_rsrc_t r, int at, int imm)
 {
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + imm, 0, 0));
 }
 
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// N loads of 16 bytes a lane from a descriptor's rows to LDS, lane i's 16 bytes of load j to dst + 1024 j + 16 i from 1024 j
+// + at[j] on.  Inline, because the compiler would wait for them before every later LDS read; who reads them waits by
+// itself.  The nops: scalars written just before, M0 too.
+template <int N>
+__device__ __forceinline__ void rows_to_lds(uint32_t dst, const uint32_t (&at)[N], u32x4 r)
+{
+    static_assert(N == 2 || N == 4, "16 rows of 128 or 256 bytes");
+    if constexpr (N == 4)
+        __asm__ volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
+                         "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
+                         "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds"
+                         : : "s"(dst), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(r) : "m0", "memory");
+    else
+        __asm__ volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds"
+                         : : "s"(dst), "v"(at[0]), "v"(at[1]), "s"(r) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
 // Partial results of the key ranges in the workspace: O (f32, normalized over
 // the range) [range][row][head][D], then LSE in log2 units [range][row][head]
-// (-inf: no key).
+// (-inf: no key), then the number of ranges [row][head] (1: the result is in place).
 __device__ __forceinline__ float *part_o(const AttnArgs &a, int64_t range, int64_t t, int64_t h)
 {
     return reinterpret_cast<float *>(a.ws) + ((range * a.n.T + t) * a.H + h) * a.c.D;
@@ -135,6 +174,10 @@ __device__ __forceinline__ float *part_o(const AttnArgs &a, int64_t range, int64
 __device__ __forceinline__ float *part_lse(const AttnArgs &a, int64_t ranges, int64_t range, int64_t t, int64_t h)
 {
     return reinterpret_cast<float *>(a.ws) + ranges * a.n.T * a.H * a.c.D + (range * a.n.T + t) * a.H + h;
+}
+__device__ __forceinline__ int *part_ranges(const AttnArgs &a, int64_t ranges, int64_t t, int64_t h)
+{
+    return reinterpret_cast<int *>(a.ws) + ranges * a.n.T * a.H * (a.c.D + 1) + t * a.H + h;
 }
 __device__ __forceinline__ void store_out4(const AttnArgs &a, int64_t t, int64_t h, int d, f32x4 v)
 {
@@ -145,6 +188,15 @@ __device__ __forceinline__ void store_out4(const AttnArgs &a, int64_t t, int64_t
         const bf16x4 o = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
         *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.o) + at) = o;
     }
+}
+
+__device__ __forceinline__ void store_lse(const AttnArgs &a, const AttnPlan &p, const Work &w, int64_t t, int64_t h, float lse2)
+{
+    if (p.key_ranges > 1 && w.range == 0) *part_ranges(a, p.key_ranges, t, h) = w.ranges;
+    if (w.ranges > 1)
+        *part_lse(a, p.key_ranges, w.range, t, h) = lse2;
+    else if (a.lse != nullptr)
+        a.lse[h * a.n.T + t] = lse2 * kLn2;
 }
 
 // Row r of the tile: the channels D / 4 g + 8 s + 0..7 of it for s < D / 32, and the places that it sees.
@@ -211,7 +263,8 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
             const int page = __builtin_amdgcn_readlane(now.page, (i & 31) + 32 * h);
             const int place = __builtin_amdgcn_readlane(now.place, (i & 31) + 32 * h);
             t.place[h] = place;
-            const __amdgpu_buffer_rsrc_t rk = rows_of<D>(a, w, a.c.k, page, place), rv = rows_of<D>(a, w, a.c.v, page, place);
+            const __amdgpu_buffer_rsrc_t rk = resource(rows_of<D>(a, w, a.c.k, page, place));
+            const __amdgpu_buffer_rsrc_t rv = resource(rows_of<D>(a, w, a.c.v, page, place));
 #pragma unroll
             for (int s = 0; s < KS; ++s) t.k[h][s] = load_rows(rk, x * D * 2 + g * D / 2, s * 16);
 #pragma unroll
@@ -330,13 +383,315 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
         v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : v * (1.0f / rr);
         const float lse2 = none ? -INFINITY : mm + __builtin_amdgcn_logf(ll);
         const int64_t at = w.row0 + row, tok = w.blk.row + at / G, h = w.hk * G + at % G;
-        if (p.key_ranges == 1) {
+        if (w.ranges == 1)
             store_out4(a, tok, h, d4 * 4, v);
-            if (d4 == 0 && a.lse != nullptr) a.lse[h * a.n.T + tok] = lse2 * kLn2;
-        } else {
+        else
             *reinterpret_cast<f32x4 *>(part_o(a, w.range, tok, h) + d4 * 4) = v;
-            if (d4 == 0) *part_lse(a, p.key_ranges, w.range, tok, h) = lse2;
+        if (d4 == 0) store_lse(a, p, w, tok, h, lse2);
+    }
+}
+
+// Many rows: matrix- and vector-bound, on the schedule of the other caches'
+// attention.  Eight waves of 32 rows, two per SIMD: waves 0-3 and 4-7 alternate, in
+// opposite phases, between
+//   M(u): matrix instructions only: O^T += V^T P^T of tile u - 1, then S^T = K
+//         Q^T of tile u (64 keys), fragments read kAhead of them ahead;
+//   V(u): vector instructions only: the weights of tile u, and this wave's part of
+//         tile u + 3 (K's for waves 0-3, V's for waves 4-7) asked for, to LDS,
+// with a barrier between phases, so that a SIMD's matrix unit works for one
+// wave while its vector unit works for the other.  LDS is a ring of four stages:
+// tile u + 3 goes where tile u - 1 was.  Its K was last read by M(u - 1) of waves
+// 4-7, its V by M(u) of waves 4-7: a barrier before V(u) of the waves that load it.
+constexpr int kManyWaves = 8, kManyRows = 32 * kManyWaves, kManyKeys = 64;
+
+template <int D, bool SPARSE>
+__global__ __launch_bounds__(64 * kManyWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void attn_many_kernel(AttnArgs a, AttnPlan p)
+{
+    constexpr int KS = D / 32, DB = D / 16, CH = D / 8;  // CH: 16-byte chunks of a row
+    constexpr int T_BYTES = kManyKeys * D * 2, STAGE = 2 * T_BYTES;  // a K or V tile; both
+    __shared__ __attribute__((aligned(1024))) char smem[4 * STAGE];
+    __shared__ int holes[kManyWaves];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int grp = wave >> 2, g = lane >> 4, x = lane & 15;
+    const Work w = work_of<SPARSE>(a, p);
+    if (w.rows <= 0) return;
+    const int G = a.H / a.c.heads;
+    const int row0 = wave * 32;  // of the tile
+    const float c = a.scale * kLog2e;
+    const int T = (w.k1 - w.k0 + kManyKeys - 1) / kManyKeys;  // tiles of keys
+
+    bf16x8 qf[2][KS];
+    int lim[2];  // places that this lane's rows see, less its first key of a unit
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) lim[qb] = load_q<D>(a, w, row0 + qb * 16 + x, G, qf[qb]) - 4 * g;
+    f32x4 o[DB][2], s[4][2];
+    bf16x8 pw[2][2];
+    float mref[2] = {kNone, kNone}, lsum[2] = {0.f, 0.f}, rsum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db][0] = o[db][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // This wave's unit of a tile: K's (waves 0-3) or V's (4-7) rows 16 (wave % 4) .. + 15.  Lane i has where it lies in
+    // tile i of 64, and in those of the 64 tiles after them.
+    const int mine = (wave & 3) * kUnit;
+    uint16_t *const base = grp ? a.c.v : a.c.k;  // wave-uniform
+    constexpr int VR = 64 / CH, NL = kUnit / VR;  // rows that a load of the wave takes, and the loads
+    auto units = [&](int u0) { return unit_at<SPARSE>(a, w, w.k0 + (u0 + lane) * kManyKeys + mine); };
+    Unit now = units(0), later = units(64);
+    // Whether a page of those units does not exist: then all waves look every tile's pages up again.
+    auto hole = [&](const Unit &x, int u0) {
+        return __builtin_amdgcn_ballot_w64(x.page < 0 && w.k0 + (u0 + lane) * kManyKeys + mine < w.k1) != 0;
+    };
+    if (!SPARSE) holes[wave] = hole(now, 0) || hole(later, 64);
+    // Where a load of the wave finds what its lanes' places in LDS hold: chunks change places with the row (v_slot, k_slot).
+    uint32_t vofs[NL];
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+        const int row = VR * j + lane / CH, ch = lane % CH;
+        vofs[j] = lane / CH * D * 2 + (grp ? v_slot<D>(row, ch) : k_slot<D>(row, ch)) * 16;
+    }
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char *)smem + (grp ? T_BYTES : 0) + mine * D * 2);
+    auto load = [&](int u) __attribute__((always_inline)) {  // tile u to LDS, asked for in order; zeros where there is none
+        if ((u & 63) == 0 && u > 0) {
+            now = later;
+            later = units(u + 64);
+            if (!SPARSE && hole(later, u + 64)) holes[wave] = 1;  // read 61 tiles later or more
         }
+        const u32x4 r = rows_of<D>(a, w, base, __builtin_amdgcn_readlane(now.page, u & 63),
+                                   __builtin_amdgcn_readlane(now.place, u & 63));
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + (u & 3) * STAGE);
+        rows_to_lds(dst, vofs, r);
+    };
+    // the loads of all tiles but the last two asked for have landed
+    auto landed = [&]() __attribute__((always_inline)) { __asm__ volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * NL) : "memory"); };
+    // The first places of a tile's four units: with selected pages lane i has those of tile i of 64.
+    int at4[4] = {kNowhere, kNowhere, kNowhere, kNowhere};
+    int gaps = 0;
+    auto places = [&](int u, int (&pl)[4]) __attribute__((always_inline)) {
+        if constexpr (SPARSE) {
+            if ((u & 63) == 0) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) at4[t] = unit_at<SPARSE>(a, w, w.k0 + (u + lane) * kManyKeys + t * kUnit).place;
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) pl[t] = __builtin_amdgcn_readlane(at4[t], u & 63);
+        } else {
+            if ((u & 63) == 0) gaps = __builtin_amdgcn_readfirstlane(holes[0] | holes[1] | holes[2] | holes[3]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) pl[t] = w.k0 + u * kManyKeys + t * kUnit;
+            if (gaps != 0) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) pl[t] = __builtin_amdgcn_readfirstlane(unit_at<SPARSE>(a, w, pl[t]).place);
+            }
+        }
+    };
+
+    // Fragments in LDS: chunk D / 32 g + ks of K's row x (and 16, 32, 48 rows on), channels 16 db + 4 (x % 4) of V's row 4 g +
+    // x / 4.  ks and db change bits of the address that no other term of it has: an exclusive or instead of a register.
+    const uint32_t koff = x * D * 2 + k_slot<D>(x, D / 32 * g) * 16;
+    const uint32_t voff = T_BYTES + (4 * g + (x >> 2)) * D * 2 + v_slot<D>(4 * g + (x >> 2), (x & 3) >> 1) * 16 + (x & 1) * 8;
+    constexpr int NK = 4 * KS, NV = 2 * DB, kAhead = 4;
+    auto at = [&](int u) { return (u & 3) * STAGE; };
+    auto kfrag = [&](uint32_t t, int i) -> bf16x8 {  // i = ks * 4 + kb
+        return *(const lds_bf16x8 *)((lds_char *)smem + ((t + koff) ^ (i >> 2) * 16) + (i & 3) * 16 * D * 2);
+    };
+    auto vfrag = [&](uint32_t t, int i) -> bf16x8 {  // i = ks * DB + db
+        lds_char *p = (lds_char *)smem + ((t + voff) ^ (i % DB) * 32) + i / DB * 32 * D * 2;
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)p);
+        const bf16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 16 * D * 2));
+        return bf16x8{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
+    };
+    using T_ = std::true_type;
+    using F_ = std::false_type;
+    bf16x8 r[kAhead];
+    // the first fragments of M(u), read before the barrier that starts it
+    auto mprefetch = [&](int u, auto do_pv) __attribute__((always_inline)) {
+        constexpr int N0 = decltype(do_pv)::value ? NV : 0;
+        const uint32_t vt = at(u - 1), kt = at(u);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) r[j] = j < N0 ? vfrag(vt, j) : kfrag(kt, j - N0);
+    };
+    auto mphase = [&](int u, auto do_pv, auto do_qk) __attribute__((always_inline)) {
+        constexpr bool PV = decltype(do_pv)::value, QK = decltype(do_qk)::value;
+        constexpr int N0 = PV ? NV : 0, N = N0 + (QK ? NK : 0);
+        const uint32_t vt = at(u - 1), kt = at(u);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (j < N0) {
+                const int ks = j / DB, db = j % DB;
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb)
+                    o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[j % kAhead], pw[ks][qb], o[db][qb], 0, 0, 0);
+            } else {
+                const int ks = (j - N0) >> 2, kb = (j - N0) & 3;
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb)
+                    s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[j % kAhead], qf[qb][ks],
+                                                                       ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[kb][qb], 0,
+                                                                       0, 0);
+            }
+            if (j + kAhead < N) r[j % kAhead] = j + kAhead < N0 ? vfrag(vt, j + kAhead) : kfrag(kt, j + kAhead - N0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // weights of a tile; MASK: some row does not see some place of it
+    auto weigh = [&](const int (&pl)[4], auto mask) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(mask)::value;
+        int end[2] = {lim[0], lim[1]};
+        if constexpr (MASK) __asm__ volatile("" : "+v"(end[0]), "+v"(end[1]));  // else eight limits are kept across the loop
+        auto valid = [&](int kb, int i, int qb) { return !MASK || pl[kb] + i < end[qb]; };
+        float e_sum[2], r_sum[2];
+        auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+                const float nm = -mref[qb];
+                float a0 = -0.f, a1 = -0.f, ar = -0.f;
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        float e0 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][i], c, nm));
+                        float e1 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][i + 1], c, nm));
+                        e0 = valid(kb, i, qb) ? e0 : 0.f;
+                        e1 = valid(kb, i + 1, qb) ? e1 : 0.f;
+                        put_pair(pw[kb >> 1][qb], (kb & 1) * 4 + i, e0, e1, ar);
+                        a0 += e0;
+                        a1 += e1;
+                    }
+                e_sum[qb] = a0 + a1;
+                r_sum[qb] = ar;
+            }
+        };
+        weights();
+        if (__builtin_amdgcn_ballot_w64(!(e_sum[0] <= kSpecLimit) || !(e_sum[1] <= kSpecLimit)) != 0) {
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+                float m = -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m = fmaxf(m, valid(kb, i, qb) ? s[kb][qb][i] : -INFINITY);
+                m = quad_max(m);
+                const float mnew = fmaxf(mref[qb], m == -INFINITY ? kNone : m * c);
+                const float alpha = __builtin_amdgcn_exp2f(mref[qb] - mnew);
+                mref[qb] = mnew;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) o[db][qb] *= alpha;
+                lsum[qb] *= alpha;
+                rsum[qb] *= alpha;
+            }
+            weights();
+        }
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) lsum[qb] += e_sum[qb], rsum[qb] += r_sum[qb];
+    };
+    auto vphase = [&](int u) __attribute__((always_inline)) {
+        int pl[4];
+        places(u, pl);
+        if (max(max(pl[0], pl[1]), max(pl[2], pl[3])) + kUnit > w.least)
+            weigh(pl, T_{});
+        else
+            weigh(pl, F_{});
+    };
+    // nothing moves across a barrier between phases, scores and weights included
+    auto phase_barrier = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        __asm__ volatile("" : "+v"(s[0][0]), "+v"(s[0][1]), "+v"(s[1][0]), "+v"(s[1][1]), "+v"(s[2][0]),
+                         "+v"(s[2][1]), "+v"(s[3][0]), "+v"(s[3][1]));
+        __asm__ volatile("" : "+v"(pw[0][0]), "+v"(pw[0][1]), "+v"(pw[1][0]), "+v"(pw[1][1]));
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // what a V phase does for the ring: tile u + 3 asked for, tile u + 1 there
+    auto feed = [&](int u) __attribute__((always_inline)) {
+        load(u + 3);
+        landed();
+    };
+
+    if (T > 0) {
+        load(0);
+        load(1);
+        load(2);
+        landed();
+        __syncthreads();
+        // Pairs of phases u = 0 .. T - 1, two barriers each in both groups: group 0 runs M(u) | V(u), group 1
+        // V(u - 1) | M(u); then the last M (of weights only) of each group.
+        if (row0 >= w.rows) {
+            // A wave past the last row only brings its share of the keys, between the same barriers.
+            __syncthreads();
+            if (grp != 0) __syncthreads();
+            for (int u = 0; u < T - 1; ++u) {
+                feed(u);
+                __syncthreads();
+                __syncthreads();
+            }
+            if (grp == 0) __syncthreads();
+        } else if (grp == 0) {
+            __asm__ volatile("; group 0");
+            mprefetch(0, F_{});
+            mphase(0, F_{}, T_{});
+            phase_barrier();
+            for (int u = 0; u < T - 1; ++u) {
+                feed(u);
+                vphase(u);
+                mprefetch(u + 1, T_{});
+                phase_barrier();
+                mphase(u + 1, T_{}, T_{});
+                phase_barrier();
+            }
+            vphase(T - 1);
+            mprefetch(T, T_{});
+            phase_barrier();
+            __asm__ volatile("; last M, group 0");
+            mphase(T, T_{}, F_{});
+        } else {
+            __asm__ volatile("; group 1");
+            mprefetch(0, F_{});
+            phase_barrier();
+            mphase(0, F_{}, T_{});
+            phase_barrier();
+            for (int u = 1; u < T; ++u) {
+                feed(u - 1);
+                vphase(u - 1);
+                mprefetch(u, T_{});
+                phase_barrier();
+                mphase(u, T_{}, T_{});
+                phase_barrier();
+            }
+            vphase(T - 1);
+            mprefetch(T, T_{});
+            __asm__ volatile("; last M, group 1");
+            mphase(T, T_{}, F_{});
+        }
+    }
+    __asm__ volatile("s_waitcnt vmcnt(0)" : : : "memory");  // nothing lands in LDS after the workgroup
+    // lane indices from a fresh copy of the thread index: none stays live across the key loop
+    int tid_e = (int)threadIdx.x;
+    __asm__ volatile("" : "+v"(tid_e));
+    const int g_e = (tid_e & 63) >> 4, x_e = tid_e & 15;
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const float ll = quad_sum(lsum[qb]), rr = quad_sum(rsum[qb]);
+        const int row = row0 + qb * 16 + x_e;
+        if (row >= w.rows) continue;
+        const bool none = ll == 0.f;
+        const float inv = none ? 0.f : 1.0f / rr;
+        const float lse2 = none ? -INFINITY : mref[qb] + __builtin_amdgcn_logf(ll);
+        const int64_t at = w.row0 + row, tok = w.blk.row + at / G, h = w.hk * G + at % G;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            const f32x4 v = o[db][qb] * inv;
+            if (w.ranges == 1)
+                store_out4(a, tok, h, db * 16 + 4 * g_e, v);
+            else
+                *reinterpret_cast<f32x4 *>(part_o(a, w.range, tok, h) + db * 16 + 4 * g_e) = v;
+        }
+        if (g_e == 0) store_lse(a, p, w, tok, h, lse2);
     }
 }
 
@@ -346,11 +701,12 @@ __device__ __forceinline__ bool covered(const Batch &n, int64_t t)
     return t >= n.first[0] && t < n.first[n.B];
 }
 
-// The key ranges' partial results joined, in order.  Up to kFewRanges of them:
-// D / 4 lanes per (row, head), R >= ranges of them read at once.
+// The key ranges' partial results joined, in order, for rows with more than one.
+// `most`: the plan's ranges.  Up to kFewRanges of them: D / 4 lanes per (row, head),
+// R >= most of them read at once.
 constexpr int kFewRanges = 8;
 template <int D, int R>
-__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, int ranges)
+__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, int most)
 {
     constexpr int LPR = D / 4;
     const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
@@ -358,12 +714,15 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, int rang
     const int d = threadIdx.x % LPR * 4;
     const int64_t h = id % a.H, t = id / a.H;
     if (!covered(a.n, t)) return;
+    const int ranges = *part_ranges(a, most, t, h);
+    if (ranges <= 1) return;
     float lse[R];
     f32x4 part[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {  // past the last range that again, with no weight
-        lse[k] = *part_lse(a, ranges, min(k, ranges - 1), t, h);
-        part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, min(k, ranges - 1), t, h) + d);
+        const int at = min(k, min(ranges, most) - 1);
+        lse[k] = *part_lse(a, most, at, t, h);
+        part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, at, t, h) + d);
     }
     float m = lse[0];
 #pragma unroll
@@ -384,7 +743,7 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, int rang
 // More: a workgroup per (row, head), D / 4 lanes along the channels and 1024 /
 // D along the ranges, whose sums meet in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int ranges)
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int most)
 {
     constexpr int LPR = D / 4, SL = 256 / LPR;
     __shared__ float weight[64], total;
@@ -392,13 +751,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int ranges)
     const int i = threadIdx.x, d = i % LPR, slice = i / LPR;
     const int64_t id = blockIdx.x, h = id % a.H, t = id / a.H;
     if (!covered(a.n, t)) return;
+    const int ranges = min(*part_ranges(a, most, t, h), most);
+    if (ranges <= 1) return;
     constexpr int KEEP = 64 / SL;  // requested before the weights are known
     f32x4 part[KEEP];
 #pragma unroll
     for (int k = 0; k < KEEP; ++k)
         part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, min(k * SL + slice, ranges - 1), t, h) + d * 4);
     if (i < 64) {
-        const float e = i < ranges ? *part_lse(a, ranges, i, t, h) : -INFINITY;
+        const float e = i < ranges ? *part_lse(a, most, i, t, h) : -INFINITY;
         float m = e;
 #pragma unroll
         for (int s = 32; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
@@ -433,6 +794,7 @@ hipError_t launch_tiles(const AttnArgs &a, const AttnPlan &p, hipStream_t stream
     switch (p.tile_rows) {
     case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
     case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
+    case kManyRows: hipLaunchKernelGGL((attn_many_kernel<D, SPARSE>), grid, dim3(64 * kManyWaves), 0, stream, a, p); break;
     default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -462,15 +824,23 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
 {
     AttnPlan p{};
     const int64_t G = s.H / s.heads, queries = s.count > 0 ? std::min(s.q_block, s.max_rows) : s.max_rows;
-    p.tile_rows = queries * G <= 16 ? 16 : 32;
+    // rows of a sequence (of a block of queries) that share a key head: at most, and on the average
+    const int64_t most = queries * G, mean = s.count > 0 ? most : std::min(most, (s.T + (int64_t)s.B - 1) / s.B * G);
+    p.tile_rows = most <= 16 || mean <= 16 ? 16 : most <= 32 || mean <= 32 ? 32 : kManyRows;
     p.block = s.count > 0 ? s.q_block : (int)std::max<int64_t>(1, p.tile_rows / G);
     p.tiles = (int)((std::min(p.block, s.T) * G + p.tile_rows - 1) / p.tile_rows);
-    // As many ranges as fill the compute units with two workgroups each, of at least two rounds of a workgroup's waves.
-    const int64_t units = ((int64_t)s.T / p.block + std::min(s.B, s.T)) * p.tiles * s.heads;
-    const int64_t keys = s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len;
-    const int64_t slots = 2 * (int64_t)n_cu;
-    p.key_ranges = (int32_t)std::max<int64_t>(1, std::min({slots / std::max<int64_t>(1, units), keys / 256, (int64_t)64}));
-    p.ws_bytes = p.key_ranges > 1 ? p.key_ranges * ((int64_t)s.T * s.H * (s.D + 1)) * (int64_t)sizeof(float) : 0;
+    // Keys are cut where there are too few tiles to fill the compute units, with two workgroups of few rows or one of many
+    // each.  One sequence: into as many ranges as fill them; several, whose lengths are not known here: at what would give
+    // each slot four ranges if all were as long as the longest.
+    const bool many = p.tile_rows == kManyRows;
+    const int64_t tiles = std::min<int64_t>((int64_t)s.T / p.block + s.B, s.T) * p.tiles * s.heads;
+    const int64_t keys = std::max<int64_t>(1, s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len);
+    const int64_t slots = n_cu * (many ? 1 : 2), least = many ? 512 : 256;
+    const int64_t full = (keys * tiles + slots - 1) / slots;  // keys of a slot if all tiles had so many
+    const int64_t size = std::max(least, s.B == 1 || s.count > 0 ? (tiles > slots / 2 ? keys : full) : full / 4);
+    p.key_ranges = (int32_t)std::min<int64_t>(64, (keys + size - 1) / size);
+    p.range_units = (int32_t)((keys + p.key_ranges - 1) / p.key_ranges + kKeyAlign - 1) / kKeyAlign;
+    p.ws_bytes = p.key_ranges > 1 ? (p.key_ranges * (s.D + 1) + 1) * ((int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
     return p;
 }
 

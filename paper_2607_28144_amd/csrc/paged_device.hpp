@@ -46,15 +46,16 @@ struct Block {
 __device__ __forceinline__ Block block_of(const Batch &n, int shift, int size, int64_t j)
 {
     Block k{0, 0, 0, 0, 0};
-    const int b = last_from(n.B, j, [&](int i) { return (int64_t)(first_of(n, i) / size) + i; });
+    // the same for all lanes, which the compiler does not see in what was loaded: scalars
+    const int b = __builtin_amdgcn_readfirstlane(last_from(n.B, j, [&](int i) { return (int64_t)(first_of(n, i) / size) + i; }));
     if (b < 0) return k;
-    const int f0 = first_of(n, b), f1 = first_of(n, b + 1);
+    const int f0 = __builtin_amdgcn_readfirstlane(first_of(n, b)), f1 = __builtin_amdgcn_readfirstlane(first_of(n, b + 1));
     const int64_t at = (j - f0 / size - b) * size;
     if (at >= f1 - f0) return k;
     k.b = b;
     k.row = f0 + (int)at;
     k.rows = min(size, f1 - k.row);
-    k.len = places_of(n, b, shift);
+    k.len = __builtin_amdgcn_readfirstlane(places_of(n, b, shift));
     k.pos = k.len - (f1 - k.row);
     return k;
 }

@@ -47,9 +47,10 @@ struct AttnShape {
     int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len;  // count 0: every page
 };
 // Tiles of rows (queries times the heads that share a key head), `block` queries each and `tiles` of them to a block
-// (more than one where a query block is larger than a tile), and the ranges that the keys are cut into.
+// (more than one where a query block is larger than a tile); keys are cut into ranges of range_units times 64, key_ranges
+// of them at most.
 struct AttnPlan {
-    int32_t tile_rows, block, tiles, key_ranges;
+    int32_t tile_rows, block, tiles, key_ranges, range_units;
     int64_t ws_bytes;
 };
 AttnPlan attn_plan(const AttnShape &s, int n_cu);

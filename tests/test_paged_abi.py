@@ -206,7 +206,7 @@ def test_plans(lib):
                 assert p.tile_rows == 0 and n.value == 0
                 continue
             assert p.tile_rows % 16 == 0 and 1 <= p.key_ranges <= 64
-            assert n.value == (4 * p.key_ranges * s.T * s.H * (s.D + 1) if p.key_ranges > 1 else 0)
+            assert n.value == (4 * s.T * s.H * (p.key_ranges * (s.D + 1) + 1) if p.key_ranges > 1 else 0)
 
 
 torch = pytest.importorskip("torch")
