@@ -184,67 +184,117 @@ __device__ __forceinline__ uint64_t order_of(double s)
 }
 constexpr uint64_t kTaken = ~(uint64_t)0;
 
+// x summed over the D / 8 lanes that hold a row (each gets the result), by
+// exchanges within 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ double from_lane(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t l = __builtin_amdgcn_mov_dpp((int)u, CTRL, 0xf, 0xf, true);
+    const uint32_t h = __builtin_amdgcn_mov_dpp((int)(u >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)h << 32 | l);
+}
+template <int LPR>
+__device__ __forceinline__ double row_sum(double x)
+{
+    x += from_lane<0xb1>(x);                    // of two lanes: quad_perm 1 0 3 2
+    x += from_lane<0x4e>(x);                    // of four: 2 3 0 1
+    x += from_lane<0x141>(x);                   // of eight: the half row mirrored
+    if (LPR == 16) x += from_lane<0x140>(x);    // of sixteen: the row mirrored
+    return x;
+}
+
 // A workgroup per block of queries and key head.  The sum of the block's
 // queries and the scores are taken in 64 bits, so that the choice is that of
 // the exact scores: in 32, two pages whose scores lie within 2^-22 of one another
-// would go by the order of summation.  D / 8 lanes share a page's mean.  The
-// count-th largest score is found digit by digit from the top, eight bits a pass
-// over the scores in LDS, until a digit splits none that are left.
+// would go by the order of summation.  D / 8 lanes share a page's mean, kAtOnce
+// of them in flight: their latencies are what bounds it.  The count-th largest
+// score is found digit by digit from the top, eight bits a pass over the scores in
+// LDS, until a digit splits none that are left.
+constexpr int kSelectThreads = 512, kAtOnce = 8;
+
 template <int D>
-__global__ __launch_bounds__(256) void select_kernel(SelectArgs a)
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
 {
-    constexpr int LPR = D / 8, RPP = 256 / LPR;
+    constexpr int LPR = D / 8, RPP = kSelectThreads / LPR;
+    constexpr int WAVES = kSelectThreads / 64;
     extern __shared__ uint64_t key[];
-    __shared__ double part[RPP][D], qsum[D];
+    __shared__ double part[WAVES][D], qsum[D];
     __shared__ uint32_t hist[256];
     __shared__ uint64_t prefix_s;
     __shared__ int left_s, done_s;
+    static_assert(sizeof(part) + sizeof(qsum) + sizeof(hist) + 64 + kMaxSelectColumns * sizeof(uint64_t) <= 160 * 1024,
+                  "the scores of the largest call and the rest fit the LDS");
     const int hk = blockIdx.y, tid = threadIdx.x, G = a.H / a.c.heads;
     int32_t *out = a.selected + ((int64_t)blockIdx.x * a.c.heads + hk) * a.count;
     const Block k = block_of(a.n, a.c.shift, a.q_block, blockIdx.x);
     const int end = k.rows == 0 ? 0 : a.causal ? max(0, k.pos + k.rows) : k.len;
     const int seen = (end + (1 << a.c.shift) - 1) >> a.c.shift;  // candidates; at most the columns
     if (seen <= a.count) {
-        for (int i = tid; i < a.count; i += 256) out[i] = i < seen ? i : -1;
+        for (int i = tid; i < a.count; i += kSelectThreads) out[i] = i < seen ? i : -1;
         return;
     }
     const int d0 = tid % LPR * 8, r0 = tid / LPR;
+    const int32_t *pages = a.n.table + k.b * a.n.table_stride;
+    auto lookup = [&](int p0, int (&at)[kAtOnce]) {  // the pool's pages of this lane's candidates from p0 on, -1 for none
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int p = p0 + j * RPP + r0;
+            at[j] = pages[min(p, seen - 1)];
+            if (p >= seen || at[j] >= a.c.pages) at[j] = -1;
+        }
+    };
+    int at[kAtOnce];
+    lookup(0, at);
     {
         double s[8] = {};
-        const int64_t rows = (int64_t)k.rows * G;
-        for (int64_t r = r0; r < rows; r += RPP) {
-            const u32x4 x = load16(a.q + (k.row + r / G) * a.q_ss + (hk * G + r % G) * a.q_sh + d0);
+        const int rows = k.rows * G;  // at most H T
+        for (int r = r0; r < rows; r += RPP) {
+            const int query = r / G;
+            const u32x4 x = load16(a.q + (int64_t)(k.row + query) * a.q_ss + (int64_t)(hk * G + r - query * G) * a.q_sh + d0);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[2 * e] += (double)lo(x[e]), s[2 * e + 1] += (double)hi(x[e]);
         }
+        // over the rows that a wave has at once, then over the waves
 #pragma unroll
-        for (int e = 0; e < 8; ++e) part[r0][d0 + e] = s[e];
+        for (int e = 0; e < 8; ++e) {
+#pragma unroll
+            for (int m = LPR; m < 64; m <<= 1) s[e] += __shfl_xor(s[e], m, 64);
+            if ((tid & 63) < LPR) part[tid >> 6][d0 + e] = s[e];
+        }
     }
     __syncthreads();
     if (tid < D) {
         double sum = 0;
 #pragma unroll
-        for (int r = 0; r < RPP; ++r) sum += part[r][tid];
+        for (int r = 0; r < WAVES; ++r) sum += part[r][tid];
         qsum[tid] = sum;
     }
     __syncthreads();
     double qs[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) qs[e] = qsum[d0 + e];
-    for (int p0 = 0; p0 < seen; p0 += RPP) {
-        const int p = p0 + r0;
-        const int page = p < seen ? a.n.table[k.b * a.n.table_stride + p] : -1;
-        const bool there = page >= 0 && page < a.c.pages;
-        double s = 0;
-        if (there) {
-            const u32x4 x = load16(a.c.means + ((int64_t)page * a.c.heads + hk) * D + d0);
+    for (int p0 = 0; p0 < seen; p0 += RPP * kAtOnce) {
+        u32x4 x[kAtOnce];
+        bool there[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = fma(qs[2 * e], (double)lo(x[e]), fma(qs[2 * e + 1], (double)hi(x[e]), s));
+        for (int j = 0; j < kAtOnce; ++j) {
+            there[j] = at[j] >= 0;
+            x[j] = u32x4{0, 0, 0, 0};
+            if (there[j]) x[j] = load16(a.c.means + ((int64_t)at[j] * a.c.heads + hk) * D + d0);
         }
+        if (p0 + RPP * kAtOnce < seen) lookup(p0 + RPP * kAtOnce, at);
 #pragma unroll
-        for (int m = LPR / 2; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
-        if (p < seen && d0 == 0)
-            key[p] = p < a.keep_first || p >= seen - a.keep_last ? kTaken : there ? order_of(s) : order_of(-__builtin_inf());
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int p = p0 + j * RPP + r0;
+            if (p0 + j * RPP >= seen) break;
+            double s = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = fma(qs[2 * e], (double)lo(x[j][e]), fma(qs[2 * e + 1], (double)hi(x[j][e]), s));
+            s = row_sum<LPR>(s);
+            if (p < seen && d0 == 0)
+                key[p] = p < a.keep_first || p >= seen - a.keep_last ? kTaken : order_of(there[j] ? s : -__builtin_inf());
+        }
     }
     // digits from the top: scores with key >> shift above `prefix` are taken, `left` of those equal to it
     uint64_t prefix = 0;
@@ -252,9 +302,9 @@ __global__ __launch_bounds__(256) void select_kernel(SelectArgs a)
     bool done = false;
     while (!done && shift > 0) {
         shift -= 8;
-        hist[tid] = 0;
+        if (tid < 256) hist[tid] = 0;
         __syncthreads();
-        for (int p = tid; p < seen; p += 256) {
+        for (int p = tid; p < seen; p += kSelectThreads) {
             const uint64_t v = key[p];
             if (shift == 56 || v >> (shift + 8) == prefix) atomicAdd(&hist[(v >> shift) & 255], 1u);
         }
@@ -329,9 +379,9 @@ hipError_t launch_select(const SelectArgs &a, hipStream_t stream)
     const dim3 grid((unsigned)(a.n.T / a.q_block + a.n.B), (unsigned)a.c.heads);
     const size_t lds = a.n.columns <= a.count ? 0 : (size_t)a.n.columns * 8;
     if (a.c.D == 128)
-        hipLaunchKernelGGL(select_kernel<128>, grid, dim3(256), lds, stream, a);
+        hipLaunchKernelGGL(select_kernel<128>, grid, dim3(kSelectThreads), lds, stream, a);
     else
-        hipLaunchKernelGGL(select_kernel<64>, grid, dim3(256), lds, stream, a);
+        hipLaunchKernelGGL(select_kernel<64>, grid, dim3(kSelectThreads), lds, stream, a);
     return hipGetLastError();
 }
 

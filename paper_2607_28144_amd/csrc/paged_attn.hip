@@ -218,7 +218,7 @@ __device__ __forceinline__ int load_q(const AttnArgs &a, const Work &w, int r, i
 constexpr int kFewWaves = 4;
 
 template <int D, int MB, bool SPARSE>
-__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(MB == 1 ? 2 : 1)))
 void attn_few_kernel(AttnArgs a, AttnPlan p)
 {
     constexpr int KS = D / 32, DB = D / 16, CH = D / 8;  // CH: 16-byte chunks of a row
@@ -794,6 +794,7 @@ hipError_t launch_tiles(const AttnArgs &a, const AttnPlan &p, hipStream_t stream
     switch (p.tile_rows) {
     case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
     case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
+    case 64: hipLaunchKernelGGL((attn_few_kernel<D, 4, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
     case kManyRows: hipLaunchKernelGGL((attn_many_kernel<D, SPARSE>), grid, dim3(64 * kManyWaves), 0, stream, a, p); break;
     default: return hipErrorInvalidValue;
     }
@@ -826,18 +827,20 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     const int64_t G = s.H / s.heads, queries = s.count > 0 ? std::min(s.q_block, s.max_rows) : s.max_rows;
     // rows of a sequence (of a block of queries) that share a key head: at most, and on the average
     const int64_t most = queries * G, mean = s.count > 0 ? most : std::min(most, (s.T + (int64_t)s.B - 1) / s.B * G);
-    p.tile_rows = most <= 16 || mean <= 16 ? 16 : most <= 32 || mean <= 32 ? 32 : kManyRows;
+    p.tile_rows = most <= 16 || mean <= 16 ? 16 : most <= 32 || mean <= 32 ? 32 : most <= 64 || mean <= 64 ? 64 : kManyRows;
     p.block = s.count > 0 ? s.q_block : (int)std::max<int64_t>(1, p.tile_rows / G);
     p.tiles = (int)((std::min(p.block, s.T) * G + p.tile_rows - 1) / p.tile_rows);
     // Keys are cut where there are too few tiles to fill the compute units, with two workgroups of few rows or one of many
     // each.  One sequence: into as many ranges as fill them; several, whose lengths are not known here: at what would give
     // each slot four ranges if all were as long as the longest.
     const bool many = p.tile_rows == kManyRows;
-    const int64_t tiles = std::min<int64_t>((int64_t)s.T / p.block + s.B, s.T) * p.tiles * s.heads;
+    const int64_t each = (s.T + (int64_t)s.B - 1) / s.B;  // rows of a sequence, on the average
+    const int64_t tiles = std::min<int64_t>(s.B * ((each + p.block - 1) / p.block), s.T) * p.tiles * s.heads;
     const int64_t keys = std::max<int64_t>(1, s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len);
     const int64_t slots = n_cu * (many ? 1 : 2), least = many ? 512 : 256;
     const int64_t full = (keys * tiles + slots - 1) / slots;  // keys of a slot if all tiles had so many
-    const int64_t size = std::max(least, s.B == 1 || s.count > 0 ? (tiles > slots / 2 ? keys : full) : full / 4);
+    const int64_t even = std::max<int64_t>(1, slots / tiles);
+    const int64_t size = std::max(least, s.B == 1 || s.count > 0 ? (keys + even - 1) / even : full / 4);
     p.key_ranges = (int32_t)std::min<int64_t>(64, (keys + size - 1) / size);
     p.range_units = (int32_t)((keys + p.key_ranges - 1) / p.key_ranges + kKeyAlign - 1) / kKeyAlign;
     p.ws_bytes = p.key_ranges > 1 ? (p.key_ranges * (s.D + 1) + 1) * ((int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
