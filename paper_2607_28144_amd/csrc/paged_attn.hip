@@ -419,7 +419,7 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
     if (w.rows <= 0) return;
     const int G = a.H / a.c.heads;
     const int row0 = wave * 32;  // of the tile
-    const float c = a.scale * kLog2e;
+    const float c = log2_scale(a.scale);
     const int T = (w.k1 - w.k0 + kManyKeys - 1) / kManyKeys;  // tiles of keys
 
     bf16x8 qf[2][KS];
@@ -538,12 +538,21 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
         }
         __builtin_amdgcn_s_setprio(0);
     };
-    // weights of a tile; MASK: some row does not see some place of it
-    auto weigh = [&](const int (&pl)[4], auto mask) __attribute__((always_inline)) {
-        constexpr bool MASK = decltype(mask)::value;
-        int end[2] = {lim[0], lim[1]};
-        if constexpr (MASK) __asm__ volatile("" : "+v"(end[0]), "+v"(end[1]));  // else eight limits are kept across the loop
-        auto valid = [&](int kb, int i, int qb) { return !MASK || pl[kb] + i < end[qb]; };
+    // weights of tile u
+    auto vphase = [&](int u) __attribute__((always_inline)) {
+        int pl[4];
+        places(u, pl);
+        if (max(max(pl[0], pl[1]), max(pl[2], pl[3])) + kUnit > w.least) {  // some row does not see some place of it
+            int end[2] = {lim[0], lim[1]};
+            __asm__ volatile("" : "+v"(end[0]), "+v"(end[1]));  // else eight limits are kept across the loop
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int qb = 0; qb < 2; ++qb)
+                        if (pl[kb] + i >= end[qb]) s[kb][qb][i] = -INFINITY;
+        }
         float e_sum[2], r_sum[2];
         auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -554,10 +563,8 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
                 for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                     for (int i = 0; i < 4; i += 2) {
-                        float e0 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][i], c, nm));
-                        float e1 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][i + 1], c, nm));
-                        e0 = valid(kb, i, qb) ? e0 : 0.f;
-                        e1 = valid(kb, i + 1, qb) ? e1 : 0.f;
+                        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][i], c, nm));
+                        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][i + 1], c, nm));
                         put_pair(pw[kb >> 1][qb], (kb & 1) * 4 + i, e0, e1, ar);
                         a0 += e0;
                         a1 += e1;
@@ -574,9 +581,8 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) m = fmaxf(m, valid(kb, i, qb) ? s[kb][qb][i] : -INFINITY);
-                m = quad_max(m);
-                const float mnew = fmaxf(mref[qb], m == -INFINITY ? kNone : m * c);
+                    for (int i = 0; i < 4; ++i) m = fmaxf(m, s[kb][qb][i]);
+                const float mnew = fmaxf(mref[qb], quad_max(m) * c);
                 const float alpha = __builtin_amdgcn_exp2f(mref[qb] - mnew);
                 mref[qb] = mnew;
 #pragma unroll
@@ -588,14 +594,6 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
         }
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) lsum[qb] += e_sum[qb], rsum[qb] += r_sum[qb];
-    };
-    auto vphase = [&](int u) __attribute__((always_inline)) {
-        int pl[4];
-        places(u, pl);
-        if (max(max(pl[0], pl[1]), max(pl[2], pl[3])) + kUnit > w.least)
-            weigh(pl, T_{});
-        else
-            weigh(pl, F_{});
     };
     // nothing moves across a barrier between phases, scores and weights included
     auto phase_barrier = [&]() __attribute__((always_inline)) {
