@@ -184,8 +184,9 @@ __device__ __forceinline__ uint64_t order_of(double s)
 }
 constexpr uint64_t kTaken = ~(uint64_t)0;
 
-// x summed over the D / 8 lanes that hold a row (each gets the result), by
-// exchanges within 16 lanes.
+// Exchanges within 16 lanes, by a lane's number: its neighbour 1 and 2 off, its
+// mirror image in 8, the lane 8 off.
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kMirror8 = 0x141, kRotate8 = 0x128;
 template <int CTRL>
 __device__ __forceinline__ double from_lane(double x)
 {
@@ -194,13 +195,58 @@ __device__ __forceinline__ double from_lane(double x)
     const uint32_t h = __builtin_amdgcn_mov_dpp((int)(u >> 32), CTRL, 0xf, 0xf, true);
     return __builtin_bit_cast(double, (uint64_t)h << 32 | l);
 }
-template <int LPR>
-__device__ __forceinline__ double row_sum(double x)
+// Of 2 n sums spread over pairs of lanes, those that this lane keeps (`upper`: the last n), with its partner's part.
+template <int CTRL, int N>
+__device__ __forceinline__ void keep_half(double (&x)[N], int n, bool upper)
 {
-    x += from_lane<0xb1>(x);                    // of two lanes: quad_perm 1 0 3 2
-    x += from_lane<0x4e>(x);                    // of four: 2 3 0 1
-    x += from_lane<0x141>(x);                   // of eight: the half row mirrored
-    if (LPR == 16) x += from_lane<0x140>(x);    // of sixteen: the row mirrored
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+        if (j >= n) break;
+        const double mine = upper ? x[j + n] : x[j], other = upper ? x[j] : x[j + n];
+        x[j] = mine + from_lane<CTRL>(other);
+    }
+}
+// Eight sums spread over the D / 8 lanes that hold a row: each lane gets one of them, that of number `which`.
+template <int LPR>
+__device__ __forceinline__ double share_out(double (&x)[8], int &which)
+{
+    const int l = threadIdx.x;
+    if constexpr (LPR == 16) {
+        keep_half<kRotate8>(x, 4, l & 8);
+        keep_half<kMirror8>(x, 2, l & 4);
+        keep_half<kXor2>(x, 1, l & 2);
+        which = (l & 8 ? 4 : 0) + (l & 4 ? 2 : 0) + (l & 2 ? 1 : 0);
+        return x[0] + from_lane<kXor1>(x[0]);
+    } else {
+        keep_half<kMirror8>(x, 4, l & 4);
+        keep_half<kXor2>(x, 2, l & 2);
+        keep_half<kXor1>(x, 1, l & 1);
+        which = (l & 4 ? 4 : 0) + (l & 2 ? 2 : 0) + (l & 1 ? 1 : 0);
+        return x[0];
+    }
+}
+
+// The larger of a wave's numbers, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kXor1, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kXor2, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kMirror8, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kRotate8, 0xf, 0xf, true));
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+    const auto u = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(u[0], u[1]);
+}
+// The sum of the numbers of the lanes up to this one.
+__device__ __forceinline__ uint32_t wave_upto(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes below, within 16
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // lane 15 to the next 16, 31 to the last 32
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
     return x;
 }
 
@@ -222,8 +268,10 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
     __shared__ double part[WAVES][D], qsum[D];
     __shared__ uint32_t hist[256];
     __shared__ uint64_t prefix_s;
+    __shared__ uint32_t bound[WAVES][2];
+    __shared__ int taken_s[WAVES][2];
     __shared__ int left_s, done_s;
-    static_assert(sizeof(part) + sizeof(qsum) + sizeof(hist) + 64 + kMaxSelectColumns * sizeof(uint64_t) <= 160 * 1024,
+    static_assert(sizeof(part) + sizeof(qsum) + sizeof(hist) + sizeof(bound) + sizeof(taken_s) + 64 + kMaxSelectColumns * sizeof(uint64_t) <= 160 * 1024,
                   "the scores of the largest call and the rest fit the LDS");
     const int hk = blockIdx.y, tid = threadIdx.x, G = a.H / a.c.heads;
     int32_t *out = a.selected + ((int64_t)blockIdx.x * a.c.heads + hk) * a.count;
@@ -249,11 +297,19 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
     {
         double s[8] = {};
         const int rows = k.rows * G;  // at most H T
-        for (int r = r0; r < rows; r += RPP) {
-            const int query = r / G;
-            const u32x4 x = load16(a.q + (int64_t)(k.row + query) * a.q_ss + (int64_t)(hk * G + r - query * G) * a.q_sh + d0);
+        for (int r = r0; r < rows; r += 4 * RPP) {
+            u32x4 x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[2 * e] += (double)lo(x[e]), s[2 * e + 1] += (double)hi(x[e]);
+            for (int j = 0; j < 4; ++j) {  // past the last row that again, with no part in the sum
+                const int at = min(r + j * RPP, rows - 1), query = at / G;
+                x[j] = load16(a.q + (int64_t)(k.row + query) * a.q_ss + (int64_t)(hk * G + at - query * G) * a.q_sh + d0);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (r + j * RPP >= rows) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[2 * e] += (double)lo(x[j][e]), s[2 * e + 1] += (double)hi(x[j][e]);
+            }
         }
         // over the rows that a wave has at once, then over the waves
 #pragma unroll
@@ -274,6 +330,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
     double qs[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) qs[e] = qsum[d0 + e];
+    uint32_t low = 0, high = 0;
     for (int p0 = 0; p0 < seen; p0 += RPP * kAtOnce) {
         u32x4 x[kAtOnce];
         bool there[kAtOnce];
@@ -284,47 +341,59 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
             if (there[j]) x[j] = load16(a.c.means + ((int64_t)at[j] * a.c.heads + hk) * D + d0);
         }
         if (p0 + RPP * kAtOnce < seen) lookup(p0 + RPP * kAtOnce, at);
+        double sum[kAtOnce];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            const int p = p0 + j * RPP + r0;
-            if (p0 + j * RPP >= seen) break;
-            double s = 0;
+            sum[j] = there[j] ? 0.0 : -__builtin_inf();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s = fma(qs[2 * e], (double)lo(x[j][e]), fma(qs[2 * e + 1], (double)hi(x[j][e]), s));
-            s = row_sum<LPR>(s);
-            if (p < seen && d0 == 0)
-                key[p] = p < a.keep_first || p >= seen - a.keep_last ? kTaken : order_of(there[j] ? s : -__builtin_inf());
+            for (int e = 0; e < 4; ++e)
+                sum[j] = fma(qs[2 * e], (double)lo(x[j][e]), fma(qs[2 * e + 1], (double)hi(x[j][e]), sum[j]));
+        }
+        int j;
+        const double score = share_out<LPR>(sum, j);
+        const int p = p0 + j * RPP + r0;
+        if (p < seen) {
+            const uint64_t v = p < a.keep_first || p >= seen - a.keep_last ? kTaken : order_of(score);
+            key[p] = v;
+            // of their upper halves, the least and the most: of the pages always taken, neither
+            if (v != kTaken) low = max(low, ~(uint32_t)(v >> 32)), high = max(high, (uint32_t)(v >> 32));
         }
     }
-    // digits from the top: scores with key >> shift above `prefix` are taken, `left` of those equal to it
-    uint64_t prefix = 0;
-    int left = a.count, shift = 64;
-    bool done = false;
+    // Digits from the highest bit in which the scores' upper halves differ: those with key >> shift above `prefix` are
+    // taken, `left` of those equal to it.
+    low = wave_max(low), high = wave_max(high);
+    if ((tid & 63) == 0) bound[tid >> 6][0] = low, bound[tid >> 6][1] = high;
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) low = max(low, bound[i][0]), high = max(high, bound[i][1]);
+    low = ~low;
+    const int kept = a.keep_first + a.keep_last;  // at most count, and fewer than the candidates
+    int left = a.count - kept;
+    int shift = low == high ? 32 : 64 - __builtin_clz(low ^ high);
+    uint64_t prefix = shift >= 64 ? 0 : (uint64_t)high >> (shift - 32);
+    bool done = left == 0;  // the pages always taken are all
+    if (done) shift = 0, prefix = kTaken - 1;
     while (!done && shift > 0) {
-        shift -= 8;
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
+        const int bits = min(shift, 8);
+        shift -= bits;
         for (int p = tid; p < seen; p += kSelectThreads) {
             const uint64_t v = key[p];
-            if (shift == 56 || v >> (shift + 8) == prefix) atomicAdd(&hist[(v >> shift) & 255], 1u);
+            if (v != kTaken && (shift + bits >= 64 || v >> (shift + bits) == prefix))
+                atomicAdd(&hist[(v >> shift) & ((1u << bits) - 1)], 1u);
         }
         __syncthreads();
         if (tid < 64) {  // lane i has the digits 255 - 4 i .. 252 - 4 i
             uint32_t c[4], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c[i] = hist[255 - 4 * tid - i], sum += c[i];
-            uint32_t upto = sum;
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const uint32_t o = __shfl_up(upto, m, 64);
-                if (tid >= m) upto += o;
-            }
+            for (int i = 0; i < 4; ++i) c[i] = hist[255 - 4 * tid - i], hist[255 - 4 * tid - i] = 0, sum += c[i];
+            const uint32_t upto = wave_upto(sum);
             uint32_t above = upto - sum;
             if (above < (uint32_t)left && upto >= (uint32_t)left) {  // one lane: the digit of the last one taken is here
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (above < (uint32_t)left && above + c[i] >= (uint32_t)left) {
-                        prefix_s = prefix << 8 | (uint64_t)(255 - 4 * tid - i);
+                        prefix_s = prefix << bits | (uint64_t)(255 - 4 * tid - i);
                         left_s = left - (int)above;
                         done_s = (int)c[i] == left - (int)above;
                         break;
@@ -336,17 +405,38 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
         __syncthreads();
         prefix = prefix_s, left = left_s, done = done_s != 0;
     }
-    // in order of the pages; of equal scores the first `left`
-    if (tid >= 64) return;
+    // In order of the pages; of equal scores the first `left`.  Every wave counts those of its stretch of pages, then puts
+    // them where those before it end.
+    const int wave = tid >> 6, lane = tid & 63, stretch = ((seen + WAVES - 1) / WAVES + 63) & ~63;
+    const int first = min(seen, wave * stretch), last = min(seen, first + stretch);
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    auto look = [&](int p, bool &above, bool &equal) {
+        const uint64_t full = p < last ? key[p] : 0;
+        above = p < last && (full == kTaken || full >> shift > prefix);
+        equal = p < last && !above && full >> shift == prefix;
+    };
+    int n_above = 0, n_equal = 0;
+    for (int p = first; p < last; p += 64) {
+        bool above, equal;
+        look(p + lane, above, equal);
+        n_above += __popcll(__builtin_amdgcn_ballot_w64(above));
+        n_equal += __popcll(__builtin_amdgcn_ballot_w64(equal));
+    }
+    if (lane == 0) taken_s[wave][0] = n_above, taken_s[wave][1] = n_equal;
+    __syncthreads();
     int n = 0;
-    for (int p0 = 0; p0 < seen; p0 += 64) {
-        const int p = p0 + tid;
-        const uint64_t v = p < seen ? key[p] >> shift : 0;
-        const uint64_t eq = __builtin_amdgcn_ballot_w64(p < seen && v == prefix);
-        const uint64_t below = ((uint64_t)1 << tid) - 1;
-        const bool take = p < seen && (v > prefix || (v == prefix && __popcll(eq & below) < left));
+    for (int i = 0; i < wave; ++i) {
+        const int e = min(taken_s[i][1], left);
+        n += taken_s[i][0] + e;
+        left -= e;
+    }
+    for (int p = first; p < last; p += 64) {
+        bool above, equal;
+        look(p + lane, above, equal);
+        const uint64_t eq = __builtin_amdgcn_ballot_w64(equal);
+        const bool take = above || (equal && __popcll(eq & below) < left);
         const uint64_t taken = __builtin_amdgcn_ballot_w64(take);
-        if (take) out[n + __popcll(taken & below)] = p;
+        if (take) out[n + __popcll(taken & below)] = p + lane;
         n += __popcll(taken);
         left -= min(left, __popcll(eq));
     }

@@ -835,10 +835,18 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     const int64_t each = (s.T + (int64_t)s.B - 1) / s.B;  // rows of a sequence, on the average
     const int64_t tiles = std::min<int64_t>(s.B * ((each + p.block - 1) / p.block), s.T) * p.tiles * s.heads;
     const int64_t keys = std::max<int64_t>(1, s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len);
-    const int64_t slots = n_cu * (many ? 1 : 2), least = many ? 512 : 256;
+    const int64_t slots = n_cu * (p.tile_rows >= 64 ? 1 : 2), least = many ? 512 : 256;
     const int64_t full = (keys * tiles + slots - 1) / slots;  // keys of a slot if all tiles had so many
-    const int64_t even = std::max<int64_t>(1, slots / tiles);
-    const int64_t size = std::max(least, s.B == 1 || s.count > 0 ? (keys + even - 1) / even : full / 4);
+    int64_t ranges = std::max<int64_t>(1, slots / tiles);
+    if (s.count > 0) {
+        // all tiles have as many keys: rounds of workgroups times the keys of one and what its begin and end are worth
+        int64_t best = INT64_MAX;
+        for (int64_t r = ranges; r <= ranges + 3; ++r) {
+            const int64_t cost = (tiles * r + slots - 1) / slots * ((keys + r - 1) / r + 512);
+            if (cost < best) best = cost, ranges = r;
+        }
+    }
+    const int64_t size = std::max(least, s.B == 1 || s.count > 0 ? (keys + ranges - 1) / ranges : full / 4);
     p.key_ranges = (int32_t)std::min<int64_t>(64, (keys + size - 1) / size);
     p.range_units = (int32_t)((keys + p.key_ranges - 1) / p.key_ranges + kKeyAlign - 1) / kKeyAlign;
     p.ws_bytes = p.key_ranges > 1 ? (p.key_ranges * (s.D + 1) + 1) * ((int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
