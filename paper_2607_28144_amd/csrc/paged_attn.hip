@@ -257,7 +257,13 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
         u32x4 k[2][KS], v[NVJ];
         int place[2];
     };
-    auto load = [&](Piece &t, int i) {
+    // Tile i's rows, asked for in order.  Without a branch (there may be no such tile: zeros, and no memory is read), so that
+    // they are counted and not waited for.
+    auto load = [&](Piece &t, int i) __attribute__((always_inline)) {
+        if ((i & 31) == 0 && i > 0) {
+            now = later;
+            later = units(i + 32);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int page = __builtin_amdgcn_readlane(now.page, (i & 31) + 32 * h);
@@ -272,14 +278,9 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
         }
     };
     lds_char *vl = (lds_char *)smem + wave * V_BYTES;
-    Piece cur, nxt;
-    if (tiles > 0) load(cur, 0);
-    for (int i = 0; i < tiles; ++i) {
-        if (((i + 1) & 31) == 0) {
-            now = later;
-            later = units(i + 1 + 32);
-        }
-        if (i + 1 < tiles) load(nxt, i + 1);  // in flight beside this tile
+    // Tile i, and then its registers to tile i + 2: between them and the next one's, two tiles are in flight.
+    auto one = [&](Piece &cur, int i) __attribute__((always_inline)) {
+        const int place[2] = {cur.place[0], cur.place[1]};
 #pragma unroll
         for (int j = 0; j < NVJ; ++j) {
             const int row = lane / CH + VR * j;
@@ -296,12 +297,13 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
                     s[mb][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, cur.k[h][t]), q[mb][t],
                                                                        s[mb][h], 0, 0, 0);
             }
-        if (max(cur.place[0], cur.place[1]) + kUnit > w.least) {
+        load(cur, i + 2);
+        if (max(place[0], place[1]) + kUnit > w.least) {
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (cur.place[e >> 2] + 4 * g + (e & 3) >= lim[mb]) s[mb][e >> 2][e & 3] = -INFINITY;
+                    if (place[e >> 2] + 4 * g + (e & 3) >= lim[mb]) s[mb][e >> 2][e & 3] = -INFINITY;
         }
         bf16x8 pw[MB];
         float le[MB], re[MB];
@@ -339,7 +341,13 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) o[mb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pw[mb], o[mb][d], 0, 0, 0);
         }
-        cur = nxt;
+    };
+    Piece even, odd;
+    load(even, 0);
+    load(odd, 1);
+    for (int i = 0; i < tiles; i += 2) {  // a tile past the last one has no place: no weights
+        one(even, i);
+        one(odd, i + 1);
     }
     // the four waves' results, in a fixed order
 #pragma unroll
@@ -835,7 +843,7 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     const int64_t each = (s.T + (int64_t)s.B - 1) / s.B;  // rows of a sequence, on the average
     const int64_t tiles = std::min<int64_t>(s.B * ((each + p.block - 1) / p.block), s.T) * p.tiles * s.heads;
     const int64_t keys = std::max<int64_t>(1, s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len);
-    const int64_t slots = n_cu * (p.tile_rows >= 64 ? 1 : 2), least = many ? 512 : 256;
+    const int64_t slots = n_cu * (p.tile_rows * s.D >= 32 * 128 ? 1 : 2), least = many ? 512 : 256;
     const int64_t full = (keys * tiles + slots - 1) / slots;  // keys of a slot if all tiles had so many
     int64_t ranges = std::max<int64_t>(1, slots / tiles);
     if (s.count > 0) {
