@@ -118,9 +118,10 @@ typedef struct {
 regenvc_status regenvc_paged_attn_workspace(const regenvc_paged_attn_shape *shape, int32_t n_cu, int64_t *bytes);
 
 /* Its decomposition: rows of a workgroup's tile (queries times the H / heads
-   heads that share a key head) and the ranges that the keys are cut into. */
+   heads that share a key head), workgroups launched, and whether keys may be cut
+   into ranges (the device decides by the sequences' lengths). */
 typedef struct {
-    int32_t tile_rows, key_ranges;
+    int32_t tile_rows, workgroups, split;
 } regenvc_paged_attn_plan;
 regenvc_status regenvc_paged_attn_plan_query(const regenvc_paged_attn_shape *shape, int32_t n_cu,
                                              regenvc_paged_attn_plan *plan);

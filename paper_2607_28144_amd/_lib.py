@@ -83,7 +83,7 @@ class PagedAttnShape(ctypes.Structure):
 
 class PagedAttnPlan(ctypes.Structure):
     """regenvc_paged_attn_plan: the decomposition of attention over pages."""
-    _fields_ = [(n, ctypes.c_int32) for n in ("tile_rows", "key_ranges")]
+    _fields_ = [(n, ctypes.c_int32) for n in ("tile_rows", "workgroups", "split")]
 
 
 class Norm(ctypes.Structure):

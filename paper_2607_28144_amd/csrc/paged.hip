@@ -184,9 +184,6 @@ __device__ __forceinline__ uint64_t order_of(double s)
 }
 constexpr uint64_t kTaken = ~(uint64_t)0;
 
-// Exchanges within 16 lanes, by a lane's number: its neighbour 1 and 2 off, its
-// mirror image in 8, the lane 8 off.
-constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kMirror8 = 0x141, kRotate8 = 0x128;
 template <int CTRL>
 __device__ __forceinline__ double from_lane(double x)
 {
@@ -224,30 +221,6 @@ __device__ __forceinline__ double share_out(double (&x)[8], int &which)
         which = (l & 4 ? 4 : 0) + (l & 2 ? 2 : 0) + (l & 1 ? 1 : 0);
         return x[0];
     }
-}
-
-// The larger of a wave's numbers, in every lane.
-__device__ __forceinline__ uint32_t wave_max(uint32_t x)
-{
-    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kXor1, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kXor2, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kMirror8, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kRotate8, 0xf, 0xf, true));
-    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = max(r[0], r[1]);
-    const auto u = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return max(u[0], u[1]);
-}
-// The sum of the numbers of the lanes up to this one.
-__device__ __forceinline__ uint32_t wave_upto(uint32_t x)
-{
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes below, within 16
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // lane 15 to the next 16, 31 to the last 32
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
-    return x;
 }
 
 // A workgroup per block of queries and key head.  The sum of the block's

@@ -175,8 +175,7 @@ bool empty(const regenvc_paged_attn_shape &s)
 regenvc_status plan_of(const char *fn, const regenvc_paged_attn_shape &s, int n_cu, paged::AttnPlan *p)
 {
     *p = paged::attn_plan({s.B, s.T, s.H, s.heads, s.D, s.page, s.q_block, s.count, s.max_rows, s.max_len}, n_cu);
-    const int64_t groups = ((int64_t)s.T / p->block + s.B) * p->tiles;
-    if (groups > kMaxGroups || groups * s.heads * p->key_ranges > kMaxGroups)
+    if (p->groups > kMaxGroups || p->groups * p->tile_rows > INT32_MAX)  // rows of partial results are counted in 32 bits
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: more than %lld workgroups", fn, (long long)kMaxGroups);
     return REGENVC_OK;
 }
@@ -317,7 +316,7 @@ regenvc_status regenvc_paged_attn_plan_query(const regenvc_paged_attn_shape *sha
     if (st != REGENVC_OK) return st;
     paged::AttnPlan p{};
     if (!empty(*shape) && (st = plan_of(fn, *shape, n_cu, &p)) != REGENVC_OK) return st;
-    *plan = regenvc_paged_attn_plan{p.tile_rows, p.key_ranges};
+    *plan = regenvc_paged_attn_plan{p.tile_rows, (int32_t)p.groups, p.split};
     return done();
 }
 

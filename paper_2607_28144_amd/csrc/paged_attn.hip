@@ -37,65 +37,127 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kUnit = 16;
 constexpr int kNowhere = 0x3fffffff;  // the place of a unit that does not exist: past every limit
 constexpr int kKeyAlign = 64;         // ranges of keys begin at multiples of it
+constexpr int kMostRanges = 64;       // of a tile's keys
 
 // What a workgroup works on: `rows` rows (query, head) of a block of queries, from
 // its row `row0` on, and of their keys range `range` of `ranges`, [k0, k1) in units
 // of 16.  Key i is place i, or with selected pages place i % page of the page that
-// entry i / page names.  A tile of many keys is cut into more ranges than one of
-// few: sequences of a call differ, and the longest would be the last to end.
+// entry i / page names.
 struct Work {
     Block blk;
     int hk, row0, rows, range, ranges;
+    int part;               // first row of the workgroup's partial results
     int k0, k1;
     int see, least;         // places that its last, its first row sees
     const int32_t *pages;   // the sequence's row of the table
     const int32_t *chosen;  // of the block and key head
 };
 
+// Sequences of a call differ in length, which only the device knows, and a long
+// one would be the last to end: where there are too few tiles to even that out (the
+// plan says so), every wave goes over the sequences, 64 at a time, adds up what there
+// is to do, and finds the one that workgroup `id` has a piece of.  One sequence's
+// keys are cut into as many ranges as fill the slots once; of several, at 5/4 of what
+// a slot has on the average.  (Chunks of several lengths, 124 tiles of queries x
+// places: at the average length of all sequences by the host's bound 101 us.)
+struct Piece {
+    int b, ranges, tile, range, hk;  // tile -1: no such piece
+};
+template <bool SPARSE>
+__device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, uint32_t id)
+{
+    const int lane = threadIdx.x & 63, heads = a.c.heads;
+    int tiles = 0, keys = 0;
+    float mean = 0.f;  // keys of a row, on the average
+    auto look = [&](int c) {
+        const int b = c + lane, at = min(b, a.n.B - 1), n = max(0, first_of(a.n, at + 1) - first_of(a.n, at));
+        keys = places_of(a.n, at, a.c.shift);
+        if constexpr (SPARSE) keys = min(keys, a.count << a.c.shift);
+        mean = a.causal && !SPARSE ? max(1.f, keys - 0.5f * min(n, keys)) : (float)keys;
+        tiles = b < a.n.B ? (n + p.block - 1) / p.block * p.tiles : 0;
+    };
+    float all = 0.f;
+    for (int c = 0; c < a.n.B; c += 64) {
+        look(c);
+        all += tiles * mean;
+    }
+    all = wave_sum(all) * heads;
+    const bool one = a.n.B == 1;
+    const float size = fmaxf((float)p.least, all * (one ? 1.f : 1.25f) / p.slots);
+    Piece k{0, 1, -1, 0, 0};
+    uint32_t before = 0;
+    for (int c = 0; c < a.n.B; c += 64) {
+        if (a.n.B > 64) look(c);
+        // of one sequence, as many as there are workgroups for; of several, the mean of a row: there are enough
+        const int most = one ? (int)(p.groups / max(1, tiles * heads)) : kMostRanges;
+        const int ranges = max(1, min(min(kMostRanges, most), (int)(one ? floorf(keys / size) : ceilf(mean / size))));
+        const uint32_t mine = (uint32_t)tiles * ranges * heads, upto = before + wave_upto(mine);
+        const uint64_t done = __builtin_amdgcn_ballot_w64(upto <= id);
+        if (done != ~(uint64_t)0) {
+            const int at = __popcll(done);  // upto ascends
+            k.b = c + at;
+            k.ranges = __builtin_amdgcn_readlane(ranges, at);
+            const uint32_t rest = id - (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at);
+            const uint32_t per = (uint32_t)k.ranges * heads;
+            const uint32_t t = rest / per, r2 = rest - t * per;
+            k.tile = __builtin_amdgcn_readlane(tiles, at) - 1 - (int)t;  // the last first: in a causal call it has the most keys
+            k.range = (int)(r2 / (uint32_t)heads);
+            k.hk = (int)r2 - k.range * heads;
+            return k;
+        }
+        before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    }
+    return k;
+}
+
 template <bool SPARSE>
 __device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
 {
     Work w;
-    // range, then key head, then tile, then block, the last one first: in a causal call it has the most keys
-    const uint32_t id = gridDim.x - 1 - blockIdx.x;
-    const uint32_t heads = a.c.heads, tiles = p.tiles;
-    const uint32_t q = id / (uint32_t)p.key_ranges;
-    w.range = (int)(id - q * p.key_ranges);
-    const uint32_t q2 = q / heads;
-    w.hk = (int)(q - q2 * heads);
-    const uint32_t j = q2 / tiles;
-    w.row0 = (int)(q2 - j * tiles) * p.tile_rows;
-    w.blk = block_of(a.n, a.c.shift, p.block, j);
-    const int G = a.H / a.c.heads, all = w.blk.rows * G;
-    w.rows = min(p.tile_rows, all - w.row0);
-    w.pages = a.n.table + w.blk.b * a.n.table_stride;
-    w.chosen = nullptr;
+    const int heads = a.c.heads, G = a.H / heads;
+    int64_t j;
+    w.rows = w.range = w.part = 0;
     w.ranges = 1;
     w.k0 = w.k1 = w.see = w.least = 0;
-    if (w.rows <= 0) return w;
+    if (p.split) {
+        const Piece k = piece_of<SPARSE>(a, p, blockIdx.x);
+        if (k.tile < 0) return w;
+        const int b = __builtin_amdgcn_readfirstlane(k.b), f0 = __builtin_amdgcn_readfirstlane(first_of(a.n, b));
+        const int i = __builtin_amdgcn_readfirstlane(k.tile / p.tiles);
+        j = (int64_t)(f0 / p.block) + b + i;
+        w.blk = sequence_block(a.n, a.c.shift, b, (int64_t)i * p.block, p.block);
+        w.row0 = __builtin_amdgcn_readfirstlane((k.tile - i * p.tiles) * p.tile_rows);
+        w.hk = __builtin_amdgcn_readfirstlane(k.hk);
+        w.range = __builtin_amdgcn_readfirstlane(k.range);
+        w.ranges = __builtin_amdgcn_readfirstlane(k.ranges);
+        w.part = (int)blockIdx.x * p.tile_rows;
+    } else {
+        // key head, then tile, then block, the last block first
+        const uint32_t id = gridDim.x - 1 - blockIdx.x, q = id / (uint32_t)heads;
+        w.hk = (int)(id - q * heads);
+        j = q / (uint32_t)p.tiles;
+        w.row0 = (int)(q - j * p.tiles) * p.tile_rows;
+        w.blk = block_of(a.n, a.c.shift, p.block, j);
+    }
+    w.rows = max(0, min(p.tile_rows, w.blk.rows * G - w.row0));
+    w.pages = a.n.table + w.blk.b * a.n.table_stride;
+    w.chosen = nullptr;
+    if (w.rows == 0) return w;
     const int first = w.blk.pos + w.row0 / G, last = w.blk.pos + (w.row0 + w.rows - 1) / G;
     w.see = a.causal ? max(0, last + 1) : w.blk.len;
     w.least = a.causal ? max(0, first + 1) : w.blk.len;
     int keys = w.see;
     if constexpr (SPARSE) {
-        w.chosen = a.selected + ((int64_t)j * a.c.heads + w.hk) * a.count;
+        w.chosen = a.selected + (j * heads + w.hk) * a.count;
         // entries behind the last that is none
         int n = 0;
         for (int i = threadIdx.x & 63; i < a.count; i += 64)
             if (w.chosen[i] >= 0) n = i + 1;
-#pragma unroll
-        for (int m = 32; m >= 1; m >>= 1) n = max(n, __shfl_xor(n, m, 64));
-        keys = __builtin_amdgcn_readfirstlane(n) << a.c.shift;
+        keys = (int)__builtin_amdgcn_readfirstlane(wave_max(n)) << a.c.shift;
     }
     const uint32_t units = ((uint32_t)keys + kKeyAlign - 1) / kKeyAlign;  // < 2^24, ranges <= 64
-    const uint32_t ranges = max(1u, min((uint32_t)p.key_ranges, (units + p.range_units - 1) / p.range_units));
-    w.ranges = (int)ranges;
-    if (w.range >= w.ranges) {
-        w.rows = 0;
-        return w;
-    }
-    w.k0 = (int)(units * w.range / ranges) * kKeyAlign;
-    w.k1 = min(keys, (int)(units * (w.range + 1) / ranges) * kKeyAlign);
+    w.k0 = (int)(units * w.range / w.ranges) * kKeyAlign;
+    w.k1 = min(keys, (int)(units * (w.range + 1) / w.ranges) * kKeyAlign);
     return w;
 }
 
@@ -164,20 +226,25 @@ __device__ __forceinline__ void rows_to_lds(uint32_t dst, const uint32_t (&at)[N
 }
 #pragma clang diagnostic pop
 
-// Partial results of the key ranges in the workspace: O (f32, normalized over
-// the range) [range][row][head][D], then LSE in log2 units [range][row][head]
-// (-inf: no key), then the number of ranges [row][head] (1: the result is in place).
-__device__ __forceinline__ float *part_o(const AttnArgs &a, int64_t range, int64_t t, int64_t h)
+// Partial results of the workgroups whose tile has more than one range, in the
+// workspace: O (f32, normalized over the range) [workgroup][row of the tile][D],
+// then LSE in log2 units [workgroup][row] (-inf: no key), then for each [row of the
+// call][head] where its first range is and how many there are (1: the result is in
+// place).  Ranges of a tile are as many workgroups apart as there are key heads.
+struct Parts {
+    int first, ranges;
+};
+__device__ __forceinline__ float *part_o(const AttnArgs &a, int64_t row)
 {
-    return reinterpret_cast<float *>(a.ws) + ((range * a.n.T + t) * a.H + h) * a.c.D;
+    return reinterpret_cast<float *>(a.ws) + row * a.c.D;
 }
-__device__ __forceinline__ float *part_lse(const AttnArgs &a, int64_t ranges, int64_t range, int64_t t, int64_t h)
+__device__ __forceinline__ float *part_lse(const AttnArgs &a, const AttnPlan &p, int64_t row)
 {
-    return reinterpret_cast<float *>(a.ws) + ranges * a.n.T * a.H * a.c.D + (range * a.n.T + t) * a.H + h;
+    return reinterpret_cast<float *>(a.ws) + (int64_t)p.groups * p.tile_rows * a.c.D + row;
 }
-__device__ __forceinline__ int *part_ranges(const AttnArgs &a, int64_t ranges, int64_t t, int64_t h)
+__device__ __forceinline__ Parts *parts_of(const AttnArgs &a, const AttnPlan &p, int64_t t, int64_t h)
 {
-    return reinterpret_cast<int *>(a.ws) + ranges * a.n.T * a.H * (a.c.D + 1) + t * a.H + h;
+    return reinterpret_cast<Parts *>(a.ws + (int64_t)p.groups * p.tile_rows * (a.c.D + 1) * 4) + t * a.H + h;
 }
 __device__ __forceinline__ void store_out4(const AttnArgs &a, int64_t t, int64_t h, int d, f32x4 v)
 {
@@ -190,11 +257,13 @@ __device__ __forceinline__ void store_out4(const AttnArgs &a, int64_t t, int64_t
     }
 }
 
-__device__ __forceinline__ void store_lse(const AttnArgs &a, const AttnPlan &p, const Work &w, int64_t t, int64_t h, float lse2)
+// LSE of row `row` of the tile, token t and head h.
+__device__ __forceinline__ void store_lse(const AttnArgs &a, const AttnPlan &p, const Work &w, int row, int64_t t, int64_t h,
+                                          float lse2)
 {
-    if (p.key_ranges > 1 && w.range == 0) *part_ranges(a, p.key_ranges, t, h) = w.ranges;
+    if (p.split && w.range == 0) *parts_of(a, p, t, h) = Parts{w.part + row, w.ranges};
     if (w.ranges > 1)
-        *part_lse(a, p.key_ranges, w.range, t, h) = lse2;
+        *part_lse(a, p, w.part + row) = lse2;
     else if (a.lse != nullptr)
         a.lse[h * a.n.T + t] = lse2 * kLn2;
 }
@@ -394,8 +463,8 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
         if (w.ranges == 1)
             store_out4(a, tok, h, d4 * 4, v);
         else
-            *reinterpret_cast<f32x4 *>(part_o(a, w.range, tok, h) + d4 * 4) = v;
-        if (d4 == 0) store_lse(a, p, w, tok, h, lse2);
+            *reinterpret_cast<f32x4 *>(part_o(a, w.part + row) + d4 * 4) = v;
+        if (d4 == 0) store_lse(a, p, w, row, tok, h, lse2);
     }
 }
 
@@ -695,9 +764,9 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
             if (w.ranges == 1)
                 store_out4(a, tok, h, db * 16 + 4 * g_e, v);
             else
-                *reinterpret_cast<f32x4 *>(part_o(a, w.range, tok, h) + db * 16 + 4 * g_e) = v;
+                *reinterpret_cast<f32x4 *>(part_o(a, w.part + row) + db * 16 + 4 * g_e) = v;
         }
-        if (g_e == 0) store_lse(a, p, w, tok, h, lse2);
+        if (g_e == 0) store_lse(a, p, w, row, tok, h, lse2);
     }
 }
 
@@ -707,74 +776,87 @@ __device__ __forceinline__ bool covered(const Batch &n, int64_t t)
     return t >= n.first[0] && t < n.first[n.B];
 }
 
-// The key ranges' partial results joined, in order, for rows with more than one.
-// `most`: the plan's ranges.  Up to kFewRanges of them: D / 4 lanes per (row, head),
-// R >= most of them read at once.
-constexpr int kFewRanges = 8;
-template <int D, int R>
-__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, int most)
+constexpr int kFewRows = 2048;
+
+// A row's partial results, where there is more than one range; what lies beyond the
+// workspace is none (only of `first` that does not ascend).
+__device__ __forceinline__ bool joined(const AttnArgs &a, const AttnPlan &p, int64_t t, int64_t h, Parts &k)
+{
+    k = *parts_of(a, p, t, h);  // of a row of no sequence: anything
+    return covered(a.n, t) && k.ranges > 1 && k.ranges <= kMostRanges && k.first >= 0 &&
+           k.first + (int64_t)(k.ranges - 1) * a.c.heads * p.tile_rows < (int64_t)p.groups * p.tile_rows;
+}
+
+// The key ranges' partial results joined, in order.  Many rows: D / 4 lanes per
+// (row, head), kAtOnce ranges read at once.
+constexpr int kAtOnce = 4;
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan p)
 {
     constexpr int LPR = D / 4;
     const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
     if (id >= (int64_t)a.n.T * a.H) return;
     const int d = threadIdx.x % LPR * 4;
-    const int64_t h = id % a.H, t = id / a.H;
-    if (!covered(a.n, t)) return;
-    const int ranges = *part_ranges(a, most, t, h);
-    if (ranges <= 1) return;
-    float lse[R];
-    f32x4 part[R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) {  // past the last range that again, with no weight
-        const int at = min(k, min(ranges, most) - 1);
-        lse[k] = *part_lse(a, most, at, t, h);
-        part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, at, t, h) + d);
-    }
-    float m = lse[0];
-#pragma unroll
-    for (int k = 1; k < R; ++k) m = fmaxf(m, lse[k]);
-    m = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
+    const int64_t h = id % a.H, t = id / a.H, step = (int64_t)a.c.heads * p.tile_rows;
+    Parts k;
+    if (!joined(a, p, t, h, k)) return;
+    float m = kNone, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < k.ranges; r += kAtOnce) {
+        float lse[kAtOnce];
+        f32x4 part[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-        const float f = k < ranges ? __builtin_amdgcn_exp2f(lse[k] - m) : 0.f;
-        l += f;
-        o += part[k] * f;
+        for (int i = 0; i < kAtOnce; ++i) {  // past the last range that again, with no weight
+            const int64_t row = k.first + min(r + i, k.ranges - 1) * step;
+            lse[i] = *part_lse(a, p, row);
+            part[i] = *reinterpret_cast<const f32x4 *>(part_o(a, row) + d);
+        }
+        float mn = m;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) mn = fmaxf(mn, lse[i]);
+        const float f0 = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= f0;
+        o *= f0;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const float f = r + i < k.ranges ? __builtin_amdgcn_exp2f(lse[i] - m) : 0.f;
+            l += f;
+            o += part[i] * f;
+        }
     }
     store_out4(a, t, h, d, l == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.0f / l));
     if (d == 0 && a.lse != nullptr) a.lse[h * a.n.T + t] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// More: a workgroup per (row, head), D / 4 lanes along the channels and 1024 /
-// D along the ranges, whose sums meet in LDS.
+// Few rows, of many ranges each: a workgroup per (row, head), D / 4 lanes along the
+// channels and 1024 / D along the ranges, whose sums meet in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int most)
+__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, AttnPlan p)
 {
-    constexpr int LPR = D / 4, SL = 256 / LPR;
-    __shared__ float weight[64], total;
+    constexpr int LPR = D / 4, SL = 256 / LPR, KEEP = kMostRanges / SL;
+    __shared__ float weight[kMostRanges], total;
     __shared__ f32x4 sum[SL][LPR];
     const int i = threadIdx.x, d = i % LPR, slice = i / LPR;
-    const int64_t id = blockIdx.x, h = id % a.H, t = id / a.H;
-    if (!covered(a.n, t)) return;
-    const int ranges = min(*part_ranges(a, most, t, h), most);
-    if (ranges <= 1) return;
-    constexpr int KEEP = 64 / SL;  // requested before the weights are known
-    f32x4 part[KEEP];
+    const int64_t id = blockIdx.x, h = id % a.H, t = id / a.H, step = (int64_t)a.c.heads * p.tile_rows;
+    Parts k;
+    if (!joined(a, p, t, h, k)) return;
+    f32x4 part[KEEP];  // requested before the weights are known
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k)
-        part[k] = *reinterpret_cast<const f32x4 *>(part_o(a, min(k * SL + slice, ranges - 1), t, h) + d * 4);
+    for (int n = 0; n < KEEP; ++n) {
+        part[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (n * SL < k.ranges)
+            part[n] = *reinterpret_cast<const f32x4 *>(part_o(a, k.first + min(n * SL + slice, k.ranges - 1) * step) + d * 4);
+    }
     if (i < 64) {
-        const float e = i < ranges ? *part_lse(a, most, i, t, h) : -INFINITY;
+        const float e = i < k.ranges ? *part_lse(a, p, k.first + i * step) : -INFINITY;
         float m = e;
 #pragma unroll
         for (int s = 32; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
         m = m == -INFINITY ? 0.f : m;
         const float f = __builtin_amdgcn_exp2f(e - m);
         weight[i] = f;
-        float l = f;
-#pragma unroll
-        for (int s = 32; s >= 1; s >>= 1) l += __shfl_xor(l, s, 64);
+        const float l = wave_sum(f);
         if (i == 0) {
             total = l;
             if (a.lse != nullptr) a.lse[h * a.n.T + t] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -783,20 +865,20 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int most)
     __syncthreads();
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k)
-        if (k * SL + slice < ranges) o += part[k] * weight[k * SL + slice];
+    for (int n = 0; n < KEEP; ++n)
+        if (n * SL + slice < k.ranges) o += part[n] * weight[n * SL + slice];
     sum[slice][d] = o;
     __syncthreads();
     if (slice != 0) return;
 #pragma unroll
-    for (int k = 1; k < SL; ++k) o += sum[k][d];
+    for (int n = 1; n < SL; ++n) o += sum[n][d];
     store_out4(a, t, h, d * 4, total == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.0f / total));
 }
 
 template <int D, bool SPARSE>
 hipError_t launch_tiles(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(((int64_t)a.n.T / p.block + a.n.B) * p.tiles * a.c.heads * p.key_ranges));
+    const dim3 grid((unsigned)p.groups);
     switch (p.tile_rows) {
     case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
     case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
@@ -811,17 +893,12 @@ template <int D>
 hipError_t launch_d(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
     const hipError_t e = a.selected != nullptr ? launch_tiles<D, true>(a, p, stream) : launch_tiles<D, false>(a, p, stream);
-    if (e != hipSuccess || p.key_ranges == 1) return e;
+    if (e != hipSuccess || !p.split) return e;
     const int64_t rows = (int64_t)a.n.T * a.H;
-    const dim3 few((unsigned)((rows * (D / 4) + 255) / 256));
-    if (p.key_ranges <= 2)
-        hipLaunchKernelGGL((attn_join_few_kernel<D, 2>), few, dim3(256), 0, stream, a, p.key_ranges);
-    else if (p.key_ranges <= 4)
-        hipLaunchKernelGGL((attn_join_few_kernel<D, 4>), few, dim3(256), 0, stream, a, p.key_ranges);
-    else if (p.key_ranges <= kFewRanges)
-        hipLaunchKernelGGL((attn_join_few_kernel<D, kFewRanges>), few, dim3(256), 0, stream, a, p.key_ranges);
+    if (rows <= kFewRows)
+        hipLaunchKernelGGL((attn_join_few_kernel<D>), dim3((unsigned)rows), dim3(256), 0, stream, a, p);
     else
-        hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)rows), dim3(256), 0, stream, a, p.key_ranges);
+        hipLaunchKernelGGL((attn_join_kernel<D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, stream, a, p);
     return hipGetLastError();
 }
 
@@ -836,28 +913,18 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     p.tile_rows = most <= 16 || mean <= 16 ? 16 : most <= 32 || mean <= 32 ? 32 : most <= 64 || mean <= 64 ? 64 : kManyRows;
     p.block = s.count > 0 ? s.q_block : (int)std::max<int64_t>(1, p.tile_rows / G);
     p.tiles = (int)((std::min(p.block, s.T) * G + p.tile_rows - 1) / p.tile_rows);
-    // Keys are cut where there are too few tiles to fill the compute units, with two workgroups of few rows or one of many
-    // each.  One sequence: into as many ranges as fill them; several, whose lengths are not known here: at what would give
-    // each slot four ranges if all were as long as the longest.
-    const bool many = p.tile_rows == kManyRows;
-    const int64_t each = (s.T + (int64_t)s.B - 1) / s.B;  // rows of a sequence, on the average
-    const int64_t tiles = std::min<int64_t>(s.B * ((each + p.block - 1) / p.block), s.T) * p.tiles * s.heads;
-    const int64_t keys = std::max<int64_t>(1, s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len);
-    const int64_t slots = n_cu * (p.tile_rows * s.D >= 32 * 128 ? 1 : 2), least = many ? 512 : 256;
-    const int64_t full = (keys * tiles + slots - 1) / slots;  // keys of a slot if all tiles had so many
-    int64_t ranges = std::max<int64_t>(1, slots / tiles);
-    if (s.count > 0) {
-        // all tiles have as many keys: rounds of workgroups times the keys of one and what its begin and end are worth
-        int64_t best = INT64_MAX;
-        for (int64_t r = ranges; r <= ranges + 3; ++r) {
-            const int64_t cost = (tiles * r + slots - 1) / slots * ((keys + r - 1) / r + 512);
-            if (cost < best) best = cost, ranges = r;
-        }
-    }
-    const int64_t size = std::max(least, s.B == 1 || s.count > 0 ? (keys + ranges - 1) / ranges : full / 4);
-    p.key_ranges = (int32_t)std::min<int64_t>(64, (keys + size - 1) / size);
-    p.range_units = (int32_t)((keys + p.key_ranges - 1) / p.key_ranges + kKeyAlign - 1) / kKeyAlign;
-    p.ws_bytes = p.key_ranges > 1 ? (p.key_ranges * (s.D + 1) + 1) * ((int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
+    // workgroups that run at once: one of 64 rows or more of 128 channels to a compute unit, two smaller ones
+    p.slots = n_cu * (p.tile_rows * s.D >= 32 * 128 ? 1 : 2);
+    p.least = p.tile_rows == kManyRows ? 512 : 256;
+    const int64_t blocks = (int64_t)s.T / p.block + s.B, tiles = std::min<int64_t>(blocks, s.T) * p.tiles * s.heads;
+    const int64_t keys = s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len;
+    // Keys are cut where there are too few tiles for their number to even out the differences; a cut tile has at least two
+    // ranges of `least` keys.  Workgroups: piece_of makes at most one to a tile and one to a slot; of one sequence one to a
+    // slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
+    const int64_t rounds = s.B > 1 || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
+    p.split = tiles < (s.B > 1 ? 4 : 2) * (int64_t)p.slots && s.B <= 1024 && keys >= 2 * p.least;
+    p.groups = !p.split ? blocks * p.tiles * s.heads : s.B > 1 ? tiles + p.slots : std::max(tiles, rounds * p.slots);
+    p.ws_bytes = p.split ? (p.groups * p.tile_rows * (int64_t)(s.D + 1) + 2 * (int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
     return p;
 }
 

@@ -1,5 +1,5 @@
 // Device helpers of the kernels of a cache in pages: which sequence a piece of
-// a call belongs to.
+// a call belongs to, and sums over a wave.
 #pragma once
 #include "paged_kernels.hpp"
 
@@ -43,21 +43,58 @@ __device__ __forceinline__ int last_from(int B, int64_t j, F from)
 struct Block {
     int b, row, rows, pos, len;
 };
-__device__ __forceinline__ Block block_of(const Batch &n, int shift, int size, int64_t j)
+// The queries of sequence b from its row `at` on, `size` at most.
+__device__ __forceinline__ Block sequence_block(const Batch &n, int shift, int b, int64_t at, int size)
 {
-    Block k{0, 0, 0, 0, 0};
+    Block k{b, 0, 0, 0, 0};
     // the same for all lanes, which the compiler does not see in what was loaded: scalars
-    const int b = __builtin_amdgcn_readfirstlane(last_from(n.B, j, [&](int i) { return (int64_t)(first_of(n, i) / size) + i; }));
-    if (b < 0) return k;
     const int f0 = __builtin_amdgcn_readfirstlane(first_of(n, b)), f1 = __builtin_amdgcn_readfirstlane(first_of(n, b + 1));
-    const int64_t at = (j - f0 / size - b) * size;
     if (at >= f1 - f0) return k;
-    k.b = b;
     k.row = f0 + (int)at;
     k.rows = min(size, f1 - k.row);
     k.len = __builtin_amdgcn_readfirstlane(places_of(n, b, shift));
     k.pos = k.len - (f1 - k.row);
     return k;
+}
+__device__ __forceinline__ Block block_of(const Batch &n, int shift, int size, int64_t j)
+{
+    const int b = __builtin_amdgcn_readfirstlane(last_from(n.B, j, [&](int i) { return (int64_t)(first_of(n, i) / size) + i; }));
+    if (b < 0) return Block{0, 0, 0, 0, 0};
+    return sequence_block(n, shift, b, (j - __builtin_amdgcn_readfirstlane(first_of(n, b)) / size - b) * size, size);
+}
+
+// Exchanges within 16 lanes, by a lane's number: its neighbour 1 and 2 off, its
+// mirror image in 8, the lane 8 off.
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kMirror8 = 0x141, kRotate8 = 0x128;
+// The larger of a wave's numbers, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kXor1, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kXor2, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kMirror8, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kRotate8, 0xf, 0xf, true));
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+    const auto u = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(u[0], u[1]);
+}
+// The sum of the numbers of the lanes up to this one.
+__device__ __forceinline__ uint32_t wave_upto(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes below, within 16
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // lane 15 to the next 16, 31 to the last 32
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+// The sum of a wave's numbers, the same in every lane.
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
+    return x;
 }
 
 }  // namespace paged

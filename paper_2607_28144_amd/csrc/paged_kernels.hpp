@@ -47,11 +47,11 @@ struct AttnShape {
     int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len;  // count 0: every page
 };
 // Tiles of rows (queries times the heads that share a key head), `block` queries each and `tiles` of them to a block
-// (more than one where a query block is larger than a tile); keys are cut into ranges of range_units times 64, key_ranges
-// of them at most.
+// (more than one where a query block is larger than a tile).  split: the keys of a tile may be cut into ranges, which the
+// device decides by the sequences' lengths; `slots` workgroups run at once, a range has `least` keys or more.
 struct AttnPlan {
-    int32_t tile_rows, block, tiles, key_ranges, range_units;
-    int64_t ws_bytes;
+    int32_t tile_rows, block, tiles, split, slots, least;
+    int64_t groups, ws_bytes;
 };
 AttnPlan attn_plan(const AttnShape &s, int n_cu);
 

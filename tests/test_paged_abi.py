@@ -203,10 +203,10 @@ def test_plans(lib):
             assert lib.regenvc_paged_attn_plan_query(ref(s), n_cu, ref(p)) == 0
             assert lib.regenvc_paged_attn_workspace(ref(s), n_cu, ref(n)) == 0
             if s.B * s.T * s.H == 0:
-                assert p.tile_rows == 0 and n.value == 0
+                assert p.tile_rows == p.workgroups == p.split == 0 and n.value == 0
                 continue
-            assert p.tile_rows % 16 == 0 and 1 <= p.key_ranges <= 64
-            assert n.value == (4 * s.T * s.H * (p.key_ranges * (s.D + 1) + 1) if p.key_ranges > 1 else 0)
+            assert p.tile_rows in (16, 32, 64, 256) and p.workgroups >= s.heads
+            assert n.value == (4 * (p.workgroups * p.tile_rows * (s.D + 1) + 2 * s.T * s.H) if p.split else 0)
 
 
 torch = pytest.importorskip("torch")
