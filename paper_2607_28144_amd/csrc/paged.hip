@@ -24,120 +24,207 @@ __device__ __forceinline__ u32x4 load16(const uint16_t *p)
 }
 
 // ---------------------------------------------------------------- append
-// HBM-bound: every channel is read once and written once.  D / 8 lanes hold a
-// head, 16 bytes each, so a wave works on 8 (D = 64) or 4 heads at once; the
-// heads of q, k and v follow one another.  The angles are a lane's own (8
-// channels of every head that it meets) and formed once per token, in 64 bits
-// before the whole turns are taken off: at place 2^20 an f32 product would be
-// off by 0.06 rad.  The halves layout pairs a lane with one rot / 16 lanes on,
-// whose raw channels come by lane exchange and are normed here again.
-constexpr int kBatchLoads = 4;  // groups of heads in flight
-
-template <int D>
-__global__ __launch_bounds__(64) void append_kernel(AppendArgs a)
+// x summed over the D / 8 lanes that hold a head (each gets the result).
+template <int LPH>
+__device__ __forceinline__ float head_sum(float x)
 {
-    constexpr int LPH = D / 8, HPW = 64 / LPH;
-    const int lane = threadIdx.x, sub = lane / LPH, d0 = lane % LPH * 8;
-    const int t = blockIdx.x, splits = gridDim.y;
-    // the sequence and place of this token
-    const int b = last_from(a.n.B, t, [&](int i) { return (int64_t)first_of(a.n, i); });
-    if (b < 0 || t >= first_of(a.n, b + 1)) return;
-    const int pos = max(0, a.n.lens[b]) - (first_of(a.n, b + 1) - t);
-    const int col = pos >> a.c.shift;
-    int page = -1;
-    if (pos >= 0 && col < a.n.columns) page = a.n.table[b * a.n.table_stride + col];
-    const bool stored = page >= 0 && page < a.c.pages;
-    const int64_t cell = (int64_t)page * a.c.heads * (D << a.c.shift) + (int64_t)(pos & ((1 << a.c.shift) - 1)) * D;
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kXor1, 0xf, 0xf, true));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kXor2, 0xf, 0xf, true));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kMirror8, 0xf, 0xf, true));
+    if (LPH == 16) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kRotate8, 0xf, 0xf, true));
+    return x;
+}
 
-    const int rot = 2 * a.pairs;
-    const bool turned = d0 < rot;
-    float cs[8], sn[8];  // of each channel's pair; the sine with the sign that its partner enters with
-    if (turned) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int d = d0 + e, i = a.interleaved ? d >> 1 : d < a.pairs ? d : d - a.pairs;
-            const float x = (float)__builtin_amdgcn_fract((double)pos * a.turns[i]);
-            const bool second = a.interleaved ? d & 1 : d >= a.pairs;
-            cs[e] = a.amplitude * __builtin_amdgcn_cosf(x);
-            sn[e] = a.amplitude * __builtin_amdgcn_sinf(x) * (second ? 1.f : -1.f);
-        }
-    }
-    const int partner = a.interleaved ? lane : d0 < a.pairs ? lane + a.pairs / 8 : lane - a.pairs / 8;  // in the same head
-    const int pd0 = partner % LPH * 8;
-    const int total = a.H + 2 * a.c.heads, groups = (total + HPW - 1) / HPW;
-    u32x4 wq = {}, wk = {}, wqp = {}, wkp = {};
-    if (a.w_q != nullptr) wq = load16(a.w_q + d0), wqp = load16(a.w_q + (turned ? pd0 : d0));
-    if (a.w_k != nullptr) wk = load16(a.w_k + d0), wkp = load16(a.w_k + (turned ? pd0 : d0));
+// HBM-bound: every channel is read once and written once.  A workgroup takes the
+// new tokens of one stretch of up to 64 places within a page; its waves take the
+// heads of q, k and v, which follow one another, 64 / (D / 8) of them at a time (16
+// bytes a lane), through all of its tokens, four in flight.  Sines and cosines of
+// the stretch are formed once, in LDS; the angles in 64 bits before the whole turns
+// are taken off: at place 2^20 an f32 product would be off by 0.06 rad.  The halves
+// layout pairs a lane with one rot / 16 lanes on, whose channels come by lane
+// exchange.
+//
+// Mean keys: where a page is no longer than a stretch, the wave that has a key head
+// has all that the page's mean takes; the tokens that were there before it reads
+// back.  Sums of bf16 values in 64 bits are exact for all but absurd spreads, so
+// the mean does not depend on how the tokens came.  It is rounded to bf16, as the
+// keys that it stands for: a score then reads 1 / (2 page) of the places' bytes.
+//
+// Stretches of sequence b are numbered from first[b] / 64 + 2 b: n tokens touch at
+// most n / 64 + 2.  Tokens before place 0 are in stretches below 0: only q is written.
+constexpr int kStretch = 6, kInFlight = 4;
 
-    for (int g0 = blockIdx.y; g0 < groups; g0 += splits * kBatchLoads) {
-        u32x4 x[kBatchLoads];
+// Rows r, r + step, ... below `rows` of a page's head added to sum.
+__device__ __forceinline__ void add_rows(double (&sum)[8], const uint16_t *k, int D, int r, int step, int rows)
+{
+    for (; r < rows; r += 8 * step) {
+        u32x4 x[8];
 #pragma unroll
-        for (int j = 0; j < kBatchLoads; ++j) {
-            const int h = (g0 + j * splits) * HPW + sub;
-            x[j] = u32x4{0, 0, 0, 0};
-            if (h < a.H)
-                x[j] = load16(a.q + t * a.q_ss + h * a.q_sh + d0);
-            else if (h < a.H + a.c.heads)
-                x[j] = load16(a.k + t * a.k_ss + (h - a.H) * a.k_sh + d0);
-            else if (h < total)
-                x[j] = load16(a.v + t * a.v_ss + (h - a.H - a.c.heads) * a.v_sh + d0);
-        }
+        for (int j = 0; j < 8; ++j) x[j] = load16(k + min(r + j * step, rows - 1) * D);
 #pragma unroll
-        for (int j = 0; j < kBatchLoads; ++j) {
-            if (g0 + j * splits >= groups) break;
-            const int h = (g0 + j * splits) * HPW + sub;
-            const bool is_q = h < a.H, is_k = !is_q && h < a.H + a.c.heads;
-            const bool norm = is_q ? a.w_q != nullptr : is_k && a.w_k != nullptr;
-            float r = 1.f;
-            {
-                float s = 0.f;
+        for (int j = 0; j < 8; ++j) {
+            if (r + j * step >= rows) break;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s = fmaf(hi(x[j][e]), hi(x[j][e]), fmaf(lo(x[j][e]), lo(x[j][e]), s));
-#pragma unroll
-                for (int m = LPH / 2; m >= 1; m >>= 1) s += __shfl_xor(s, m, 64);
-                if (norm) r = 1.0f / sqrtf(s / (float)D + a.eps);
-            }
-            u32x4 p;  // the partner's raw channels
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = (uint32_t)__shfl((int)x[j][e], partner, 64);
-            if (h >= total) continue;
-            float y[8], z[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t w = is_q ? wq[e] : wk[e], wp = is_q ? wqp[e] : wkp[e];
-                y[2 * e] = norm ? lo(x[j][e]) * r * lo(w) : lo(x[j][e]);
-                y[2 * e + 1] = norm ? hi(x[j][e]) * r * hi(w) : hi(x[j][e]);
-                z[2 * e] = norm ? lo(p[e]) * r * lo(wp) : lo(p[e]);
-                z[2 * e + 1] = norm ? hi(p[e]) * r * hi(wp) : hi(p[e]);
-            }
-            if (turned && (is_q || is_k)) {
-                float f[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = y[e] * cs[e] + (a.interleaved ? y[e ^ 1] : z[e]) * sn[e];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = f[e];
-            }
-            u32x4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = is_q || is_k ? pack(y[2 * e], y[2 * e + 1]) : x[j][e];
-            uint16_t *dst;
-            if (is_q)
-                dst = a.q_out + t * a.o_ss + h * a.o_sh;
-            else if (stored)
-                dst = (is_k ? a.c.k : a.c.v) + cell + (int64_t)(is_k ? h - a.H : h - a.H - a.c.heads) * (D << a.c.shift);
-            else
-                continue;
-            *reinterpret_cast<u32x4 *>(dst + d0) = o;
+            for (int e = 0; e < 4; ++e) sum[2 * e] += (double)lo(x[j][e]), sum[2 * e + 1] += (double)hi(x[j][e]);
         }
     }
 }
 
-// Mean keys of the pages that a call's new tokens touch, from the pages as the
-// append left them.  A workgroup per page and head; sums of bf16 values in 64
-// bits are exact for all but absurd spreads, so the mean does not depend on how
-// the tokens came.  Rounded to bf16, as the keys that it stands for: a score
-// then reads 1 / (2 page) of the places' bytes.  Pages of sequence b are numbered from
-// first[b] / page + 2 b: n tokens touch at most n / page + 2.
+template <int D>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+{
+    constexpr int LPH = D / 8, HPW = 64 / LPH, S = 1 << kStretch;
+    // cosines, and sines of both signs, times the amplitude; before them, the waves' shares of the older keys' sums
+    constexpr int TURN_BYTES = 3 * S * (D / 2) * 4, PART_BYTES = 4 * 64 * 8 * 8;
+    __shared__ __attribute__((aligned(16))) char smem[TURN_BYTES > PART_BYTES ? TURN_BYTES : PART_BYTES];
+    float (*turn)[S][D / 2] = reinterpret_cast<float (*)[S][D / 2]>(smem);
+    const int tid = threadIdx.x, lane = tid & 63, sub = lane / LPH, d0 = lane % LPH * 8;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), s = min(a.c.shift, kStretch);
+    const int b = last_from(a.n.B, blockIdx.x, [&](int i) { return (int64_t)(first_of(a.n, i) >> s) + 2 * i; });
+    if (b < 0) return;
+    const int f0 = first_of(a.n, b), rows = first_of(a.n, b + 1) - f0, len = max(0, a.n.lens[b]), start = len - rows;
+    const int64_t at = ((int64_t)(start >> s) + (int64_t)blockIdx.x - (f0 >> s) - 2 * b) << s;  // the stretch's first place
+    const int begin = (int)max((int64_t)start, at), count = (int)(min((int64_t)len, at + (1 << s)) - begin);
+    if (count <= 0) return;
+    const int row0 = f0 + (begin - start);
+    const int64_t col = at >> a.c.shift;
+    int page = -1;
+    if (at >= 0 && col < a.n.columns) page = a.n.table[b * a.n.table_stride + col];
+    const bool stored = page >= 0 && page < a.c.pages;
+    const int in_page = begin & ((1 << a.c.shift) - 1);
+    const bool mean = a.c.means != nullptr && a.c.shift <= kStretch && stored;
+    const int total = a.H + 2 * a.c.heads, keys0 = a.H, keys1 = a.H + a.c.heads;
+    const int64_t page0 = (int64_t)max(page, 0) * a.c.heads;
+    // Older keys of the page, where each wave has one group of heads only: a quarter of the rows each, of all four groups.
+    const bool together = 4 * (int)gridDim.y * HPW >= total && mean && in_page > 0;
+    double older[8] = {};
+    if (together) {
+        double (*part)[64][8] = reinterpret_cast<double (*)[64][8]>(smem);
+        for (int i = 0; i < 4; ++i) {
+            const int g = (i + 4 * (int)blockIdx.y) * HPW, h = g + sub;
+            if (g >= keys1 || g + HPW <= keys0) continue;
+            double sum[8] = {};
+            const bool is_k = h >= keys0 && h < keys1;
+            if (is_k) add_rows(sum, a.c.k + ((page0 + h - keys0) << a.c.shift) * D + d0, D, wave, 4, in_page);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[wave][lane][e] = sum[e];
+            __syncthreads();
+            if (wave == i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) older[e] = (part[0][lane][e] + part[1][lane][e]) + (part[2][lane][e] + part[3][lane][e]);
+            }
+            __syncthreads();
+        }
+    }
+    const int pairs = a.pairs, rot = 2 * pairs;
+    for (int i = tid; i < count * pairs; i += 256) {
+        const int t = i / pairs, p = i - t * pairs;
+        const float x = (float)__builtin_amdgcn_fract((double)(begin + t) * a.turns[p]);
+        const float sine = a.amplitude * __builtin_amdgcn_sinf(x);
+        turn[0][t][p] = a.amplitude * __builtin_amdgcn_cosf(x);
+        turn[1][t][p] = -sine;
+        turn[2][t][p] = sine;
+    }
+    __syncthreads();
+
+    const bool turned = d0 < rot;
+    const int partner = a.interleaved ? lane : d0 < pairs ? lane + pairs / 8 : lane - pairs / 8;  // in the same head
+    const int p0 = !turned ? 0 : a.interleaved ? d0 / 2 : d0 < pairs ? d0 : d0 - pairs;  // the first of this lane's pairs
+    const float(*cosine)[D / 2] = turn[0], (*sine)[D / 2] = turn[d0 < pairs ? 1 : 2];   // sine: of the halves layout
+    for (int g = wave + 4 * blockIdx.y; g * HPW < total; g += 4 * gridDim.y) {
+        const int h = min(g * HPW + sub, total - 1);
+        const bool live = g * HPW + sub < total;
+        const bool is_q = h < keys0, is_k = !is_q && h < keys1;
+        const int hk = is_k ? h - keys0 : h - keys1;  // of k and v
+        const uint16_t *src = d0 + (is_q ? a.q + h * a.q_sh : is_k ? a.k + hk * a.k_sh : a.v + hk * a.v_sh);
+        const int64_t ss = is_q ? a.q_ss : is_k ? a.k_ss : a.v_ss;
+        const int64_t cell = (page0 + hk) << a.c.shift;
+        uint16_t *dst = d0 + (is_q ? a.q_out + row0 * a.o_ss + h * a.o_sh : (is_k ? a.c.k : a.c.v) + (cell + in_page) * D);
+        const int64_t ds = is_q ? a.o_ss : D;
+        const bool store = live && (is_q || stored), only_v = g * HPW >= keys1;
+        const uint16_t *weight = is_q ? a.w_q : is_k ? a.w_k : nullptr;
+        const bool norm = weight != nullptr, turns = turned && (is_q || is_k), sums = mean && is_k;
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = 1.f;
+        if (norm) {
+            const u32x4 x = load16(weight + d0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[2 * e] = lo(x[e]), w[2 * e + 1] = hi(x[e]);
+        }
+        double sum[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = older[e];
+        if (sums && !together) add_rows(sum, a.c.k + cell * D + d0, D, 0, 1, in_page);
+        u32x4 next[kInFlight];
+        auto load = [&](int t0) {  // past the last token that again
+#pragma unroll
+            for (int j = 0; j < kInFlight; ++j) next[j] = load16(src + (row0 + min(t0 + j, count - 1)) * ss);
+        };
+        load(0);
+        for (int t0 = 0; t0 < count; t0 += kInFlight) {
+            u32x4 x[kInFlight];
+#pragma unroll
+            for (int j = 0; j < kInFlight; ++j) x[j] = next[j];
+            load(t0 + kInFlight);
+#pragma unroll
+            for (int j = 0; j < kInFlight; ++j) {
+                const int t = t0 + j;
+                if (t >= count) break;
+                u32x4 o = x[j];
+                if (!only_v) {
+                    float q = 0.f, y[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[2 * e] = lo(x[j][e]), y[2 * e + 1] = hi(x[j][e]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) q = fmaf(y[e], y[e], q);
+                    // the mean by a product: D is a power of two
+                    const float r = __builtin_amdgcn_rsqf(fmaf(head_sum<LPH>(q), 1.0f / D, a.eps));
+                    if (norm) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = y[e] * r * w[e];
+                    }
+                    if (rot > 0) {
+                        float f[8];
+                        if (a.interleaved) {
+#pragma unroll
+                            for (int e = 0; e < 8; e += 2) {
+                                const float c = cosine[t][p0 + e / 2];
+                                f[e] = fmaf(y[e + 1], turn[1][t][p0 + e / 2], y[e] * c);
+                                f[e + 1] = fmaf(y[e], turn[2][t][p0 + e / 2], y[e + 1] * c);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f[e] = fmaf(__shfl(y[e], partner, 64), sine[t][p0 + e], y[e] * cosine[t][p0 + e]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = turns ? f[e] : y[e];
+                    }
+                    if (is_q || is_k) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = pack(y[2 * e], y[2 * e + 1]);
+                    }
+                    if (sums) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[2 * e] += (double)lo(o[e]), sum[2 * e + 1] += (double)hi(o[e]);
+                    }
+                }
+                if (store) *reinterpret_cast<u32x4 *>(dst + t * ds) = o;
+            }
+        }
+        if (sums && live) {
+            const double n = in_page + count;
+            u32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = pack((float)(sum[2 * e] / n), (float)(sum[2 * e + 1] / n));
+            *reinterpret_cast<u32x4 *>(a.c.means + (page0 + hk) * D + d0) = o;
+        }
+    }
+}
+
+// Mean keys of longer pages, from the pages as the append left them: a workgroup
+// per page that the call's new tokens touch and head.  Pages of sequence b are
+// numbered as the stretches are.
 template <int D>
 __global__ __launch_bounds__(256) void means_kernel(AppendArgs a)
 {
@@ -419,16 +506,17 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
 
 hipError_t launch_append(const AppendArgs &a, int n_cu, hipStream_t stream)
 {
-    const int hpw = 512 / a.c.D, groups = (a.H + 2 * a.c.heads + hpw - 1) / hpw;
-    // few tokens: a token's heads over several waves
-    const int splits = std::max(1, std::min(groups, 8 * n_cu / a.n.T));
-    const dim3 grid((unsigned)a.n.T, (unsigned)splits);
+    const int hpw = 512 / a.c.D, groups = (a.H + 2 * a.c.heads + hpw - 1) / hpw, s = std::min(a.c.shift, kStretch);
+    const int64_t stretches = ((int64_t)a.n.T >> s) + 2 * (int64_t)a.n.B;
+    // the heads of a stretch over several workgroups, as far as 16 waves to a compute unit take
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((groups + 3) / 4, 4 * n_cu / std::max<int64_t>(1, stretches - a.n.B)));
+    const dim3 grid((unsigned)stretches, (unsigned)splits);
     if (a.c.D == 128)
-        hipLaunchKernelGGL(append_kernel<128>, grid, dim3(64), 0, stream, a);
+        hipLaunchKernelGGL(append_kernel<128>, grid, dim3(256), 0, stream, a);
     else
-        hipLaunchKernelGGL(append_kernel<64>, grid, dim3(64), 0, stream, a);
+        hipLaunchKernelGGL(append_kernel<64>, grid, dim3(256), 0, stream, a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.c.means == nullptr) return e;
+    if (e != hipSuccess || a.c.means == nullptr || a.c.heads == 0 || a.c.shift <= kStretch) return e;
     const dim3 pages((unsigned)((a.n.T >> a.c.shift) + 2 * a.n.B), (unsigned)a.c.heads);
     if (a.c.D == 128)
         hipLaunchKernelGGL(means_kernel<128>, pages, dim3(256), 0, stream, a);

@@ -62,19 +62,22 @@ struct Work {
 // places: at the average length of all sequences by the host's bound 101 us.)
 struct Piece {
     int b, ranges, tile, range, hk;  // tile -1: no such piece
+    int first, rows, len;            // of the sequence
 };
 template <bool SPARSE>
 __device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, uint32_t id)
 {
     const int lane = threadIdx.x & 63, heads = a.c.heads;
-    int tiles = 0, keys = 0;
+    int first = 0, rows = 0, len = 0, tiles = 0, keys = 0;
     float mean = 0.f;  // keys of a row, on the average
     auto look = [&](int c) {
-        const int b = c + lane, at = min(b, a.n.B - 1), n = max(0, first_of(a.n, at + 1) - first_of(a.n, at));
-        keys = places_of(a.n, at, a.c.shift);
+        const int b = c + lane, at = min(b, a.n.B - 1);
+        first = first_of(a.n, at);
+        rows = max(0, first_of(a.n, at + 1) - first);
+        keys = len = places_of(a.n, at, a.c.shift);
         if constexpr (SPARSE) keys = min(keys, a.count << a.c.shift);
-        mean = a.causal && !SPARSE ? max(1.f, keys - 0.5f * min(n, keys)) : (float)keys;
-        tiles = b < a.n.B ? (n + p.block - 1) / p.block * p.tiles : 0;
+        mean = a.causal && !SPARSE ? max(1.f, keys - 0.5f * min(rows, keys)) : (float)keys;
+        tiles = b < a.n.B ? (rows + p.block - 1) / p.block * p.tiles : 0;
     };
     float all = 0.f;
     for (int c = 0; c < a.n.B; c += 64) {
@@ -84,7 +87,7 @@ __device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, 
     all = wave_sum(all) * heads;
     const bool one = a.n.B == 1;
     const float size = fmaxf((float)p.least, all * (one ? 1.f : 1.25f) / p.slots);
-    Piece k{0, 1, -1, 0, 0};
+    Piece k{0, 1, -1, 0, 0, 0, 0, 0};
     uint32_t before = 0;
     for (int c = 0; c < a.n.B; c += 64) {
         if (a.n.B > 64) look(c);
@@ -103,6 +106,9 @@ __device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, 
             k.tile = __builtin_amdgcn_readlane(tiles, at) - 1 - (int)t;  // the last first: in a causal call it has the most keys
             k.range = (int)(r2 / (uint32_t)heads);
             k.hk = (int)r2 - k.range * heads;
+            k.first = __builtin_amdgcn_readlane(first, at);
+            k.rows = __builtin_amdgcn_readlane(rows, at);
+            k.len = __builtin_amdgcn_readlane(len, at);
             return k;
         }
         before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
@@ -122,10 +128,13 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
     if (p.split) {
         const Piece k = piece_of<SPARSE>(a, p, blockIdx.x);
         if (k.tile < 0) return w;
-        const int b = __builtin_amdgcn_readfirstlane(k.b), f0 = __builtin_amdgcn_readfirstlane(first_of(a.n, b));
-        const int i = __builtin_amdgcn_readfirstlane(k.tile / p.tiles);
-        j = (int64_t)(f0 / p.block) + b + i;
-        w.blk = sequence_block(a.n, a.c.shift, b, (int64_t)i * p.block, p.block);
+        const int i = __builtin_amdgcn_readfirstlane(k.tile / p.tiles), at = i * p.block;  // at < rows: the tile exists
+        w.blk.b = __builtin_amdgcn_readfirstlane(k.b);
+        w.blk.row = k.first + at;
+        w.blk.rows = min(p.block, k.rows - at);
+        w.blk.len = k.len;
+        w.blk.pos = k.len - k.rows + at;
+        j = (int64_t)(k.first / p.block) + w.blk.b + i;
         w.row0 = __builtin_amdgcn_readfirstlane((k.tile - i * p.tiles) * p.tile_rows);
         w.hk = __builtin_amdgcn_readfirstlane(k.hk);
         w.range = __builtin_amdgcn_readfirstlane(k.range);

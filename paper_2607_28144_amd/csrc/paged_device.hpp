@@ -43,24 +43,21 @@ __device__ __forceinline__ int last_from(int B, int64_t j, F from)
 struct Block {
     int b, row, rows, pos, len;
 };
-// The queries of sequence b from its row `at` on, `size` at most.
-__device__ __forceinline__ Block sequence_block(const Batch &n, int shift, int b, int64_t at, int size)
+__device__ __forceinline__ Block block_of(const Batch &n, int shift, int size, int64_t j)
 {
-    Block k{b, 0, 0, 0, 0};
+    Block k{0, 0, 0, 0, 0};
     // the same for all lanes, which the compiler does not see in what was loaded: scalars
+    const int b = __builtin_amdgcn_readfirstlane(last_from(n.B, j, [&](int i) { return (int64_t)(first_of(n, i) / size) + i; }));
+    if (b < 0) return k;
     const int f0 = __builtin_amdgcn_readfirstlane(first_of(n, b)), f1 = __builtin_amdgcn_readfirstlane(first_of(n, b + 1));
+    const int64_t at = (j - f0 / size - b) * size;
     if (at >= f1 - f0) return k;
+    k.b = b;
     k.row = f0 + (int)at;
     k.rows = min(size, f1 - k.row);
     k.len = __builtin_amdgcn_readfirstlane(places_of(n, b, shift));
     k.pos = k.len - (f1 - k.row);
     return k;
-}
-__device__ __forceinline__ Block block_of(const Batch &n, int shift, int size, int64_t j)
-{
-    const int b = __builtin_amdgcn_readfirstlane(last_from(n.B, j, [&](int i) { return (int64_t)(first_of(n, i) / size) + i; }));
-    if (b < 0) return Block{0, 0, 0, 0, 0};
-    return sequence_block(n, shift, b, (j - __builtin_amdgcn_readfirstlane(first_of(n, b)) / size - b) * size, size);
 }
 
 // Exchanges within 16 lanes, by a lane's number: its neighbour 1 and 2 off, its
