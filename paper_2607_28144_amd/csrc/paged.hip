@@ -10,6 +10,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));  // eight bf16, the first of a pair in the low half
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
@@ -36,7 +37,7 @@ __device__ __forceinline__ float head_sum(float x)
 }
 
 // HBM-bound: every channel is read once and written once.  A workgroup takes the
-// new tokens of one stretch of up to 64 places within a page; its waves take the
+// new tokens of one stretch of up to 64 places within a page; pairs of its waves take the
 // heads of q, k and v, which follow one another, 64 / (D / 8) of them at a time (16
 // bytes a lane), through all of its tokens, four in flight.  Sines and cosines of
 // the stretch are formed once, in LDS; the angles in 64 bits before the whole turns
@@ -44,8 +45,8 @@ __device__ __forceinline__ float head_sum(float x)
 // layout pairs a lane with one rot / 16 lanes on, whose channels come by lane
 // exchange.
 //
-// Mean keys: where a page is no longer than a stretch, the wave that has a key head
-// has all that the page's mean takes; the tokens that were there before it reads
+// Mean keys: where a page is no longer than a stretch, the waves that have a key head
+// have all that the page's mean takes; the tokens that were there before they read
 // back.  Sums of bf16 values in 64 bits are exact for all but absurd spreads, so
 // the mean does not depend on how the tokens came.  It is rounded to bf16, as the
 // keys that it stands for: a score then reads 1 / (2 page) of the places' bytes.
@@ -71,13 +72,14 @@ __device__ __forceinline__ void add_rows(double (&sum)[8], const uint16_t *k, in
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+__global__ __launch_bounds__(512) void append_kernel(AppendArgs a)
 {
     constexpr int LPH = D / 8, HPW = 64 / LPH, S = 1 << kStretch;
-    // cosines, and sines of both signs, times the amplitude; before them, the waves' shares of the older keys' sums
-    constexpr int TURN_BYTES = 3 * S * (D / 2) * 4, PART_BYTES = 4 * 64 * 8 * 8;
-    __shared__ __attribute__((aligned(16))) char smem[TURN_BYTES > PART_BYTES ? TURN_BYTES : PART_BYTES];
-    float (*turn)[S][D / 2] = reinterpret_cast<float (*)[S][D / 2]>(smem);
+    // A token's cosines, then its sines of both signs, times the amplitude.  The two sines are read together, by the two
+    // halves of a head: four banks apart.
+    constexpr int NEG = D / 2, POS = D + 4, ROW = 3 * D / 2 + 8;
+    __shared__ __attribute__((aligned(16))) float turn[S][ROW];
+    __shared__ double part[4][64][8];  // sums of keys, of the second wave of each pair
     const int tid = threadIdx.x, lane = tid & 63, sub = lane / LPH, d0 = lane % LPH * 8;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), s = min(a.c.shift, kStretch);
     const int b = last_from(a.n.B, blockIdx.x, [&](int i) { return (int64_t)(first_of(a.n, i) >> s) + 2 * i; });
@@ -95,43 +97,26 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
     const bool mean = a.c.means != nullptr && a.c.shift <= kStretch && stored;
     const int total = a.H + 2 * a.c.heads, keys0 = a.H, keys1 = a.H + a.c.heads;
     const int64_t page0 = (int64_t)max(page, 0) * a.c.heads;
-    // Older keys of the page, where each wave has one group of heads only: a quarter of the rows each, of all four groups.
-    const bool together = 4 * (int)gridDim.y * HPW >= total && mean && in_page > 0;
-    double older[8] = {};
-    if (together) {
-        double (*part)[64][8] = reinterpret_cast<double (*)[64][8]>(smem);
-        for (int i = 0; i < 4; ++i) {
-            const int g = (i + 4 * (int)blockIdx.y) * HPW, h = g + sub;
-            if (g >= keys1 || g + HPW <= keys0) continue;
-            double sum[8] = {};
-            const bool is_k = h >= keys0 && h < keys1;
-            if (is_k) add_rows(sum, a.c.k + ((page0 + h - keys0) << a.c.shift) * D + d0, D, wave, 4, in_page);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) part[wave][lane][e] = sum[e];
-            __syncthreads();
-            if (wave == i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) older[e] = (part[0][lane][e] + part[1][lane][e]) + (part[2][lane][e] + part[3][lane][e]);
-            }
-            __syncthreads();
-        }
-    }
     const int pairs = a.pairs, rot = 2 * pairs;
-    for (int i = tid; i < count * pairs; i += 256) {
+    for (int i = tid; i < count * pairs; i += 512) {
         const int t = i / pairs, p = i - t * pairs;
         const float x = (float)__builtin_amdgcn_fract((double)(begin + t) * a.turns[p]);
         const float sine = a.amplitude * __builtin_amdgcn_sinf(x);
-        turn[0][t][p] = a.amplitude * __builtin_amdgcn_cosf(x);
-        turn[1][t][p] = -sine;
-        turn[2][t][p] = sine;
+        turn[t][p] = a.amplitude * __builtin_amdgcn_cosf(x);
+        turn[t][NEG + p] = -sine;
+        turn[t][POS + p] = sine;
     }
     __syncthreads();
 
     const bool turned = d0 < rot;
     const int partner = a.interleaved ? lane : d0 < pairs ? lane + pairs / 8 : lane - pairs / 8;  // in the same head
     const int p0 = !turned ? 0 : a.interleaved ? d0 / 2 : d0 < pairs ? d0 : d0 - pairs;  // the first of this lane's pairs
-    const float(*cosine)[D / 2] = turn[0], (*sine)[D / 2] = turn[d0 < pairs ? 1 : 2];   // sine: of the halves layout
-    for (int g = wave + 4 * blockIdx.y; g * HPW < total; g += 4 * gridDim.y) {
+    const int sine0 = (d0 < pairs ? NEG : POS) + p0;  // in the halves layout
+    const bool whole = LPH == 16 && rot == D;         // then a lane's partner is 8 lanes on
+    // a pair of waves to a group of heads, for every other batch of tokens
+    const int pair = wave >> 1, second = wave & 1;
+    for (int g0 = 4 * blockIdx.y; g0 * HPW < total; g0 += 4 * gridDim.y) {
+        const int g = g0 + pair;
         const int h = min(g * HPW + sub, total - 1);
         const bool live = g * HPW + sub < total;
         const bool is_q = h < keys0, is_k = !is_q && h < keys1;
@@ -152,21 +137,20 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[2 * e] = lo(x[e]), w[2 * e + 1] = hi(x[e]);
         }
-        double sum[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = older[e];
-        if (sums && !together) add_rows(sum, a.c.k + cell * D + d0, D, 0, 1, in_page);
+        double sum[8] = {};
+        if (sums && live) add_rows(sum, a.c.k + cell * D + d0, D, second, 2, in_page);
         u32x4 next[kInFlight];
         auto load = [&](int t0) {  // past the last token that again
 #pragma unroll
             for (int j = 0; j < kInFlight; ++j) next[j] = load16(src + (row0 + min(t0 + j, count - 1)) * ss);
         };
-        load(0);
-        for (int t0 = 0; t0 < count; t0 += kInFlight) {
+        const int end = g * HPW < total ? count : 0;
+        if (second * kInFlight < end) load(second * kInFlight);
+        for (int t0 = second * kInFlight; t0 < end; t0 += 2 * kInFlight) {
             u32x4 x[kInFlight];
 #pragma unroll
             for (int j = 0; j < kInFlight; ++j) x[j] = next[j];
-            load(t0 + kInFlight);
+            load(t0 + 2 * kInFlight);
 #pragma unroll
             for (int j = 0; j < kInFlight; ++j) {
                 const int t = t0 + j;
@@ -187,15 +171,28 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
                     if (rot > 0) {
                         float f[8];
                         if (a.interleaved) {
+                            const f32x4 c = *(const f32x4 *)&turn[t][p0], neg = *(const f32x4 *)&turn[t][NEG + p0];
+                            const f32x4 pos = *(const f32x4 *)&turn[t][POS + p0];
 #pragma unroll
-                            for (int e = 0; e < 8; e += 2) {
-                                const float c = cosine[t][p0 + e / 2];
-                                f[e] = fmaf(y[e + 1], turn[1][t][p0 + e / 2], y[e] * c);
-                                f[e + 1] = fmaf(y[e], turn[2][t][p0 + e / 2], y[e + 1] * c);
+                            for (int e = 0; e < 4; ++e) {
+                                f[2 * e] = fmaf(y[2 * e + 1], neg[e], y[2 * e] * c[e]);
+                                f[2 * e + 1] = fmaf(y[2 * e], pos[e], y[2 * e + 1] * c[e]);
                             }
                         } else {
+                            float z[8];
+                            if (whole) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] = fmaf(__shfl(y[e], partner, 64), sine[t][p0 + e], y[e] * cosine[t][p0 + e]);
+                                for (int e = 0; e < 8; ++e) z[e] = __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(y[e]), kRotate8, 0xf, 0xf, true));
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) z[e] = __shfl(y[e], partner, 64);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const f32x4 c = *(const f32x4 *)&turn[t][p0 + 4 * i], v = *(const f32x4 *)&turn[t][sine0 + 4 * i];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) f[4 * i + e] = fmaf(z[4 * i + e], v[e], y[4 * i + e] * c[e]);
+                            }
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e) y[e] = turns ? f[e] : y[e];
@@ -212,13 +209,22 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
                 if (store) *reinterpret_cast<u32x4 *>(dst + t * ds) = o;
             }
         }
-        if (sums && live) {
+        if (!mean) continue;  // the same for all waves
+        if (second) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[pair][lane][e] = sum[e];
+        }
+        __syncthreads();
+        if (sums && live && !second) {
             const double n = in_page + count;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += part[pair][lane][e];
             u32x4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = pack((float)(sum[2 * e] / n), (float)(sum[2 * e + 1] / n));
             *reinterpret_cast<u32x4 *>(a.c.means + (page0 + hk) * D + d0) = o;
         }
+        __syncthreads();
     }
 }
 
@@ -508,13 +514,13 @@ hipError_t launch_append(const AppendArgs &a, int n_cu, hipStream_t stream)
 {
     const int hpw = 512 / a.c.D, groups = (a.H + 2 * a.c.heads + hpw - 1) / hpw, s = std::min(a.c.shift, kStretch);
     const int64_t stretches = ((int64_t)a.n.T >> s) + 2 * (int64_t)a.n.B;
-    // the heads of a stretch over several workgroups, as far as 16 waves to a compute unit take
+    // the heads of a stretch over several workgroups, as far as 32 waves to a compute unit take
     const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((groups + 3) / 4, 4 * n_cu / std::max<int64_t>(1, stretches - a.n.B)));
     const dim3 grid((unsigned)stretches, (unsigned)splits);
     if (a.c.D == 128)
-        hipLaunchKernelGGL(append_kernel<128>, grid, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(append_kernel<128>, grid, dim3(512), 0, stream, a);
     else
-        hipLaunchKernelGGL(append_kernel<64>, grid, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(append_kernel<64>, grid, dim3(512), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.c.means == nullptr || a.c.heads == 0 || a.c.shift <= kStretch) return e;
     const dim3 pages((unsigned)((a.n.T >> a.c.shift) + 2 * a.n.B), (unsigned)a.c.heads);
