@@ -72,13 +72,13 @@ __device__ __forceinline__ void add_rows(double (&sum)[8], const uint16_t *k, in
 }
 
 template <int D>
-__global__ __launch_bounds__(512) void append_kernel(AppendArgs a)
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void append_kernel(AppendArgs a)
 {
     constexpr int LPH = D / 8, HPW = 64 / LPH, S = 1 << kStretch;
     // A token's cosines, then its sines of both signs, times the amplitude.  The two sines are read together, by the two
     // halves of a head: four banks apart.
     constexpr int NEG = D / 2, POS = D + 4, ROW = 3 * D / 2 + 8;
-    __shared__ __attribute__((aligned(16))) float turn[S][ROW];
+    __shared__ f32x4 turn[S][ROW / 4];
     __shared__ double part[4][64][8];  // sums of keys, of the second wave of each pair
     const int tid = threadIdx.x, lane = tid & 63, sub = lane / LPH, d0 = lane % LPH * 8;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), s = min(a.c.shift, kStretch);
@@ -102,9 +102,10 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs a)
         const int t = i / pairs, p = i - t * pairs;
         const float x = (float)__builtin_amdgcn_fract((double)(begin + t) * a.turns[p]);
         const float sine = a.amplitude * __builtin_amdgcn_sinf(x);
-        turn[t][p] = a.amplitude * __builtin_amdgcn_cosf(x);
-        turn[t][NEG + p] = -sine;
-        turn[t][POS + p] = sine;
+        float *row = reinterpret_cast<float *>(turn[t]);
+        row[p] = a.amplitude * __builtin_amdgcn_cosf(x);
+        row[NEG + p] = -sine;
+        row[POS + p] = sine;
     }
     __syncthreads();
 
@@ -171,8 +172,7 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs a)
                     if (rot > 0) {
                         float f[8];
                         if (a.interleaved) {
-                            const f32x4 c = *(const f32x4 *)&turn[t][p0], neg = *(const f32x4 *)&turn[t][NEG + p0];
-                            const f32x4 pos = *(const f32x4 *)&turn[t][POS + p0];
+                            const f32x4 c = turn[t][p0 / 4], neg = turn[t][(NEG + p0) / 4], pos = turn[t][(POS + p0) / 4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 f[2 * e] = fmaf(y[2 * e + 1], neg[e], y[2 * e] * c[e]);
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(512) void append_kernel(AppendArgs a)
                             }
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                const f32x4 c = *(const f32x4 *)&turn[t][p0 + 4 * i], v = *(const f32x4 *)&turn[t][sine0 + 4 * i];
+                                const f32x4 c = turn[t][p0 / 4 + i], v = turn[t][sine0 / 4 + i];
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) f[4 * i + e] = fmaf(z[4 * i + e], v[e], y[4 * i + e] * c[e]);
                             }
