@@ -285,6 +285,18 @@ __device__ __forceinline__ double from_lane(double x)
     const uint32_t h = __builtin_amdgcn_mov_dpp((int)(u >> 32), CTRL, 0xf, 0xf, true);
     return __builtin_bit_cast(double, (uint64_t)h << 32 | l);
 }
+// x summed over the four rows of 16 lanes.
+__device__ __forceinline__ double rows_sum(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const auto l = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+    const auto h = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    const double y = __builtin_bit_cast(double, (uint64_t)h[0] << 32 | l[0]) + __builtin_bit_cast(double, (uint64_t)h[1] << 32 | l[1]);
+    const uint64_t v = __builtin_bit_cast(uint64_t, y);
+    const auto m = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    const auto n = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
+    return __builtin_bit_cast(double, (uint64_t)n[0] << 32 | m[0]) + __builtin_bit_cast(double, (uint64_t)n[1] << 32 | m[1]);
+}
 // Of 2 n sums spread over pairs of lanes, those that this lane keeps (`upper`: the last n), with its partner's part.
 template <int CTRL, int N>
 __device__ __forceinline__ void keep_half(double (&x)[N], int n, bool upper)
@@ -323,13 +335,13 @@ __device__ __forceinline__ double share_out(double (&x)[8], int &which)
 // of them in flight: their latencies are what bounds it.  The count-th largest
 // score is found digit by digit from the top, eight bits a pass over the scores in
 // LDS, until a digit splits none that are left.
-constexpr int kSelectThreads = 512, kAtOnce = 8;
+constexpr int kAtOnce = 8;
 
-template <int D>
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void select_kernel(SelectArgs a)
 {
-    constexpr int LPR = D / 8, RPP = kSelectThreads / LPR;
-    constexpr int WAVES = kSelectThreads / 64;
+    constexpr int LPR = D / 8, RPP = THREADS / LPR;
+    constexpr int WAVES = THREADS / 64;
     extern __shared__ uint64_t key[];
     __shared__ double part[WAVES][D], qsum[D];
     __shared__ uint32_t hist[256];
@@ -345,7 +357,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
     const int end = k.rows == 0 ? 0 : a.causal ? max(0, k.pos + k.rows) : k.len;
     const int seen = (end + (1 << a.c.shift) - 1) >> a.c.shift;  // candidates; at most the columns
     if (seen <= a.count) {
-        for (int i = tid; i < a.count; i += kSelectThreads) out[i] = i < seen ? i : -1;
+        for (int i = tid; i < a.count; i += THREADS) out[i] = i < seen ? i : -1;
         return;
     }
     const int d0 = tid % LPR * 8, r0 = tid / LPR;
@@ -359,29 +371,40 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
         }
     };
     int at[kAtOnce];
+    u32x4 x[kAtOnce];
+    bool there[kAtOnce];
+    auto load = [&](const int (&at)[kAtOnce]) {
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            there[j] = at[j] >= 0;
+            x[j] = u32x4{0, 0, 0, 0};
+            if (there[j]) x[j] = load16(a.c.means + ((int64_t)at[j] * a.c.heads + hk) * D + d0);
+        }
+    };
     lookup(0, at);
     {
         double s[8] = {};
         const int rows = k.rows * G;  // at most H T
         for (int r = r0; r < rows; r += 4 * RPP) {
-            u32x4 x[4];
+            u32x4 y[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {  // past the last row that again, with no part in the sum
-                const int at = min(r + j * RPP, rows - 1), query = at / G;
-                x[j] = load16(a.q + (int64_t)(k.row + query) * a.q_ss + (int64_t)(hk * G + at - query * G) * a.q_sh + d0);
+                const int i = min(r + j * RPP, rows - 1), query = i / G;
+                y[j] = load16(a.q + (int64_t)(k.row + query) * a.q_ss + (int64_t)(hk * G + i - query * G) * a.q_sh + d0);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (r + j * RPP >= rows) break;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[2 * e] += (double)lo(x[j][e]), s[2 * e + 1] += (double)hi(x[j][e]);
+                for (int e = 0; e < 4; ++e) s[2 * e] += (double)lo(y[j][e]), s[2 * e + 1] += (double)hi(y[j][e]);
             }
         }
+        load(at);  // in flight until the queries' sum is there
         // over the rows that a wave has at once, then over the waves
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-#pragma unroll
-            for (int m = LPR; m < 64; m <<= 1) s[e] += __shfl_xor(s[e], m, 64);
+            if (LPR == 8) s[e] += from_lane<kRotate8>(s[e]);
+            s[e] = rows_sum(s[e]);
             if ((tid & 63) < LPR) part[tid >> 6][d0 + e] = s[e];
         }
     }
@@ -398,15 +421,6 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
     for (int e = 0; e < 8; ++e) qs[e] = qsum[d0 + e];
     uint32_t low = 0, high = 0;
     for (int p0 = 0; p0 < seen; p0 += RPP * kAtOnce) {
-        u32x4 x[kAtOnce];
-        bool there[kAtOnce];
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            there[j] = at[j] >= 0;
-            x[j] = u32x4{0, 0, 0, 0};
-            if (there[j]) x[j] = load16(a.c.means + ((int64_t)at[j] * a.c.heads + hk) * D + d0);
-        }
-        if (p0 + RPP * kAtOnce < seen) lookup(p0 + RPP * kAtOnce, at);
         double sum[kAtOnce];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
@@ -414,6 +428,10 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 sum[j] = fma(qs[2 * e], (double)lo(x[j][e]), fma(qs[2 * e + 1], (double)hi(x[j][e]), sum[j]));
+        }
+        if (p0 + RPP * kAtOnce < seen) {
+            lookup(p0 + RPP * kAtOnce, at);
+            load(at);
         }
         int j;
         const double score = share_out<LPR>(sum, j);
@@ -443,7 +461,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectArgs a)
     while (!done && shift > 0) {
         const int bits = min(shift, 8);
         shift -= bits;
-        for (int p = tid; p < seen; p += kSelectThreads) {
+        for (int p = tid; p < seen; p += THREADS) {
             const uint64_t v = key[p];
             if (v != kTaken && (shift + bits >= 64 || v >> (shift + bits) == prefix))
                 atomicAdd(&hist[(v >> shift) & ((1u << bits) - 1)], 1u);
@@ -531,14 +549,20 @@ hipError_t launch_append(const AppendArgs &a, int n_cu, hipStream_t stream)
     return hipGetLastError();
 }
 
-hipError_t launch_select(const SelectArgs &a, hipStream_t stream)
+hipError_t launch_select(const SelectArgs &a, int n_cu, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.n.T / a.q_block + a.n.B), (unsigned)a.c.heads);
     const size_t lds = a.n.columns <= a.count ? 0 : (size_t)a.n.columns * 8;
-    if (a.c.D == 128)
-        hipLaunchKernelGGL(select_kernel<128>, grid, dim3(kSelectThreads), lds, stream, a);
+    // few workgroups: as many waves to each as there can be, whose latencies and 64-bit products are what it takes
+    const bool few = (int64_t)grid.x * grid.y <= n_cu;
+    if (a.c.D == 128 && few)
+        hipLaunchKernelGGL((select_kernel<128, 1024>), grid, dim3(1024), lds, stream, a);
+    else if (a.c.D == 128)
+        hipLaunchKernelGGL((select_kernel<128, 256>), grid, dim3(256), lds, stream, a);
+    else if (few)
+        hipLaunchKernelGGL((select_kernel<64, 1024>), grid, dim3(1024), lds, stream, a);
     else
-        hipLaunchKernelGGL(select_kernel<64>, grid, dim3(kSelectThreads), lds, stream, a);
+        hipLaunchKernelGGL((select_kernel<64, 256>), grid, dim3(256), lds, stream, a);
     return hipGetLastError();
 }
 

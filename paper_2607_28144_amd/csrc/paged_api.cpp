@@ -290,7 +290,8 @@ regenvc_status regenvc_paged_select(const regenvc_tensor *q, const regenvc_page_
     if ((st = regenvc::abi::device_ok()) != REGENVC_OK) return st;
     const paged::SelectArgs a{pool_of(*pool), batch_of(*batch), u16(q->ptr), q->stride_s, q->stride_h, selected, H,
                               q_block,        count,            keep_first,  keep_last,   causal != 0};
-    return regenvc::abi::launch_status(paged::launch_select(a, static_cast<hipStream_t>(stream)), fn);
+    return regenvc::abi::launch_status(paged::launch_select(a, regenvc::device_cu_count(), static_cast<hipStream_t>(stream)),
+                                       fn);
 }
 
 regenvc_status regenvc_paged_attn_workspace(const regenvc_paged_attn_shape *shape, int32_t n_cu, int64_t *bytes)

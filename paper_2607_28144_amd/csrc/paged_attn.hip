@@ -128,13 +128,13 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
     if (p.split) {
         const Piece k = piece_of<SPARSE>(a, p, blockIdx.x);
         if (k.tile < 0) return w;
-        const int i = __builtin_amdgcn_readfirstlane(k.tile / p.tiles), at = i * p.block;  // at < rows: the tile exists
+        const int i = p.tiles == 1 ? k.tile : __builtin_amdgcn_readfirstlane(k.tile / p.tiles), at = i * p.block;  // at < rows: the tile exists
         w.blk.b = __builtin_amdgcn_readfirstlane(k.b);
         w.blk.row = k.first + at;
         w.blk.rows = min(p.block, k.rows - at);
         w.blk.len = k.len;
         w.blk.pos = k.len - k.rows + at;
-        j = (int64_t)(k.first / p.block) + w.blk.b + i;
+        j = !SPARSE ? 0 : (p.block == 1 ? k.first : (int64_t)(k.first / p.block)) + w.blk.b + i;
         w.row0 = __builtin_amdgcn_readfirstlane((k.tile - i * p.tiles) * p.tile_rows);
         w.hk = __builtin_amdgcn_readfirstlane(k.hk);
         w.range = __builtin_amdgcn_readfirstlane(k.range);
@@ -152,22 +152,29 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, const AttnPlan &p)
     w.pages = a.n.table + w.blk.b * a.n.table_stride;
     w.chosen = nullptr;
     if (w.rows == 0) return w;
-    const int first = w.blk.pos + w.row0 / G, last = w.blk.pos + (w.row0 + w.rows - 1) / G;
+    const int first = w.blk.pos + (w.row0 == 0 ? 0 : w.row0 / G), last = w.blk.pos + (w.row0 + w.rows - 1) / G;
     w.see = a.causal ? max(0, last + 1) : w.blk.len;
     w.least = a.causal ? max(0, first + 1) : w.blk.len;
     int keys = w.see;
     if constexpr (SPARSE) {
         w.chosen = a.selected + (j * heads + w.hk) * a.count;
-        // entries behind the last that is none
-        int n = 0;
-        for (int i = threadIdx.x & 63; i < a.count; i += 64)
-            if (w.chosen[i] >= 0) n = i + 1;
-        keys = (int)__builtin_amdgcn_readfirstlane(wave_max(n)) << a.c.shift;
+        keys = a.count << a.c.shift;
     }
     const uint32_t units = ((uint32_t)keys + kKeyAlign - 1) / kKeyAlign;  // < 2^24, ranges <= 64
-    w.k0 = (int)(units * w.range / w.ranges) * kKeyAlign;
-    w.k1 = min(keys, (int)(units * (w.range + 1) / w.ranges) * kKeyAlign);
+    w.k0 = w.ranges == 1 ? 0 : (int)(units * w.range / w.ranges) * kKeyAlign;
+    w.k1 = w.ranges == 1 ? keys : min(keys, (int)(units * (w.range + 1) / w.ranges) * kKeyAlign);
     return w;
+}
+// Where the keys end: with selected pages, behind the list's last entry that is not none.  Apart from work_of, so that the
+// list is read beside what else a workgroup begins with.
+template <bool SPARSE>
+__device__ __forceinline__ int end_of(const AttnArgs &a, const Work &w)
+{
+    if constexpr (!SPARSE) return w.k1;
+    int n = 0;
+    for (int i = threadIdx.x & 63; i < a.count; i += 64)
+        if (w.chosen[i] >= 0) n = i + 1;
+    return min(w.k1, (int)__builtin_amdgcn_readfirstlane(wave_max(n)) << a.c.shift);
 }
 
 // Where the unit from key i on lies: its page in the pool (-1: nowhere) and its first place.
@@ -293,12 +300,16 @@ __device__ __forceinline__ int load_q(const AttnArgs &a, const Work &w, int r, i
 // own, 32 keys at a time, with nothing shared: K goes from memory to registers
 // and the matrix unit; V through 2 D x 32 bytes of wave-private LDS, for the
 // transposition.  The waves' results meet in LDS.
-constexpr int kFewWaves = 4;
+//
+// 16 rows: eight waves, so that few places need no second launch to join ranges
+// (1024 keys are four rounds); more rows take the registers of two waves each.
+constexpr int few_waves(int rows) { return rows == 16 ? 8 : 4; }
 
 template <int D, int MB, bool SPARSE>
-__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(MB == 1 ? 2 : 1)))
+__global__ __launch_bounds__(64 * few_waves(16 * MB)) __attribute__((amdgpu_waves_per_eu(MB == 1 ? 2 : 1)))
 void attn_few_kernel(AttnArgs a, AttnPlan p)
 {
+    constexpr int kFewWaves = few_waves(16 * MB);
     constexpr int KS = D / 32, DB = D / 16, CH = D / 8;  // CH: 16-byte chunks of a row
     constexpr int VR = 64 / CH, NVJ = 32 / VR;           // rows of V that a load of the wave takes, and the loads
     constexpr int V_BYTES = 32 * D * 2;
@@ -328,9 +339,9 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
     // Units of this wave's tiles i = 0, 1, ... (keys key_of(i) .. + 31), two each: lane 32 h + i % 32 holds half h of tile
     // i of 32, and those of the 32 tiles after them.
     const int step = 32 * kFewWaves, begin = w.k0 + 32 * wave;
-    const int tiles = max(0, (w.k1 - begin + step - 1) / step);
     auto units = [&](int i0) { return unit_at<SPARSE>(a, w, begin + (i0 + (lane & 31)) * step + (lane >> 5) * kUnit); };
     Unit now = units(0), later = units(32);
+    const int tiles = max(0, (end_of<SPARSE>(a, w) - begin + step - 1) / step);
     struct Piece {
         u32x4 k[2][KS], v[NVJ];
         int place[2];
@@ -423,11 +434,12 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
     Piece even, odd;
     load(even, 0);
     load(odd, 1);
-    for (int i = 0; i < tiles; i += 2) {  // a tile past the last one has no place: no weights
+    for (int i = 0; i < tiles; i += 2) {
         one(even, i);
+        if (i + 1 >= tiles) break;
         one(odd, i + 1);
     }
-    // the four waves' results, in a fixed order
+    // the waves' results, in a fixed order
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         l[mb] = quad_sum(l[mb]);
@@ -443,6 +455,7 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
 #pragma unroll
         for (int t = 1; t < kFewWaves; ++t) mm = fmaxf(mm, stat[t][0][row]);
         const float f = __builtin_amdgcn_exp2f(m[mb] - mm);
+        if (row >= w.rows) continue;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
             *reinterpret_cast<f32x4 *>(sum + row * D + (((d * 4 + g) ^ (x & 7)) * 4)) = o[mb][d] * f;
@@ -506,7 +519,6 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
     const int G = a.H / a.c.heads;
     const int row0 = wave * 32;  // of the tile
     const float c = log2_scale(a.scale);
-    const int T = (w.k1 - w.k0 + kManyKeys - 1) / kManyKeys;  // tiles of keys
 
     bf16x8 qf[2][KS];
     int lim[2];  // places that this lane's rows see, less its first key of a unit
@@ -530,6 +542,7 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
         return __builtin_amdgcn_ballot_w64(x.page < 0 && w.k0 + (u0 + lane) * kManyKeys + mine < w.k1) != 0;
     };
     if (!SPARSE) holes[wave] = hole(now, 0) || hole(later, 64);
+    const int T = max(0, (end_of<SPARSE>(a, w) - w.k0 + kManyKeys - 1) / kManyKeys);  // tiles of keys
     // Where a load of the wave finds what its lanes' places in LDS hold: chunks change places with the row (v_slot, k_slot).
     uint32_t vofs[NL];
 #pragma unroll
@@ -889,9 +902,9 @@ hipError_t launch_tiles(const AttnArgs &a, const AttnPlan &p, hipStream_t stream
 {
     const dim3 grid((unsigned)p.groups);
     switch (p.tile_rows) {
-    case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
-    case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
-    case 64: hipLaunchKernelGGL((attn_few_kernel<D, 4, SPARSE>), grid, dim3(64 * kFewWaves), 0, stream, a, p); break;
+    case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, dim3(64 * few_waves(16)), 0, stream, a, p); break;
+    case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, dim3(64 * few_waves(32)), 0, stream, a, p); break;
+    case 64: hipLaunchKernelGGL((attn_few_kernel<D, 4, SPARSE>), grid, dim3(64 * few_waves(64)), 0, stream, a, p); break;
     case kManyRows: hipLaunchKernelGGL((attn_many_kernel<D, SPARSE>), grid, dim3(64 * kManyWaves), 0, stream, a, p); break;
     default: return hipErrorInvalidValue;
     }
@@ -922,8 +935,8 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     p.tile_rows = most <= 16 || mean <= 16 ? 16 : most <= 32 || mean <= 32 ? 32 : most <= 64 || mean <= 64 ? 64 : kManyRows;
     p.block = s.count > 0 ? s.q_block : (int)std::max<int64_t>(1, p.tile_rows / G);
     p.tiles = (int)((std::min(p.block, s.T) * G + p.tile_rows - 1) / p.tile_rows);
-    // workgroups that run at once: one of 64 rows or more of 128 channels to a compute unit, two smaller ones
-    p.slots = n_cu * (p.tile_rows * s.D >= 32 * 128 ? 1 : 2);
+    // workgroups that run at once: two of 32 rows of 64 channels to a compute unit, or one of any other
+    p.slots = n_cu * (p.tile_rows == 32 && s.D == 64 ? 2 : 1);
     p.least = p.tile_rows == kManyRows ? 512 : 256;
     const int64_t blocks = (int64_t)s.T / p.block + s.B, tiles = std::min<int64_t>(blocks, s.T) * p.tiles * s.heads;
     const int64_t keys = s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len;
@@ -931,7 +944,7 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     // ranges of `least` keys.  Workgroups: piece_of makes at most one to a tile and one to a slot; of one sequence one to a
     // slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
     const int64_t rounds = s.B > 1 || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
-    p.split = tiles < (s.B > 1 ? 4 : 2) * (int64_t)p.slots && s.B <= 1024 && keys >= 2 * p.least;
+    p.split = tiles < (s.B > 1 ? 4 : 2) * (int64_t)p.slots && s.B <= 1024 && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
     p.groups = !p.split ? blocks * p.tiles * s.heads : s.B > 1 ? tiles + p.slots : std::max(tiles, rounds * p.slots);
     p.ws_bytes = p.split ? (p.groups * p.tile_rows * (int64_t)(s.D + 1) + 2 * (int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
     return p;

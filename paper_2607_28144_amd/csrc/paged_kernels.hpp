@@ -41,7 +41,7 @@ struct SelectArgs {
     int32_t H, q_block, count, keep_first, keep_last, causal;
 };
 constexpr int kMaxSelectColumns = 16384;  // a score of 64 bits each, in LDS
-hipError_t launch_select(const SelectArgs &a, hipStream_t stream);
+hipError_t launch_select(const SelectArgs &a, int n_cu, hipStream_t stream);
 
 struct AttnShape {
     int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len;  // count 0: every page
