@@ -296,6 +296,73 @@ __device__ __forceinline__ int load_q(const AttnArgs &a, const Work &w, int r, i
     return a.causal ? max(0, w.blk.pos + query + 1) : w.blk.len;
 }
 
+__device__ __forceinline__ bool finite4(f32x4 v)
+{
+    return fmaf(v[3], 0.f, fmaf(v[2], 0.f, fmaf(v[1], 0.f, v[0] * 0.f))) == 0.f;
+}
+
+// Row `row` of the tile by one wave, a key to a lane, with only the places that it
+// sees.  The matrix products of a causal tile take a weight of 0 times the values of
+// places that some of its rows do not see: where those hold an infinity or NaN,
+// the product is NaN, and the row is done again here.  (So is a row that is not
+// finite by what it sees: the same comes out.)  Slow, and off every path of finite values.
+template <int D, bool SPARSE>
+__device__ __forceinline__ void redo_row(const AttnArgs &a, const AttnPlan &p, const Work &w, int row)
+{
+    constexpr int PER = D / 64;
+    const int lane = threadIdx.x & 63, G = a.H / a.c.heads;
+    const int at = w.row0 + row, query = at / G;
+    const int64_t tok = w.blk.row + query, h = w.hk * G + at - query * G;
+    const int lim = max(0, w.blk.pos + query + 1);  // causal
+    const uint16_t *q = a.q + tok * a.q_ss + h * a.q_sh;
+    const float c = log2_scale(a.scale);
+    auto wide = [](uint16_t u) { return __uint_as_float((uint32_t)u << 16); };
+    float m = kNone, l = 0.f, r = 0.f, o[PER] = {};
+    for (int i0 = w.k0; i0 < w.k1; i0 += 64) {
+        const int i = i0 + lane;
+        const Unit u = unit_at<SPARSE>(a, w, i & -kUnit);
+        const bool see = u.page >= 0 && u.place + (i & (kUnit - 1)) < lim;
+        const int64_t cell = (((int64_t)max(u.page, 0) * a.c.heads + w.hk) << a.c.shift) +
+                             (see ? (u.place + (i & (kUnit - 1))) & ((1 << a.c.shift) - 1) : 0);
+        float s = -INFINITY;
+        if (see) {
+            s = 0.f;
+            for (int d = 0; d < D; ++d) s = fmaf(wide(q[d]), wide(a.c.k[cell * D + d]), s);
+        }
+        float top = s;
+#pragma unroll
+        for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+        const float mn = fmaxf(m, top * c), alpha = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        const float e = see ? __builtin_amdgcn_exp2f(fmaf(s, c, -m)) : 0.f, er = (float)(__bf16)e;
+        l = l * alpha + wave_sum(e);
+        r = r * alpha + wave_sum(er);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) o[k] *= alpha;
+        const uint64_t seen = __builtin_amdgcn_ballot_w64(see);
+        for (int k = 0; k < 64; ++k) {
+            if (!(seen >> k & 1)) continue;
+            const float x = __shfl(er, k, 64);
+            const int64_t from = (int64_t)__shfl((long long)cell, k, 64) * D;
+#pragma unroll
+            for (int n = 0; n < PER; ++n) o[n] = fmaf(x, wide(a.c.v[from + lane + 64 * n]), o[n]);
+        }
+    }
+    const bool none = l == 0.f;
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+        const int d = lane + 64 * n;
+        const float v = none ? 0.f : o[n] / r;
+        if (w.ranges > 1)
+            part_o(a, w.part + row)[d] = v;
+        else if (a.f32)
+            static_cast<float *>(a.o)[tok * a.o_ss + h * a.o_sh + d] = v;
+        else
+            static_cast<__bf16 *>(a.o)[tok * a.o_ss + h * a.o_sh + d] = (__bf16)v;
+    }
+    if (lane == 0) store_lse(a, p, w, row, tok, h, none ? -INFINITY : m + __builtin_amdgcn_logf(l));
+}
+
 // Few rows (tiles of 16 MB): memory-bound.  Every wave walks key tiles of its
 // own, 32 keys at a time, with nothing shared: K goes from memory to registers
 // and the matrix unit; V through 2 D x 32 bytes of wave-private LDS, for the
@@ -317,6 +384,7 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
     constexpr int LDS = kFewWaves * V_BYTES > RED ? kFewWaves * V_BYTES : RED;
     __shared__ __attribute__((aligned(1024))) char smem[LDS];
     __shared__ float stat[kFewWaves][3][16 * MB];
+    __shared__ int again[16 * MB];
     const int lane = threadIdx.x & 63, g = lane >> 4, x = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Work w = work_of<SPARSE>(a, p);
@@ -460,6 +528,8 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
         for (int d = 0; d < DB; ++d)
             *reinterpret_cast<f32x4 *>(sum + row * D + (((d * 4 + g) ^ (x & 7)) * 4)) = o[mb][d] * f;
     }
+    const bool apart = a.causal && w.see > w.least;  // rows of the tile see different places
+    if (apart && threadIdx.x < 16 * MB) again[threadIdx.x] = 0;
     __syncthreads();
     for (int t = threadIdx.x; t < w.rows * (D / 4); t += 64 * kFewWaves) {
         const int row = t / (D / 4), d4 = t % (D / 4);
@@ -482,12 +552,17 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
         v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : v * (1.0f / rr);
         const float lse2 = none ? -INFINITY : mm + __builtin_amdgcn_logf(ll);
         const int64_t at = w.row0 + row, tok = w.blk.row + at / G, h = w.hk * G + at % G;
+        if (apart && !finite4(v)) again[row] = 1;
         if (w.ranges == 1)
             store_out4(a, tok, h, d4 * 4, v);
         else
             *reinterpret_cast<f32x4 *>(part_o(a, w.part + row) + d4 * 4) = v;
         if (d4 == 0) store_lse(a, p, w, row, tok, h, lse2);
     }
+    if (!apart) return;
+    __syncthreads();
+    for (int row = wave; row < w.rows; row += kFewWaves)
+        if (__builtin_amdgcn_readfirstlane(again[row]) != 0) redo_row<D, SPARSE>(a, p, w, row);
 }
 
 // Many rows: matrix- and vector-bound, on the schedule of the other caches'
@@ -775,20 +850,31 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
     for (int qb = 0; qb < 2; ++qb) {
         const float ll = quad_sum(lsum[qb]), rr = quad_sum(rsum[qb]);
         const int row = row0 + qb * 16 + x_e;
-        if (row >= w.rows) continue;
         const bool none = ll == 0.f;
         const float inv = none ? 0.f : 1.0f / rr;
         const float lse2 = none ? -INFINITY : mref[qb] + __builtin_amdgcn_logf(ll);
         const int64_t at = w.row0 + row, tok = w.blk.row + at / G, h = w.hk * G + at % G;
+        bool bad = false;
+        if (row < w.rows) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const f32x4 v = o[db][qb] * inv;
-            if (w.ranges == 1)
-                store_out4(a, tok, h, db * 16 + 4 * g_e, v);
-            else
-                *reinterpret_cast<f32x4 *>(part_o(a, w.part + row) + db * 16 + 4 * g_e) = v;
+            for (int db = 0; db < DB; ++db) {
+                const f32x4 v = o[db][qb] * inv;
+                bad |= !finite4(v);
+                if (w.ranges == 1)
+                    store_out4(a, tok, h, db * 16 + 4 * g_e, v);
+                else
+                    *reinterpret_cast<f32x4 *>(part_o(a, w.part + row) + db * 16 + 4 * g_e) = v;
+            }
+            if (g_e == 0) store_lse(a, p, w, row, tok, h, lse2);
         }
-        if (g_e == 0) store_lse(a, p, w, row, tok, h, lse2);
+        uint64_t rows_bad = __builtin_amdgcn_ballot_w64(bad);
+        if (rows_bad != 0 && a.causal && w.see > w.least) {
+            rows_bad |= rows_bad >> 32, rows_bad |= rows_bad >> 16;  // lane x of a row has it
+            // the stores above are this wave's own and come before
+            __asm__ volatile("s_waitcnt vmcnt(0)" : : : "memory");
+            for (int i = 0; i < 16; ++i)
+                if (rows_bad >> i & 1) redo_row<D, SPARSE>(a, p, w, row0 + qb * 16 + i);
+        }
     }
 }
 

@@ -261,3 +261,57 @@ def test_lists_of_any_form(q_block):
     for causal in (True, False):
         o, lse = paged().attn_pages_fwd(bf16(c.q), cache, table, first, n, ints(lists), q_block, causal)
         check(f"lists q_block={q_block}", o, lse, c, causal, selected=lists, q_block=q_block)
+
+
+@pytest.mark.parametrize("rows,H,heads,D", [(2, 2, 1, 64), (9, 4, 2, 128), (40, 2, 2, 128), (60, 1, 1, 64), (300, 2, 2, 128),
+                                            (300, 4, 2, 64)])
+@pytest.mark.parametrize("bits", [0x7fc0, 0x7f80, 0xff80])
+def test_nonfinite_values_in_places_that_a_query_does_not_see(rows, H, heads, D, bits):
+    """An infinity or NaN in the keys or values of a later token of the same chunk is of no account to those before it;
+    those from it on get what the definition gives."""
+    c = Case([rows, 1], [rows + 700, 90], H, heads, D, 32, seed=rows)
+    n, at = rows + 700, rows // 2
+    for tensor, place, channel in ((c.v, n - rows + at, 5), (c.v, n - 1, D - 1), (c.k, n - 1 - rows // 4, 3)):
+        tensor[c.table[0, place // 32], :, place % 32, channel] = bits
+    q, k, v = c.wide()
+    with np.errstate(invalid="ignore", over="ignore"):
+        ro, rl, _, _ = opaged.attn(q, k, v, c.table, c.first, c.lens, True, synth.default_scale(D))
+    o, lse = paged().attn_fwd(bf16(c.q), *held(c), out_dtype=torch.float32)
+    go, gl = host(o), host(lse)
+    fine, lf = np.isfinite(ro), np.isfinite(rl)
+    assert fine[:at].all() and not fine[at:rows].all() and fine[rows:].all()
+    # the bounds of `check` where sum p|v| + |O| <= 3 and the largest sum |q||k| scale <= 20 (an infinite key that gives a
+    # score of -inf has no part in it): 3 (2^-8 + 2 es), es = 20 * 14 * 2^-24 + 2^-22 < 2^-15; n = 1000
+    assert np.isfinite(go[fine]).all() and np.abs(go[fine] - ro[fine]).max() <= 3 * (2.0 ** -8 + 2.0 ** -14)
+    assert np.isfinite(gl[lf]).all() and np.abs(gl[lf] - rl[lf]).max() <= 2.0 ** -15 + 189 * 2.0 ** -24 + 2.0 ** -19
+    # what is not finite by what the query sees: an infinite value with weight, or NaN
+    assert (np.isnan(go) | np.isinf(go))[~fine & np.isnan(ro)].all()
+    inf = np.isinf(ro)
+    assert np.array_equal(go[inf], ro[inf])
+
+
+@pytest.mark.parametrize("rows", [20, 200])
+def test_nonfinite_values_where_nothing_is_seen(rows):
+    """Tokens before place 0 in the same tile as tokens that see an infinity: 0 and -inf."""
+    c = Case([rows], [rows // 2], 2, 2, 128, 16, seed=1)
+    c.v[c.table[0, 0], :, 0, 7] = 0x7f80
+    o, lse = paged().attn_fwd(bf16(c.q), *held(c))
+    none = rows - rows // 2
+    assert bool((o[:none] == 0).all()) and bool(torch.isneginf(lse[:, :none]).all())
+    assert bool(torch.isposinf(o[none:, :, 7]).all()) and bool(torch.isfinite(o[none:, :, :7]).all())
+
+
+@pytest.mark.parametrize("rows,q_block", [(70, 16), (200, 64), (130, 128)])
+def test_nonfinite_values_in_selected_pages(rows, q_block):
+    c = Case([rows], [rows + 500], 4, 2, 64, 16, seed=rows)
+    place = rows + 500 - rows // 3
+    c.v[c.table[0, place // 16], :, place % 16, 2] = 0x7fc0
+    clean = Case([rows], [rows + 500], 4, 2, 64, 16, seed=rows)
+    pages = -(-(rows + 500) // 16)
+    lists = np.tile(np.arange(pages, dtype=np.int32)[::-1], (c.T // q_block + 1, 2, 1))
+    o, lse = paged().attn_pages_fwd(bf16(c.q), *held(c), ints(lists), q_block, out_dtype=torch.float32)
+    co, cl = paged().attn_pages_fwd(bf16(clean.q), *held(clean), ints(lists), q_block, out_dtype=torch.float32)
+    before = place - 500
+    assert bool(torch.isfinite(o[:before]).all()) and float((o[:before] - co[:before]).abs().max()) <= 2.0 ** -6
+    assert bool(torch.isnan(o[before:, :, 2]).all()) and bool(torch.isfinite(o[before:, :, 3:]).all())
+    assert float((lse - cl).abs().max()) <= 2.0 ** -16
