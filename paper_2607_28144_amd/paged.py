@@ -101,27 +101,30 @@ class Rotary:
         self._c = _lib.RotaryTable(self.turns.data_ptr(), self.dim // 2, int(layout == "interleaved"), self.amplitude)
 
 
-def _packed(t: torch.Tensor, name: str, heads: int, D: int, T: int, idx: int, dtype=torch.bfloat16) -> _lib.Tensor:
+_BF16, _INT32 = torch.bfloat16, torch.int32
+
+
+def _packed(t: torch.Tensor, name: str, shape: Tuple[int, int, int], idx: int, dtype=_BF16) -> _lib.Tensor:
     """The descriptor of a [T, heads, D] tensor of this type on device idx; refuses any other."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    s, st = t.shape, t.stride()
-    if t.dtype is not dtype or t.get_device() != idx or len(st) != 3 or s[0] != T or s[1] != heads or s[2] != D \
-            or st[2] != 1:
-        raise ValueError(f"{name} must be a {dtype} tensor [{T}, {heads}, {D}] with unit channel stride on cuda:{idx}, got "
-                         f"{t.dtype} {tuple(s)} on {t.device}")
-    # of a single row or head, whose stride torch leaves to chance: any
-    return _lib.Tensor(t.data_ptr(), 0, st[0] if T > 1 else 0, st[1] if heads > 1 else 0)
+    if t.dtype is dtype and t.shape == shape and t.get_device() == idx:
+        st = t.stride()
+        if st[2] == 1:  # of a single row or head, whose stride torch leaves to chance: any
+            return _lib.Tensor(t.data_ptr(), 0, st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0)
+    raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} with unit channel stride on cuda:{idx}, got {t.dtype} "
+                     f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _batch(cache: PagedCache, table, first, lens, T: int, idx: int) -> _lib.PageBatch:
-    if table.dim() != 2:
-        raise ValueError(f"table must be [B, columns], got {tuple(table.shape)}")
-    B, columns = table.shape
-    _lib.int32(B=B, columns=columns, T=T)
-    stride = _lib.matrix(table, "table", torch.int32, B, columns, idx)
-    return _lib.PageBatch(table.data_ptr(), _lib.vector(first, "first", torch.int32, B + 1, idx),
-                          _lib.vector(lens, "lens", torch.int32, B, idx), stride, B, columns, T)
+def _batch(table, first, lens, T: int, idx: int) -> _lib.PageBatch:
+    """The descriptor of a call's sequences on device idx; refuses any other tensors."""
+    s = table.shape
+    if len(s) != 2:
+        raise ValueError(f"table must be [B, columns], got {tuple(s)}")
+    B, columns = s
+    if B >= 1 << 31 or columns >= 1 << 31 or T >= 1 << 31:
+        _lib.int32(B=B, columns=columns, T=T)
+    stride = _lib.matrix(table, "table", _INT32, B, columns, idx)
+    return _lib.PageBatch(table.data_ptr(), _lib.vector(first, "first", _INT32, B + 1, idx),
+                          _lib.vector(lens, "lens", _INT32, B, idx), stride, B, columns, T)
 
 
 def _index(cache: PagedCache) -> int:
@@ -139,23 +142,26 @@ def append(cache: PagedCache, table: torch.Tensor, first: torch.Tensor, lens: to
     where the cache has means.  Returns q's (q_out, which may be q; a new tensor if
     None; None without q)."""
     idx = _index(cache)
+    D = cache.D
     T = k.shape[0]
-    n = _batch(cache, table, first, lens, T, idx)
-    kd = _packed(k, "k", cache.heads, cache.D, T, idx)
-    vd = _packed(v, "v", cache.heads, cache.D, T, idx)
+    n = _batch(table, first, lens, T, idx)
+    kd = _packed(k, "k", (T, cache.heads, D), idx)
+    vd = _packed(v, "v", (T, cache.heads, D), idx)
     H, qd, od = 0, None, None
     if q is not None:
         H = q.shape[1] if q.dim() == 3 else 0
-        qd = _packed(q, "q", H, cache.D, T, idx)
+        qd = ctypes.byref(_packed(q, "q", (T, H, D), idx))
         if q_out is None:
-            q_out = torch.empty(T, H, cache.D, dtype=torch.bfloat16, device=cache.device)
-        od = _packed(q_out, "q_out", H, cache.D, T, idx)
+            q_out = torch.empty(T, H, D, dtype=_BF16, device=cache.device)
+            od = ctypes.byref(_lib.Tensor(q_out.data_ptr(), 0, H * D, D))
+        else:
+            od = ctypes.byref(_packed(q_out, "q_out", (T, H, D), idx))
         if H == 0:
             qd = od = None
     elif q_out is not None:
         raise ValueError("q_out without q")
-    wq = _lib.vector(w_q, "w_q", torch.bfloat16, cache.D, idx)
-    wk = _lib.vector(w_k, "w_k", torch.bfloat16, cache.D, idx)
+    wq = _lib.vector(w_q, "w_q", _BF16, D, idx)
+    wk = _lib.vector(w_k, "w_k", _BF16, D, idx)
     rc = None
     if rotary is not None:
         if rotary.turns.get_device() != idx:
@@ -163,8 +169,8 @@ def append(cache: PagedCache, table: torch.Tensor, first: torch.Tensor, lens: to
         rc = ctypes.byref(rotary._c)
     with _lib.on_device(idx):
         st = _lib.load().regenvc_paged_append(
-            ctypes.byref(cache._c), ctypes.byref(n), None if qd is None else ctypes.byref(qd), ctypes.byref(kd),
-            ctypes.byref(vd), wq, wk, eps, rc, None if od is None else ctypes.byref(od), H, _lib.raw_stream(idx))
+            ctypes.byref(cache._c), ctypes.byref(n), qd, ctypes.byref(kd), ctypes.byref(vd), wq, wk, eps, rc, od, H,
+            _lib.raw_stream(idx))
     _lib.check(st, "regenvc_paged_append")
     return q_out
 
@@ -192,15 +198,15 @@ def _attn(q, cache, table, first, lens, chosen, q_block, causal, scale, max_rows
     if q.dim() != 3:
         raise ValueError(f"q must be [T, H, D], got {tuple(q.shape)}")
     T, H, D = q.shape
-    n = _batch(cache, table, first, lens, T, idx)
-    qd = _packed(q, "q", H, cache.D, T, idx)
+    n = _batch(table, first, lens, T, idx)
+    qd = _packed(q, "q", (T, H, cache.D), idx)
     if out_dtype not in _DT:
         raise TypeError(f"out_dtype must be bfloat16 or float32, got {out_dtype}")
     if out is None:
         out = torch.empty(T, H, D, dtype=out_dtype, device=cache.device)
         od = _lib.Tensor(out.data_ptr(), 0, H * D, D)
     else:
-        od = _packed(out, "out", H, D, T, idx, out_dtype)
+        od = _packed(out, "out", (T, H, D), idx, out_dtype)
     if lse_out is not None:
         if tuple(lse_out.shape) != (H, T):
             raise ValueError(f"lse must be {(H, T)}, got {tuple(lse_out.shape)}")
@@ -219,7 +225,8 @@ def _attn(q, cache, table, first, lens, chosen, q_block, causal, scale, max_rows
         sp = _lib.vector(chosen, "selected", torch.int32, chosen.numel(), idx)
     rows = T if max_rows is None else int(max_rows)
     places = n.columns * cache.page if max_len is None else int(max_len)
-    _lib.int32(H=H, max_rows=rows, max_len=places)
+    if H >= 1 << 31 or not 0 <= rows < 1 << 31 or not 0 <= places < 1 << 31:
+        _lib.int32(H=H, max_rows=rows, max_len=places)
     need = _need((n.B, T, H, cache.heads, D, cache.page, q_block, count, rows, places), idx)
     with _lib.on_device(idx):
         ws = torch.empty(need, dtype=torch.uint8, device=cache.device) if need > 0 else None
@@ -258,8 +265,8 @@ def select_pages(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, first:
     if q.dim() != 3:
         raise ValueError(f"q must be [T, H, D], got {tuple(q.shape)}")
     T, H, _ = q.shape
-    n = _batch(cache, table, first, lens, T, idx)
-    qd = _packed(q, "q", H, cache.D, T, idx)
+    n = _batch(table, first, lens, T, idx)
+    qd = _packed(q, "q", (T, H, cache.D), idx)
     _lib.int32(H=H, count=count, q_block=q_block, keep_first=keep_first, keep_last=keep_last)
     if q_block < 1 or count < 0:
         raise ValueError(f"q_block={q_block}, count={count}")
