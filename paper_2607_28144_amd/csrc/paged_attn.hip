@@ -551,7 +551,8 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
                                                   ((d4 ^ (row & 7)) * 4));
         v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : v * (1.0f / rr);
         const float lse2 = none ? -INFINITY : mm + __builtin_amdgcn_logf(ll);
-        const int64_t at = w.row0 + row, tok = w.blk.row + at / G, h = w.hk * G + at % G;
+        const int at = w.row0 + row, query = at / G;  // 32 bits: a division of 64 takes longer than the row
+        const int64_t tok = w.blk.row + query, h = w.hk * G + at - query * G;
         if (apart && !finite4(v)) again[row] = 1;
         if (w.ranges == 1)
             store_out4(a, tok, h, d4 * 4, v);
@@ -853,7 +854,8 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
         const bool none = ll == 0.f;
         const float inv = none ? 0.f : 1.0f / rr;
         const float lse2 = none ? -INFINITY : mref[qb] + __builtin_amdgcn_logf(ll);
-        const int64_t at = w.row0 + row, tok = w.blk.row + at / G, h = w.hk * G + at % G;
+        const int at = w.row0 + row, query = at / G;  // 32 bits: a division of 64 takes longer than the row
+        const int64_t tok = w.blk.row + query, h = w.hk * G + at - query * G;
         bool bad = false;
         if (row < w.rows) {
 #pragma unroll

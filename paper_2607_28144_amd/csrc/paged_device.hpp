@@ -86,12 +86,17 @@ __device__ __forceinline__ uint32_t wave_upto(uint32_t x)
     x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
     return x;
 }
-// The sum of a wave's numbers, the same in every lane.
+// The sum of a wave's numbers, the same in every lane: each exchange adds the same two numbers on both sides.
 __device__ __forceinline__ float wave_sum(float x)
 {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
-    return x;
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kXor1, 0xf, 0xf, true));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kXor2, 0xf, 0xf, true));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kMirror8, 0xf, 0xf, true));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kRotate8, 0xf, 0xf, true));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(u[0]) + __uint_as_float(u[1]);
 }
 
 }  // namespace paged
