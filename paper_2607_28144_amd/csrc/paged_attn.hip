@@ -89,30 +89,34 @@ __device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, 
     const float size = fmaxf((float)p.least, all * (one ? 1.f : 1.25f) / p.slots);
     Piece k{0, 1, -1, 0, 0, 0, 0, 0};
     uint32_t before = 0;
-    for (int c = 0; c < a.n.B; c += 64) {
-        if (a.n.B > 64) look(c);
-        // of one sequence, as many as there are workgroups for; of several, the mean of a row: there are enough
-        const int most = one ? (int)(p.groups / max(1, tiles * heads)) : kMostRanges;
-        const int ranges = max(1, min(min(kMostRanges, most), (int)(one ? floorf(keys / size) : ceilf(mean / size))));
-        const uint32_t mine = (uint32_t)tiles * ranges * heads, upto = before + wave_upto(mine);
-        const uint64_t done = __builtin_amdgcn_ballot_w64(upto <= id);
-        if (done != ~(uint64_t)0) {
-            const int at = __popcll(done);  // upto ascends
-            k.b = c + at;
-            k.ranges = __builtin_amdgcn_readlane(ranges, at);
-            const uint32_t rest = id - (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at);
-            const uint32_t per = (uint32_t)k.ranges * heads;
-            const uint32_t t = rest / per, r2 = rest - t * per;
-            k.tile = __builtin_amdgcn_readlane(tiles, at) - 1 - (int)t;  // the last first: in a causal call it has the most keys
-            k.range = (int)(r2 / (uint32_t)heads);
-            k.hk = (int)r2 - k.range * heads;
-            k.first = __builtin_amdgcn_readlane(first, at);
-            k.rows = __builtin_amdgcn_readlane(rows, at);
-            k.len = __builtin_amdgcn_readlane(len, at);
-            return k;
+    // Of several, those with the longest pieces first, in three classes by their keys, so that none of them begins late.
+    for (int rank = 0; rank < (one ? 1 : 3); ++rank)
+        for (int c = 0; c < a.n.B; c += 64) {
+            if (a.n.B > 64) look(c);
+            // of one sequence, as many as there are workgroups for; of several, the mean of a row: there are enough
+            const int most = one ? (int)(p.groups / max(1, tiles * heads)) : kMostRanges;
+            const int ranges = max(1, min(min(kMostRanges, most), (int)(one ? floorf(keys / size) : ceilf(mean / size))));
+            const float piece = mean / ranges;
+            const bool now = one || (piece >= 0.7f * size ? rank == 0 : piece >= 0.3f * size ? rank == 1 : rank == 2);
+            const uint32_t mine = now ? (uint32_t)tiles * ranges * heads : 0, upto = before + wave_upto(mine);
+            const uint64_t done = __builtin_amdgcn_ballot_w64(upto <= id);
+            if (done != ~(uint64_t)0) {
+                const int at = __popcll(done);  // upto ascends
+                k.b = c + at;
+                k.ranges = __builtin_amdgcn_readlane(ranges, at);
+                const uint32_t rest = id - (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at);
+                const uint32_t per = (uint32_t)k.ranges * heads;
+                const uint32_t t = rest / per, r2 = rest - t * per;
+                k.tile = __builtin_amdgcn_readlane(tiles, at) - 1 - (int)t;  // the last first: in a causal call it has the most keys
+                k.range = (int)(r2 / (uint32_t)heads);
+                k.hk = (int)r2 - k.range * heads;
+                k.first = __builtin_amdgcn_readlane(first, at);
+                k.rows = __builtin_amdgcn_readlane(rows, at);
+                k.len = __builtin_amdgcn_readlane(len, at);
+                return k;
+            }
+            before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
-        before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-    }
     return k;
 }
 
