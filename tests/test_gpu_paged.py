@@ -315,3 +315,52 @@ def test_nonfinite_values_in_selected_pages(rows, q_block):
     assert bool(torch.isfinite(o[:before]).all()) and float((o[:before] - co[:before]).abs().max()) <= 2.0 ** -6
     assert bool(torch.isnan(o[before:, :, 2]).all()) and bool(torch.isfinite(o[before:, :, 3:]).all())
     assert float((lse - cl).abs().max()) <= 2.0 ** -16
+
+
+def plan(c, q_block=1, count=0, max_rows=None, max_len=None):
+    import ctypes
+    from paper_2607_28144_amd import _lib
+    p = _lib.PagedAttnPlan()
+    s = _lib.PagedAttnShape(c.B, c.T, c.H, c.heads, c.D, c.page, q_block, count, c.T if max_rows is None else max_rows,
+                            c.table.shape[1] * c.page if max_len is None else max_len)
+    n_cu = torch.cuda.get_device_properties(0).multi_processor_count
+    assert _lib.load().regenvc_paged_attn_plan_query(ctypes.byref(s), n_cu, ctypes.byref(p)) == 0
+    return p
+
+
+# rows of each of B sequences, their places (times 1, 2, 3 in turn), H, heads, D, tile rows
+TILES = [(2, 5, 700, 2, 2, 128, 16), (2, 30, 700, 2, 2, 64, 32), (70, 60, 200, 4, 4, 64, 64), (40, 60, 260, 4, 4, 128, 64),
+         (33, 31, 100, 8, 4, 128, 64), (2, 300, 500, 2, 2, 64, 256)]
+
+
+@pytest.mark.parametrize("B,rows,places,H,heads,D,tile", TILES)
+def test_every_tile(B, rows, places, H, heads, D, tile):
+    """Tiles of each number of rows, which the plan says are taken, with sequences that differ."""
+    lens = [places * (1 + b % 3) for b in range(B)]
+    c = Case([rows - b % 2 for b in range(B)], lens, H, heads, D, 32, seed=tile + D)
+    assert plan(c, max_rows=rows).tile_rows == tile
+    o, lse = paged().attn_fwd(bf16(c.q), *held(c), max_rows=rows, out_dtype=torch.float32)
+    check(f"tile {tile} D={D}", o, lse, c, True, f32=True)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_tiles_of_selected_pages(D):
+    """64 rows of many blocks of queries, each with pages of its own."""
+    c = Case([1000, 700], [1200, 701], 5, 5, D, 16, seed=D)
+    rng = np.random.default_rng(1)
+    blocks = c.T // 64 + 2
+    lists = np.sort(np.argsort(rng.random((blocks, 5, 44)))[:, :, :20]).astype(np.int32)
+    assert plan(c, 64, 20).tile_rows == 64
+    o, lse = paged().attn_pages_fwd(bf16(c.q), *held(c), ints(lists), 64, out_dtype=torch.float32)
+    check(f"selected, 64 rows, D={D}", o, lse, c, True, selected=lists, q_block=64, f32=True)
+
+
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_ranges_of_one_sequence_and_of_several(rows):
+    """Keys cut into ranges, which the plan allows: one long sequence alone, and between short ones."""
+    for lens in ([9000], [9000, rows, 130 + rows], [5000, 2000 + rows, 700 + rows, rows]):
+        c = Case([rows] * len(lens), lens, 2, 1, 64, 128, seed=rows + len(lens))
+        assert plan(c).split == 1
+        for causal in (True, False):
+            o, lse = paged().attn_fwd(bf16(c.q), *held(c), causal=causal, out_dtype=torch.float32)
+            check(f"ranges rows={rows} {lens}", o, lse, c, causal, f32=True)
