@@ -43,7 +43,8 @@ typedef struct {
             without places: nothing is read or written there.
      first: [B + 1], ascending, in [0, T].  Rows before first[0] and from first[B]
             on belong to no sequence: their outputs are left as they were.
-     lens:  [B], held to [0, columns * page] */
+     lens:  [B]; below 0 counts as 0.  Attention and selection hold it to columns *
+            page; an append beyond that stores what the table has room for */
 typedef struct {
     const int32_t *table, *first, *lens;
     int64_t table_stride;

@@ -647,12 +647,14 @@ void attn_many_kernel(AttnArgs a, AttnPlan p)
     // The first places of a tile's four units: with selected pages lane i has those of tile i of 64.
     int at4[4] = {kNowhere, kNowhere, kNowhere, kNowhere};
     int gaps = 0;
+    auto firsts = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) at4[t] = unit_at<SPARSE>(a, w, w.k0 + (u + lane) * kManyKeys + t * kUnit).place;
+    };
+    if constexpr (SPARSE) firsts(0);
     auto places = [&](int u, int (&pl)[4]) __attribute__((always_inline)) {
         if constexpr (SPARSE) {
-            if ((u & 63) == 0) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) at4[t] = unit_at<SPARSE>(a, w, w.k0 + (u + lane) * kManyKeys + t * kUnit).place;
-            }
+            if ((u & 63) == 0 && u > 0) firsts(u);
 #pragma unroll
             for (int t = 0; t < 4; ++t) pl[t] = __builtin_amdgcn_readlane(at4[t], u & 63);
         } else {
@@ -908,10 +910,10 @@ template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, AttnPlan p)
 {
     constexpr int LPR = D / 4;
-    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
-    if (id >= (int64_t)a.n.T * a.H) return;
+    const uint32_t id = blockIdx.x * (256u / LPR) + threadIdx.x / LPR, token = id / (uint32_t)a.H;  // at most 2^29
+    if (token >= (uint32_t)a.n.T) return;
     const int d = threadIdx.x % LPR * 4;
-    const int64_t h = id % a.H, t = id / a.H, step = (int64_t)a.c.heads * p.tile_rows;
+    const int64_t h = id - token * a.H, t = token, step = (int64_t)a.c.heads * p.tile_rows;
     Parts k;
     if (!joined(a, p, t, h, k)) return;
     float m = kNone, l = 0.f;
@@ -952,7 +954,8 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, AttnPlan
     __shared__ float weight[kMostRanges], total;
     __shared__ f32x4 sum[SL][LPR];
     const int i = threadIdx.x, d = i % LPR, slice = i / LPR;
-    const int64_t id = blockIdx.x, h = id % a.H, t = id / a.H, step = (int64_t)a.c.heads * p.tile_rows;
+    const uint32_t token = blockIdx.x / (uint32_t)a.H;
+    const int64_t h = blockIdx.x - token * a.H, t = token, step = (int64_t)a.c.heads * p.tile_rows;
     Parts k;
     if (!joined(a, p, t, h, k)) return;
     f32x4 part[KEEP];  // requested before the weights are known
@@ -1040,7 +1043,8 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     // ranges of `least` keys.  Workgroups: piece_of makes at most one to a tile and one to a slot; of one sequence one to a
     // slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
     const int64_t rounds = s.B > 1 || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
-    p.split = tiles < (s.B > 1 ? 4 : 2) * (int64_t)p.slots && s.B <= 1024 && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
+    const int64_t enough = s.B > 1 ? 4 * (int64_t)p.slots : s.count > 0 ? p.slots / 2 + 1 : 2 * (int64_t)p.slots;
+    p.split = tiles < enough && s.B <= 1024 && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
     p.groups = !p.split ? blocks * p.tiles * s.heads : s.B > 1 ? tiles + p.slots : std::max(tiles, rounds * p.slots);
     p.ws_bytes = p.split ? (p.groups * p.tile_rows * (int64_t)(s.D + 1) + 2 * (int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
     return p;
