@@ -5,9 +5,9 @@ video diffusion transformer, its per-chunk partials and log-sum-exp merge,
 cross-attention to conditioning tokens, and the q/k RMSNorm + 3D rotary
 embedding that produce the attention inputs (plus a ring step that merges a
 chunk's result straight into the running output) -- hand-written HIP kernels behind
-a C ABI (include/regenvc_attn.h).  The submodules dit, vae and mx hold the
+a C ABI (include/regenvc_attn.h).  The submodules dit, vae, mx and paged hold the
 diffusion-transformer block with its norms and their gradients, the VAE tile,
-and linear layers and a key/value cache in MXFP4.  Import is cheap: the library
+linear layers and a key/value cache in MXFP4, and a bf16 key/value cache in pages.  Import is cheap: the library
 and torch are loaded on first use.
 """
 

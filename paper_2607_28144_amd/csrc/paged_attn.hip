@@ -58,8 +58,11 @@ struct Work {
 // plan says so), every wave goes over the sequences, 64 at a time, adds up what there
 // is to do, and finds the one that workgroup `id` has a piece of.  One sequence's
 // keys are cut into as many ranges as fill the slots once; of several, at 5/4 of what
-// a slot has on the average.  (Chunks of several lengths, 124 tiles of queries x
-// places: at the average length of all sequences by the host's bound 101 us.)
+// a slot has on the average, those with the longest pieces first.  Seven chunks of 1
+// to 1365 tokens behind 0 to 10663 others, 20 heads on 4: 83 us so; cut at 1 or 1.5
+// of the average 87 and 91, in the order of the call 96, cut by a bound that the host
+// has 133 (tiles of 256 rows: each workgroup's begin and end are worth six rounds of
+// keys, so that finer pieces cost more than they even out).
 struct Piece {
     int b, ranges, tile, range, hk;  // tile -1: no such piece
     int first, rows, len;            // of the sequence
@@ -374,6 +377,14 @@ __device__ __forceinline__ void redo_row(const AttnArgs &a, const AttnPlan &p, c
 //
 // 16 rows: eight waves, so that few places need no second launch to join ranges
 // (1024 keys are four rounds); more rows take the registers of two waves each.
+// One query against 32760 places x 12 heads of 128 (201 MB): 39 us, 5.1 TB/s, and
+// 4.8 for the join of 21 ranges; queries of 16 sequences of 1 to 10920 places, 16
+// heads of 64 on 4 (75 MB): 16.4 + 3.9.  16 pages of 64 for one query: 10.9 + 3.9,
+// of which a chain of eight dependent loads has most (sequence, list, table, keys).
+// 64 rows: 25 blocks of 64 queries x 12 heads with 64 pages of 64 each (629 MB from
+// the caches, 321 from HBM): 111 us, two rounds of workgroups, each at the rate of
+// what lies behind the L2 (9.8 TB/s); the next tile's scores beside a tile's weights
+// (142 us instead of 135, with the selection) or keys in three ranges (149) lose.
 constexpr int few_waves(int rows) { return rows == 16 ? 8 : 4; }
 
 template <int D, int MB, bool SPARSE>
@@ -581,6 +592,11 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
 // wave while its vector unit works for the other.  LDS is a ring of four stages:
 // tile u + 3 goes where tile u - 1 was.  Its K was last read by M(u - 1) of waves
 // 4-7, its V by M(u) of waves 4-7: a barrier before V(u) of the waves that load it.
+// Scores of places that a row does not see are set to -inf before one form of the
+// weights (with a form for either, 90 registers spilled: 409 us instead of 335).
+// 10920 causal queries x 12 heads of 128: 335-350 us, 1.05-1.09 PFLOP/s, matrix units
+// busy for 51 % of the cycles, no LDS conflicts; 1560 queries against 32760 places:
+// 293-301 us in three ranges and 8 for their join; both at the power limit.
 constexpr int kManyWaves = 8, kManyRows = 32 * kManyWaves, kManyKeys = 64;
 
 template <int D, bool SPARSE>
