@@ -137,7 +137,7 @@ regenvc_status regenvc_paged_attn_plan_query(const regenvc_paged_attn_shape *sha
    taken.
      selected: int32 [T / q_block + B, heads, count]; block i of sequence b is
           first[b] / q_block + b + i; pages ascending, then -1; every entry is
-          written, blocks without queries with -1
+          written, blocks without queries (with H = 0: all) with -1
    keep_first, keep_last >= 0, their sum at most count; count in [1, 16384],
    columns at most 16384, q_block in [1, 2^20], T / q_block + B below 2^24. */
 regenvc_status regenvc_paged_select(const regenvc_tensor *q, const regenvc_page_pool *pool,

@@ -556,9 +556,9 @@ hipError_t launch_append(const AppendArgs &a, int n_cu, hipStream_t stream)
     return hipGetLastError();
 }
 
-hipError_t launch_select(const SelectArgs &a, int n_cu, hipStream_t stream)
+hipError_t launch_select(const SelectArgs &a, int64_t blocks, int n_cu, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.n.T / a.q_block + a.n.B), (unsigned)a.c.heads);
+    const dim3 grid((unsigned)blocks, (unsigned)a.c.heads);
     const size_t lds = a.n.columns <= a.count ? 0 : (size_t)a.n.columns * 8;
     // few workgroups: as many waves to each as there can be, whose latencies and 64-bit products are what it takes
     const bool few = (int64_t)grid.x * grid.y <= n_cu;

@@ -74,7 +74,7 @@ regenvc_status check_batch(const char *fn, const regenvc_page_batch *n, int32_t 
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: B=%d T=%d columns=%d pages of %d places: too many for one call", fn, n->B,
                      n->T, n->columns, page);
     r[0] = r[1] = r[2] = Range{0, 0};
-    if (n->B == 0 || n->T == 0) return REGENVC_OK;
+    if (n->B == 0) return REGENVC_OK;
     if ((n->columns > 0 && n->table == nullptr) || n->first == nullptr || n->lens == nullptr)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: table, first or lens is NULL", fn);
     if (!aligned(n->table, 4) || !aligned(n->first, 4) || !aligned(n->lens, 4))
@@ -277,20 +277,27 @@ regenvc_status regenvc_paged_select(const regenvc_tensor *q, const regenvc_page_
     if (batch->columns > paged::kMaxSelectColumns || blocks > kMaxGroups)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d columns, %lld blocks (at most %d, %lld)", fn, batch->columns,
                      (long long)blocks, paged::kMaxSelectColumns, (long long)kMaxGroups);
-    if (batch->B == 0 || batch->T == 0 || H == 0) return done();
-    if (pool->means == nullptr && pool->pages > 0)
+    if (blocks == 0) return done();
+    const bool any = batch->B > 0 && batch->T > 0 && H > 0;  // else every block is one without queries: -1
+    if (any && pool->means == nullptr && pool->pages > 0)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: the pool has no means", fn);
-    Range rq;
-    if ((st = packed_range("q", q, batch->T, H, pool->D, 2, &rq)) != REGENVC_OK) return st;
+    Range rq{0, 0};
+    if (any && (st = packed_range("q", q, batch->T, H, pool->D, 2, &rq)) != REGENVC_OK) return st;
     if (selected == nullptr) return failf(REGENVC_ERR_INVALID_ARG, "%s: selected is NULL", fn);
     if (!aligned(selected, 4)) return failf(REGENVC_ERR_UNSUPPORTED, "%s: selected must be 4-byte aligned", fn);
     const Range rs = range_of(selected, blocks * pool->heads * count * 4);
     for (const Range &i : {rq, r.batch[0], r.batch[1], r.batch[2], r.pool[0], r.pool[1], r.pool[2]})
         if (overlaps(rs, i)) return failf(REGENVC_ERR_INVALID_ARG, "%s: selected overlaps an input", fn);
     if ((st = regenvc::abi::device_ok()) != REGENVC_OK) return st;
-    const paged::SelectArgs a{pool_of(*pool), batch_of(*batch), u16(q->ptr), q->stride_s, q->stride_h, selected, H,
-                              q_block,        count,            keep_first,  keep_last,   causal != 0};
-    return regenvc::abi::launch_status(paged::launch_select(a, regenvc::device_cu_count(), static_cast<hipStream_t>(stream)),
+    paged::SelectArgs a{};
+    a.c = pool_of(*pool), a.n = batch_of(*batch);
+    if (any)
+        a.q = u16(q->ptr), a.q_ss = q->stride_s, a.q_sh = q->stride_h;
+    else
+        a.n.B = 0;
+    a.selected = selected, a.H = H, a.q_block = q_block, a.count = count;
+    a.keep_first = keep_first, a.keep_last = keep_last, a.causal = causal != 0;
+    return regenvc::abi::launch_status(paged::launch_select(a, blocks, regenvc::device_cu_count(), static_cast<hipStream_t>(stream)),
                                        fn);
 }
 

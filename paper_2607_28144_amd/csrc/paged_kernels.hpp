@@ -31,7 +31,7 @@ struct AppendArgs {
 };
 hipError_t launch_append(const AppendArgs &a, int n_cu, hipStream_t stream);
 
-// selected: int32 [T / q_block + B, heads, count].
+// selected: int32 [blocks, heads, count]; n.B = 0: blocks without queries.
 struct SelectArgs {
     Pool c;
     Batch n;
@@ -41,7 +41,7 @@ struct SelectArgs {
     int32_t H, q_block, count, keep_first, keep_last, causal;
 };
 constexpr int kMaxSelectColumns = 16384;  // a score of 64 bits each, in LDS
-hipError_t launch_select(const SelectArgs &a, int n_cu, hipStream_t stream);
+hipError_t launch_select(const SelectArgs &a, int64_t blocks, int n_cu, hipStream_t stream);
 
 struct AttnShape {
     int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len;  // count 0: every page

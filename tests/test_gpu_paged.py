@@ -227,6 +227,22 @@ def test_selection_ties_and_nonfinite_scores():
             assert np.array_equal(got.cpu().numpy(), ref), (sign, count)
 
 
+def test_selection_without_queries():
+    """No rows, no sequences, no heads of queries: every entry is -1."""
+    c = Case([3, 2], [40, 50], 2, 2, 64, 16, seed=1)
+    cache, table, first, n = held(c, torch.zeros(c.k.shape[0], 2, 64, dtype=torch.bfloat16, device="cuda"))
+    q = bf16(c.q)
+    for args in ((q[:0], cache, table, torch.zeros_like(first), n), (q, cache, table[:0], first[:1], n[:0]),
+                 (q[:, :0], cache, table, first, n)):
+        blocks = args[0].shape[0] // 2 + args[2].shape[0]
+        out = torch.full((blocks, 2, 4), 7, dtype=torch.int32, device="cuda")
+        paged().select_pages(*args, 4, q_block=2, out=out)
+        assert blocks > 0 and bool((out == -1).all())
+    for f in (paged().attn_fwd, lambda *a: paged().attn_pages_fwd(*a, torch.zeros(2, 2, 4, dtype=torch.int32, device="cuda"), 2)):
+        o, lse = f(q[:0], cache, table, torch.zeros_like(first), n)
+        assert o.shape == (0, 2, 64) and lse.shape == (2, 0)
+
+
 def test_selection_over_many_pages():
     """As many columns as a call takes (131072 bytes of scores in LDS), and scores that differ in their last bits."""
     pages, heads, D = 16384, 1, 64

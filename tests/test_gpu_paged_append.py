@@ -80,6 +80,7 @@ CASES = [([1], [1], 1, 1, 64, 16), ([1], [300], 12, 12, 128, 64), ([1, 1, 1], [1
 @pytest.mark.parametrize("rows,lens,H,heads,D,page", CASES)
 @pytest.mark.parametrize("layout,rot,norm,means", [("half", 1.0, True, True), ("interleaved", 1.0, False, False),
                                                    ("half", 0.5, False, True), ("interleaved", 0.25, True, False),
+                                                   ("half", 0.25, True, True),
                                                    ("none", 0, True, True), ("none", 0, False, False)])
 def test_append(rows, lens, H, heads, D, page, layout, rot, norm, means):
     c = Case(rows, lens, H, heads, D, page, seed=sum(lens) + H, lead=1, tail=2)

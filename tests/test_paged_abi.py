@@ -136,7 +136,10 @@ def test_select_refusals(lib):
     refused(lib, INV, "overlaps", call(sel=Q + 16))
     refused(lib, INV, "overlaps", call(sel=M))
     refused(lib, INV, "overlaps", call(sel=TAB))
-    assert call(n=batch(B=0)) == 0 and call(n=batch(T=0)) == 0 and call(H=0) == 0
+    # without a query there are blocks all the same, and entries to write; none with neither rows nor sequences
+    for kw in ({"n": batch(T=0)}, {"n": batch(B=0)}, {"H": 0}):
+        refused(lib, INV, "selected is NULL", call(sel=None, q=None, **kw))
+    assert call(n=batch(B=0, T=1)) == 0 and call(n=batch(B=0, T=0)) == 0
 
 
 def test_attention_refusals(lib):
