@@ -39,6 +39,11 @@ constexpr int kNowhere = 0x3fffffff;  // the place of a unit that does not exist
 constexpr int kKeyAlign = 64;         // ranges of keys begin at multiples of it
 constexpr int kMostRanges = 64;       // of a tile's keys
 
+// Sequences of a call whose keys are cut. Each workgroup goes over all of them to find its piece, and over more of them
+// that costs more than ranges give. Single tokens of 4 heads over one key head, D = 128, cut or not: 256 sequences of up to
+// 2048 places 45 or 40 us, 65 17 or 26, 100 of up to 32768 216 or 376, 256 of up to 1024 with one of 32768 36 or 292.
+constexpr int kMostCut = 256;
+
 // What a workgroup works on: `rows` rows (query, head) of a block of queries, from
 // its row `row0` on, and of their keys range `range` of `ranges`, [k0, k1) in units
 // of 16.  Key i is place i, or with selected pages place i % page of the page that
@@ -93,14 +98,16 @@ __device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, 
     Piece k{0, 1, -1, 0, 0, 0, 0, 0};
     uint32_t before = 0;
     // Of several, those with the longest pieces first, in three classes by their keys, so that none of them begins late.
-    for (int rank = 0; rank < (one ? 1 : 3); ++rank)
+    // (Beyond 64, whose lengths are not all at hand, in their order.)
+    const int classes = one || a.n.B > 64 ? 1 : 3;
+    for (int rank = 0; rank < classes; ++rank)
         for (int c = 0; c < a.n.B; c += 64) {
             if (a.n.B > 64) look(c);
             // of one sequence, as many as there are workgroups for; of several, the mean of a row: there are enough
             const int most = one ? (int)(p.groups / max(1, tiles * heads)) : kMostRanges;
             const int ranges = max(1, min(min(kMostRanges, most), (int)(one ? floorf(keys / size) : ceilf(mean / size))));
             const float piece = mean / ranges;
-            const bool now = one || (piece >= 0.7f * size ? rank == 0 : piece >= 0.3f * size ? rank == 1 : rank == 2);
+            const bool now = classes == 1 || (piece >= 0.7f * size ? rank == 0 : piece >= 0.3f * size ? rank == 1 : rank == 2);
             const uint32_t mine = now ? (uint32_t)tiles * ranges * heads : 0, upto = before + wave_upto(mine);
             const uint64_t done = __builtin_amdgcn_ballot_w64(upto <= id);
             if (done != ~(uint64_t)0) {
@@ -1060,7 +1067,7 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     // slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
     const int64_t rounds = s.B > 1 || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
     const int64_t enough = s.B > 1 ? 4 * (int64_t)p.slots : s.count > 0 ? p.slots / 2 + 1 : 2 * (int64_t)p.slots;
-    p.split = tiles < enough && s.B <= 1024 && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
+    p.split = tiles < enough && s.B <= kMostCut && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
     p.groups = !p.split ? blocks * p.tiles * s.heads : s.B > 1 ? tiles + p.slots : std::max(tiles, rounds * p.slots);
     p.ws_bytes = p.split ? (p.groups * p.tile_rows * (int64_t)(s.D + 1) + 2 * (int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
     return p;

@@ -8,7 +8,7 @@ from oracle import dit as odit
 from oracle import paged as opaged
 from paged_cases import Case
 from paper_2607_28144_amd import synth
-from test_gpu_paged import bf16, check, held, host, ints, paged
+from test_gpu_paged import bf16, check, held, host, ints, paged, plan
 
 pytestmark = pytest.mark.gpu
 
@@ -181,9 +181,21 @@ def test_offsets_past_32_bits(rows):
 
 
 def test_more_sequences_than_a_plan_goes_over():
-    """Beyond 1024 sequences keys are not cut; lengths of 0 to 300, every third sequence without new tokens."""
+    """Beyond 256 sequences keys are not cut; lengths of 0 to 300, every third sequence without new tokens."""
     B = 1100
     rows = [0 if b % 3 == 2 else 1 + b % 2 for b in range(B)]
     c = Case(rows, [(7 * b) % 300 for b in range(B)], 1, 1, 64, 16, seed=6)
     o, lse = paged().attn_fwd(bf16(c.q), *held(c), out_dtype=torch.float32)
     check("1100 sequences", o, lse, c, True, f32=True)
+
+
+@pytest.mark.parametrize("B", [65, 200, 256])
+def test_sequences_beyond_64(B):
+    """More sequences than a wave has lanes, whose keys may be cut: one long one among short ones, some without rows."""
+    rows = [0 if b % 7 == 3 else 1 + b % 3 for b in range(B)]
+    lens = [4000 if b == B - 2 else 3 + (11 * b) % 200 for b in range(B)]
+    c = Case(rows, lens, 2, 1, 64, 64, seed=B)
+    assert plan(c).split == 1
+    for causal in (True, False):
+        o, lse = paged().attn_fwd(bf16(c.q), *held(c), causal=causal, out_dtype=torch.float32)
+        check(f"{B} sequences", o, lse, c, causal, f32=True)
