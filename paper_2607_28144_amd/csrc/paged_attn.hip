@@ -97,7 +97,7 @@ __device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, 
     const float size = fmaxf((float)p.least, all * (one ? 1.f : 1.25f) / p.slots);
     Piece k{0, 1, -1, 0, 0, 0, 0, 0};
     uint32_t before = 0;
-    // Of several, those with the longest pieces first, in three classes by their keys, so that none of them begins late.
+    // Of up to 64, those with the longest pieces first, in three classes by their keys, so that none of them begins late.
     // (Beyond 64, whose lengths are not all at hand, in their order.)
     const int classes = one || a.n.B > 64 ? 1 : 3;
     for (int rank = 0; rank < classes; ++rank)
@@ -246,8 +246,8 @@ __device__ __forceinline__ void rows_to_lds(uint32_t dst, const uint32_t (&at)[N
                          "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
                          "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
                          "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
-                         "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds"
-                         : : "s"(dst), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(r) : "m0", "memory");
+                         "buffer_load_dwordx4 %4, %5, 0 offen offset:%6 lds"
+                         : : "s"(dst), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(r), "n"(3 * 1024) : "m0", "memory");
     else
         __asm__ volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\t"
                          "buffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
