@@ -61,8 +61,11 @@ struct Work {
 // Sequences of a call differ in length, which only the device knows, and a long
 // one would be the last to end: where there are too few tiles to even that out (the
 // plan says so), every wave goes over the sequences, 64 at a time, adds up what there
-// is to do, and finds the one that workgroup `id` has a piece of.  One sequence's
-// keys are cut into as many ranges as fill the slots once; of several, at 5/4 of what
+// is to do, and finds the one that workgroup `id` has a piece of.  Of one sequence
+// the tiles that fill whole rounds of slots stay whole, and the keys of the rest are
+// cut into as many ranges as the last round has room for: 300 tiles of 64 rows and 4096
+// selected places on 256 slots 82 us, all whole 109; 270 of 256 rows and 21840 places
+// (D = 64) 462 and 825.  Those of several are cut at 5/4 of what
 // a slot has on the average, those with the longest pieces first.  Seven chunks of 1
 // to 1365 tokens behind 0 to 10663 others, 20 heads on 4: 83 us so; cut at 1 or 1.5
 // of the average 87 and 91, in the order of the call 96, cut by a bound that the host
@@ -103,21 +106,30 @@ __device__ __forceinline__ Piece piece_of(const AttnArgs &a, const AttnPlan &p, 
     for (int rank = 0; rank < classes; ++rank)
         for (int c = 0; c < a.n.B; c += 64) {
             if (a.n.B > 64) look(c);
-            // of one sequence, as many as there are workgroups for; of several, the mean of a row: there are enough
-            const int most = one ? (int)(p.groups / max(1, tiles * heads)) : kMostRanges;
-            const int ranges = max(1, min(min(kMostRanges, most), (int)(one ? floorf(keys / size) : ceilf(mean / size))));
+            int skip = 0, most = kMostRanges;
+            float longest = size;
+            if (one) {  // lane 0: the whole tiles, lane 1: those that are cut
+                const uint32_t n = (uint32_t)__builtin_amdgcn_readfirstlane(tiles), rounds = n * heads / (uint32_t)p.fill;
+                const uint32_t whole = rounds * p.fill / heads, rest = n - whole;
+                most = lane == 0 ? 1 : (int)(((rounds + 1) * p.fill / heads - whole) / max(1u, rest));
+                tiles = lane == 0 ? whole : lane == 1 ? rest : 0;
+                skip = lane == 0 ? rest : 0;
+                if (rounds > 0) longest = (float)p.least;
+            }
+            // of several, the mean of a row: there are workgroups enough
+            const int ranges = max(1, min(min(kMostRanges, most), (int)(one ? floorf(keys / longest) : ceilf(mean / size))));
             const float piece = mean / ranges;
             const bool now = classes == 1 || (piece >= 0.7f * size ? rank == 0 : piece >= 0.3f * size ? rank == 1 : rank == 2);
             const uint32_t mine = now ? (uint32_t)tiles * ranges * heads : 0, upto = before + wave_upto(mine);
             const uint64_t done = __builtin_amdgcn_ballot_w64(upto <= id);
             if (done != ~(uint64_t)0) {
                 const int at = __popcll(done);  // upto ascends
-                k.b = c + at;
+                k.b = one ? 0 : c + at;
                 k.ranges = __builtin_amdgcn_readlane(ranges, at);
                 const uint32_t rest = id - (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at);
                 const uint32_t per = (uint32_t)k.ranges * heads;
                 const uint32_t t = rest / per, r2 = rest - t * per;
-                k.tile = __builtin_amdgcn_readlane(tiles, at) - 1 - (int)t;  // the last first: in a causal call it has the most keys
+                k.tile = __builtin_amdgcn_readlane(tiles + skip, at) - 1 - (int)t;  // the last first: in a causal call it has the most keys
                 k.range = (int)(r2 / (uint32_t)heads);
                 k.hk = (int)r2 - k.range * heads;
                 k.first = __builtin_amdgcn_readlane(first, at);
@@ -1060,15 +1072,24 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     // workgroups that run at once: two of 32 rows of 64 channels to a compute unit, or one of any other
     p.slots = n_cu * (p.tile_rows == 32 && s.D == 64 ? 2 : 1);
     p.least = p.tile_rows == kManyRows ? 512 : 256;
-    const int64_t blocks = (int64_t)s.T / p.block + s.B, tiles = std::min<int64_t>(blocks, s.T) * p.tiles * s.heads;
+    const int64_t blocks = (int64_t)s.T / p.block + s.B, most_blocks = s.B == 1 ? (s.T + (int64_t)p.block - 1) / p.block : blocks;
+    const int64_t tiles = std::min<int64_t>(most_blocks, s.T) * p.tiles * s.heads;
     const int64_t keys = s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len;
     // Keys are cut where there are too few tiles for their number to even out the differences; a cut tile has at least two
-    // ranges of `least` keys.  Workgroups: piece_of makes at most one to a tile and one to a slot; of one sequence one to a
-    // slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
-    const int64_t rounds = s.B > 1 || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
+    // ranges of `least` keys.  Workgroups: piece_of makes at most one to a tile and one to a slot; of one sequence whole
+    // rounds (`fill`) of one to a slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
+    const int64_t rounds = s.B > 1 || s.count > 0 || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
     const int64_t enough = s.B > 1 ? 4 * (int64_t)p.slots : s.count > 0 ? p.slots / 2 + 1 : 2 * (int64_t)p.slots;
-    p.split = tiles < enough && s.B <= kMostCut && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
-    p.groups = !p.split ? blocks * p.tiles * s.heads : s.B > 1 ? tiles + p.slots : std::max(tiles, rounds * p.slots);
+    p.fill = (int)rounds * p.slots;
+    const int64_t full = s.B == 1 ? tiles / p.fill : 0, rest = tiles - full * p.fill / s.heads * s.heads;
+    // Behind whole rounds the join has to be worth a round's saving: 516 tiles of 64 rows 129 and 132 us at 1024 places to a
+    // tile, 272 and 251 at 4096; 324 of them 52 and 49 at 1024.  Up to four, as partial results of all are in the workspace.
+    if (full == 0)
+        p.split = tiles < enough && s.B <= kMostCut && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
+    else
+        p.split = rounds == 1 && full <= 4 && rest > 0 && ((full + 1) * p.fill / s.heads - (tiles - rest) / s.heads) / (rest / s.heads) >= 2 &&
+                  keys >= 4 * full * p.least;
+    p.groups = !p.split ? blocks * p.tiles * s.heads : s.B > 1 ? tiles + p.slots : (full + 1) * p.fill;
     p.ws_bytes = p.split ? (p.groups * p.tile_rows * (int64_t)(s.D + 1) + 2 * (int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
     return p;
 }

@@ -50,7 +50,7 @@ struct AttnShape {
 // (more than one where a query block is larger than a tile).  split: the keys of a tile may be cut into ranges, which the
 // device decides by the sequences' lengths; `slots` workgroups run at once, a range has `least` keys or more.
 struct AttnPlan {
-    int32_t tile_rows, block, tiles, split, slots, least;
+    int32_t tile_rows, block, tiles, split, slots, least, fill;
     int64_t groups, ws_bytes;
 };
 AttnPlan attn_plan(const AttnShape &s, int n_cu);

@@ -1,6 +1,8 @@
 """The operators of the paged cache together, as a program that streams uses them:
 append, choice of pages and attention, step after step, eager and captured, on
 streams of their own; long offsets and many sequences."""
+import copy
+
 import numpy as np
 import pytest
 
@@ -199,3 +201,43 @@ def test_sequences_beyond_64(B):
     for causal in (True, False):
         o, lse = paged().attn_fwd(bf16(c.q), *held(c), causal=causal, out_dtype=torch.float32)
         check(f"{B} sequences", o, lse, c, causal, f32=True)
+
+
+def some_heads(c, heads):
+    """The case of these key heads alone, for as many query heads."""
+    d = copy.copy(c)
+    d.q, d.k, d.v, d.H, d.heads = c.q[:, heads], c.k[:, heads], c.v[:, heads], len(heads), len(heads)
+    return d
+
+
+@pytest.mark.parametrize("lead,tail,lens", [(0, 0, 1300), (3, 9, 1300), (120, 0, 1290), (0, 30, 170)])
+def test_one_sequence_of_more_tiles_than_compute_units(lead, tail, lens):
+    """Whole tiles for one round of workgroups and ranges of the others' keys, with rows of no sequence and few places."""
+    rows, count, page, heads = 168 - lead - tail, 64, 16, [0, 9, 17, 25]
+    c = Case([rows], [lens], 26, 26, 64, page, seed=lead + tail, lead=lead, tail=tail)
+    c.table = np.pad(c.table, ((0, 0), (0, 83 - c.table.shape[1])), constant_values=-1)
+    p = plan(c, 16, count, max_len=1300)
+    assert p.split == 1 and p.tile_rows == 16
+    blocks = c.T // 16 + 1
+    lists = np.sort(np.argsort(np.random.default_rng(lens).random((blocks, 26, 82)))[:, :, :count]).astype(np.int32)
+    lists[::3, :, 50:] = -1
+    o = torch.full((c.T, 26, 64), 7.0, device="cuda")
+    lse = torch.full((26, c.T), 7.0, device="cuda")
+    for causal in (True, False):
+        paged().attn_pages_fwd(bf16(c.q), *held(c), ints(lists), 16, causal=causal, max_len=1300, out_dtype=torch.float32,
+                               out=o, lse_out=lse)
+        check(f"round and rest {lead} {tail}", o[:, heads], lse[heads], some_heads(c, heads), causal, selected=lists[:, heads],
+              q_block=16, f32=True)
+        assert bool((o[:lead] == 7).all()) and bool((o[c.T - tail:] == 7).all())
+        assert bool((lse[:, :lead] == 7).all()) and bool((lse[:, c.T - tail:] == 7).all())
+
+
+@pytest.mark.parametrize("rows", [257, 320, 200])
+def test_one_sequence_of_more_large_tiles_than_compute_units(rows):
+    """The same of 256 rows: planned for 320 tokens of 130 heads."""
+    heads = [0, 1, 64, 129]
+    c = Case([rows], [2100], 130, 130, 64, 64, seed=rows, tail=320 - rows)
+    assert plan(c).split == 1 and plan(c).tile_rows == 256
+    for causal in (True, False):
+        o, lse = paged().attn_fwd(bf16(c.q), *held(c), causal=causal, out_dtype=torch.float32)
+        check(f"large round and rest {rows}", o[:, heads], lse[heads], some_heads(c, heads), causal, f32=True)
