@@ -110,9 +110,10 @@ regenvc_status regenvc_paged_attn_fwd(const regenvc_tensor *q, const regenvc_pag
                                       const regenvc_tensor *o, regenvc_dtype o_dtype, float *lse, int32_t H,
                                       float softmax_scale, void *workspace, int64_t workspace_bytes, void *stream);
 
-/* The shape of such a call, for its plan.  selected: count, or 0 without. */
+/* The shape of such a call, for its plan.  selected: count, or 0 without; causal
+   as in the call. */
 typedef struct {
-    int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len;
+    int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len, causal;
 } regenvc_paged_attn_shape;
 
 /* Workspace bytes of such a call on n_cu compute units.  Host-only. */

@@ -78,7 +78,7 @@ class RotaryTable(ctypes.Structure):
 class PagedAttnShape(ctypes.Structure):
     """regenvc_paged_attn_shape: what the plan of an attention call over pages goes by."""
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "H", "heads", "D", "page", "q_block", "count", "max_rows",
-                                              "max_len")]
+                                              "max_len", "causal")]
 
 
 class PagedAttnPlan(ctypes.Structure):

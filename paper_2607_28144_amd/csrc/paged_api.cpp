@@ -174,7 +174,7 @@ bool empty(const regenvc_paged_attn_shape &s)
 // The plan of a shape that check_shape accepts and that is not empty.
 regenvc_status plan_of(const char *fn, const regenvc_paged_attn_shape &s, int n_cu, paged::AttnPlan *p)
 {
-    *p = paged::attn_plan({s.B, s.T, s.H, s.heads, s.D, s.page, s.q_block, s.count, s.max_rows, s.max_len}, n_cu);
+    *p = paged::attn_plan({s.B, s.T, s.H, s.heads, s.D, s.page, s.q_block, s.count, s.max_rows, s.max_len, s.causal}, n_cu);
     if (p->groups > kMaxGroups || p->groups * p->tile_rows > INT32_MAX)  // rows of partial results are counted in 32 bits
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: more than %lld workgroups", fn, (long long)kMaxGroups);
     return REGENVC_OK;
@@ -341,7 +341,7 @@ regenvc_status regenvc_paged_attn_fwd(const regenvc_tensor *q, const regenvc_pag
     if (st == REGENVC_OK && selected != nullptr) st = check_block(fn, q_block, count);
     if (st != REGENVC_OK) return st;
     const regenvc_paged_attn_shape s{batch->B,   batch->T, H,       pool->heads, pool->D, pool->page, q_block,
-                                     selected != nullptr ? count : 0, max_rows, max_len};
+                                     selected != nullptr ? count : 0, max_rows, max_len, causal};
     if ((st = check_shape(fn, &s)) != REGENVC_OK) return st;
     if ((st = regenvc::abi::softmax_scale_ok(softmax_scale)) != REGENVC_OK) return st;
     if (o_dtype != REGENVC_BF16 && o_dtype != REGENVC_F32) return failf(REGENVC_ERR_INVALID_ARG, "%s: dtype %d", fn, o_dtype);

@@ -1075,20 +1075,20 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     const int64_t blocks = (int64_t)s.T / p.block + s.B, most_blocks = s.B == 1 ? (s.T + (int64_t)p.block - 1) / p.block : blocks;
     const int64_t tiles = std::min<int64_t>(most_blocks, s.T) * p.tiles * s.heads;
     const int64_t keys = s.count > 0 ? std::min<int64_t>(s.max_len, (int64_t)s.count * s.page) : s.max_len;
-    // Keys are cut where there are too few tiles for their number to even out the differences; a cut tile has at least two
-    // ranges of `least` keys.  Workgroups: piece_of makes at most one to a tile and one to a slot; of one sequence whole
-    // rounds (`fill`) of one to a slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
-    const int64_t rounds = s.B > 1 || s.count > 0 || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
-    const int64_t enough = s.B > 1 ? 4 * (int64_t)p.slots : s.count > 0 ? p.slots / 2 + 1 : 2 * (int64_t)p.slots;
+    // Keys are cut where there are too few tiles for their number to even out the differences, at least into two ranges of
+    // `least` keys.  Workgroups: piece_of makes at most one to a tile and one to a slot; of one sequence whole rounds (`fill`)
+    // of one to a slot, or two where its tiles may differ much, as those of many rows of a short causal one do.
+    const int64_t rounds = s.B > 1 || s.count > 0 || !s.causal || 4 * (int64_t)s.max_rows <= s.max_len ? 1 : 2;
     p.fill = (int)rounds * p.slots;
-    const int64_t full = s.B == 1 ? tiles / p.fill : 0, rest = tiles - full * p.fill / s.heads * s.heads;
+    const int64_t n = tiles / s.heads, full = s.B == 1 ? tiles / p.fill : 0, whole = full * p.fill / s.heads;
+    const bool room = s.B == 1 ? n > whole && ((full + 1) * p.fill / s.heads - whole) / (n - whole) >= 2
+                               : tiles < 4 * (int64_t)p.slots && s.B <= kMostCut;
     // Behind whole rounds the join has to be worth a round's saving: 516 tiles of 64 rows 129 and 132 us at 1024 places to a
     // tile, 272 and 251 at 4096; 324 of them 52 and 49 at 1024.  Up to four, as partial results of all are in the workspace.
     if (full == 0)
-        p.split = tiles < enough && s.B <= kMostCut && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
+        p.split = room && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
     else
-        p.split = rounds == 1 && full <= 4 && rest > 0 && ((full + 1) * p.fill / s.heads - (tiles - rest) / s.heads) / (rest / s.heads) >= 2 &&
-                  keys >= 4 * full * p.least;
+        p.split = room && rounds == 1 && full <= 4 && keys >= 4 * full * p.least;
     p.groups = !p.split ? blocks * p.tiles * s.heads : s.B > 1 ? tiles + p.slots : (full + 1) * p.fill;
     p.ws_bytes = p.split ? (p.groups * p.tile_rows * (int64_t)(s.D + 1) + 2 * (int64_t)s.T * s.H) * (int64_t)sizeof(float) : 0;
     return p;

@@ -44,11 +44,11 @@ constexpr int kMaxSelectColumns = 16384;  // a score of 64 bits each, in LDS
 hipError_t launch_select(const SelectArgs &a, int64_t blocks, int n_cu, hipStream_t stream);
 
 struct AttnShape {
-    int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len;  // count 0: every page
+    int32_t B, T, H, heads, D, page, q_block, count, max_rows, max_len, causal;  // count 0: every page
 };
 // Tiles of rows (queries times the heads that share a key head), `block` queries each and `tiles` of them to a block
 // (more than one where a query block is larger than a tile).  split: the keys of a tile may be cut into ranges, which the
-// device decides by the sequences' lengths; `slots` workgroups run at once, a range has `least` keys or more.
+// device decides by the sequences' lengths; `slots` workgroups run at once, a range has `least` keys or more.  Of one sequence: a round has `fill` pieces.
 struct AttnPlan {
     int32_t tile_rows, block, tiles, split, slots, least, fill;
     int64_t groups, ws_bytes;

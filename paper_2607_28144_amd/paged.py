@@ -227,7 +227,7 @@ def _attn(q, cache, table, first, lens, chosen, q_block, causal, scale, max_rows
     places = n.columns * cache.page if max_len is None else int(max_len)
     if H >= 1 << 31 or not 0 <= rows < 1 << 31 or not 0 <= places < 1 << 31:
         _lib.int32(H=H, max_rows=rows, max_len=places)
-    need = _need((n.B, T, H, cache.heads, D, cache.page, q_block, count, rows, places), idx)
+    need = _need((n.B, T, H, cache.heads, D, cache.page, q_block, count, rows, places, int(causal)), idx)
     with _lib.on_device(idx):
         ws = torch.empty(need, dtype=torch.uint8, device=cache.device) if need > 0 else None
         st = _lib.load().regenvc_paged_attn_fwd(

@@ -241,3 +241,14 @@ def test_one_sequence_of_more_large_tiles_than_compute_units(rows):
     for causal in (True, False):
         o, lse = paged().attn_fwd(bf16(c.q), *held(c), causal=causal, out_dtype=torch.float32)
         check(f"large round and rest {rows}", o[:, heads], lse[heads], some_heads(c, heads), causal, f32=True)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_whole_window_of_more_large_tiles_than_compute_units(causal):
+    """600 of 2100 places are new: a causal call keeps its tiles whole, one that sees them all does not."""
+    heads = [0, 3, 89]
+    c = Case([600], [2100], 90, 90, 64, 64, seed=9)
+    need = paged()._need((1, 600, 90, 90, 64, 64, 1, 0, 600, c.table.shape[1] * 64, int(causal)), 0)
+    assert (need > 0) == (not causal)
+    o, lse = paged().attn_fwd(bf16(c.q), *held(c), causal=causal, out_dtype=torch.float32)
+    check(f"window causal={causal}", o[:, heads], lse[heads], some_heads(c, heads), causal, f32=True)
