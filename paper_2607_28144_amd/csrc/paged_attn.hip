@@ -401,9 +401,10 @@ __device__ __forceinline__ void redo_row(const AttnArgs &a, const AttnPlan &p, c
 // heads of 64 on 4 (75 MB): 16.4 + 3.9.  16 pages of 64 for one query: 10.9 + 3.9,
 // of which a chain of eight dependent loads has most (sequence, list, table, keys).
 // 64 rows: 25 blocks of 64 queries x 12 heads with 64 pages of 64 each (629 MB from
-// the caches, 321 from HBM): 111 us, two rounds of workgroups, each at the rate of
-// what lies behind the L2 (9.8 TB/s); the next tile's scores beside a tile's weights
-// (142 us instead of 135, with the selection) or keys in three ranges (149) lose.
+// the caches, 321 from HBM): 86 us and 5 for the join, 252 tiles whole and 48 in five
+// ranges each, at the rate of what lies behind the L2; all whole it took 111.  The
+// next tile's scores beside a tile's weights (142 us instead of 135, with the
+// selection) or every tile's keys in three ranges (149) lose.
 constexpr int few_waves(int rows) { return rows == 16 ? 8 : 4; }
 
 template <int D, int MB, bool SPARSE>
@@ -1064,7 +1065,7 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     const int64_t most = queries * G, mean = s.count > 0 ? most : std::min(most, (s.T + (int64_t)s.B - 1) / s.B * G);
     p.tile_rows = most <= 16 || mean <= 16 ? 16 : most <= 32 || mean <= 32 ? 32 : most <= 64 || mean <= 64 ? 64 : kManyRows;
     // Up to 64 rows in two tiles while those leave compute units free: 64 rows of 12 heads against 10920 places 29 us, in one
-    // 34; 25 blocks of 64 queries of 12 heads, 64 pages of 64 each, in one 117 us, in two 236.
+    // 34; 25 blocks of 64 queries of 12 heads, 64 pages of 64 each, in one 117 us, in two 236 (all tiles whole).
     const int64_t sequences = s.count > 0 ? (int64_t)s.T / s.q_block + s.B : s.B;
     if (p.tile_rows == 64 && 2 * sequences * s.heads <= n_cu) p.tile_rows = 32;
     p.block = s.count > 0 ? s.q_block : (int)std::max<int64_t>(1, p.tile_rows / G);
