@@ -220,7 +220,8 @@ def _attn(q, cache, table, first, lens, chosen, q_block, causal, scale, max_rows
     if chosen is not None:
         count = chosen.shape[2] if chosen.dim() == 3 else 0
         _lib.int32(q_block=q_block, count=count)
-        if q_block < 1 or tuple(chosen.shape) != (T // q_block + n.B, cache.heads, count):
+        # (a list without entries has no address, which the call reads as every page)
+        if q_block < 1 or count < 1 or tuple(chosen.shape) != (T // q_block + n.B, cache.heads, count):
             raise ValueError(f"selected must be [T // q_block + B, heads, count], got {tuple(chosen.shape)} for q_block={q_block}")
         sp = _lib.vector(chosen, "selected", torch.int32, chosen.numel(), idx)
     rows = T if max_rows is None else int(max_rows)
@@ -294,5 +295,7 @@ def attn_pages_fwd(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, firs
     `selected` (int32 [T // q_block + B, heads, count], as from select_pages)
     names for it and their key head: indices into the sequence's row of the table,
     -1 for none (regenvc_paged_attn_fwd)."""
+    if selected is None:
+        raise ValueError("selected is None (attn_fwd attends to every page)")
     return _attn(q, cache, table, first, lens, selected, q_block, causal, scale, max_rows, max_len, out_dtype, out, return_lse,
                  lse_out)
