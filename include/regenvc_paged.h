@@ -99,11 +99,11 @@ regenvc_status regenvc_paged_append(const regenvc_page_pool *pool, const regenvc
      max_rows, max_len: the most new tokens and places of a sequence that the
           work is planned for, 0 <= max_rows <= T, 0 <= max_len <= columns * page;
           longer ones are computed right, only less evenly
-   H T is at most 2^29, q_block in [1, 2^20], count in [1, 16384]; a call of more
-   than 2^24 - 1 workgroups (tiles of 16 rows or more, times key ranges) is refused.
-   workspace:
-   256-byte aligned, at least regenvc_paged_attn_workspace bytes (NULL if that
-   is 0). */
+   H T is at most 2^29, q_block in [1, 2^20], count in [1, 16384].  A call of more
+   workgroups (tiles, times key ranges) than one launch can have is refused: 2^23 -
+   1 of tiles of 16 or 256 rows, 2^24 - 1 of 32 or 64.
+   workspace: 256-byte aligned, at least regenvc_paged_attn_workspace bytes (NULL
+   if that is 0). */
 regenvc_status regenvc_paged_attn_fwd(const regenvc_tensor *q, const regenvc_page_pool *pool,
                                       const regenvc_page_batch *batch, const int32_t *selected, int32_t q_block,
                                       int32_t count, int32_t causal, int32_t max_rows, int32_t max_len,

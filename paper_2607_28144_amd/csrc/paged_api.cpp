@@ -23,7 +23,8 @@ namespace {
 constexpr int32_t kMaxB = 1 << 20, kMaxT = 1 << 26, kMaxPages = 1 << 30;
 constexpr int64_t kMaxPlaces = (int64_t)1 << 30;   // a tile past the last place stays within int32
 constexpr int32_t kMaxBlock = 1 << 20, kMaxCount = 16384;
-constexpr int64_t kMaxGroups = (1 << 24) - 1;      // of 256 threads: fewer than 2^32 in a launch
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;  // of a launch: its size has 32 bits
+constexpr int64_t kMaxBlocks = kMaxThreads / 256;        // of a choice of pages: so many threads to each of more than a few
 constexpr int64_t kMaxRows = (int64_t)1 << 29;
 
 regenvc_status done()
@@ -175,8 +176,9 @@ bool empty(const regenvc_paged_attn_shape &s)
 regenvc_status plan_of(const char *fn, const regenvc_paged_attn_shape &s, int n_cu, paged::AttnPlan *p)
 {
     *p = paged::attn_plan({s.B, s.T, s.H, s.heads, s.D, s.page, s.q_block, s.count, s.max_rows, s.max_len, s.causal}, n_cu);
-    if (p->groups > kMaxGroups || p->groups * p->tile_rows > INT32_MAX)  // rows of partial results are counted in 32 bits
-        return failf(REGENVC_ERR_UNSUPPORTED, "%s: more than %lld workgroups", fn, (long long)kMaxGroups);
+    const int64_t most = kMaxThreads / paged::attn_threads(p->tile_rows);
+    if (p->groups > most || p->groups * p->tile_rows > INT32_MAX)  // rows of partial results are counted in 32 bits
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: more than %lld workgroups", fn, (long long)most);
     return REGENVC_OK;
 }
 
@@ -274,9 +276,9 @@ regenvc_status regenvc_paged_select(const regenvc_tensor *q, const regenvc_page_
     if (keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > count)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: keep_first=%d keep_last=%d of count=%d", fn, keep_first, keep_last, count);
     const int64_t blocks = (int64_t)batch->T / q_block + batch->B;
-    if (batch->columns > paged::kMaxSelectColumns || blocks > kMaxGroups)
+    if (batch->columns > paged::kMaxSelectColumns || blocks > kMaxBlocks)
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: %d columns, %lld blocks (at most %d, %lld)", fn, batch->columns,
-                     (long long)blocks, paged::kMaxSelectColumns, (long long)kMaxGroups);
+                     (long long)blocks, paged::kMaxSelectColumns, (long long)kMaxBlocks);
     if (blocks == 0) return done();
     const bool any = batch->B > 0 && batch->T > 0 && H > 0;  // else every block is one without queries: -1
     if (any && pool->means == nullptr && pool->pages > 0)

@@ -405,7 +405,7 @@ __device__ __forceinline__ void redo_row(const AttnArgs &a, const AttnPlan &p, c
 // ranges each, at the rate of what lies behind the L2; all whole it took 111.  The
 // next tile's scores beside a tile's weights (142 us instead of 135, with the
 // selection) or every tile's keys in three ranges (149) lose.
-constexpr int few_waves(int rows) { return rows == 16 ? 8 : 4; }
+constexpr int few_waves(int rows) { return attn_threads(rows) / 64; }
 
 template <int D, int MB, bool SPARSE>
 __global__ __launch_bounds__(64 * few_waves(16 * MB)) __attribute__((amdgpu_waves_per_eu(MB == 1 ? 2 : 1)))
@@ -618,6 +618,7 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
 // busy for 51 % of the cycles, no LDS conflicts; 1560 queries against 32760 places:
 // 293-301 us in three ranges and 8 for their join; both at the power limit.
 constexpr int kManyWaves = 8, kManyRows = 32 * kManyWaves, kManyKeys = 64;
+static_assert(attn_threads(kManyRows) == 64 * kManyWaves, "what the plan counts on");
 
 template <int D, bool SPARSE>
 __global__ __launch_bounds__(64 * kManyWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -1031,12 +1032,12 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, AttnPlan
 template <int D, bool SPARSE>
 hipError_t launch_tiles(const AttnArgs &a, const AttnPlan &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)p.groups);
+    const dim3 grid((unsigned)p.groups), block((unsigned)attn_threads(p.tile_rows));
     switch (p.tile_rows) {
-    case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, dim3(64 * few_waves(16)), 0, stream, a, p); break;
-    case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, dim3(64 * few_waves(32)), 0, stream, a, p); break;
-    case 64: hipLaunchKernelGGL((attn_few_kernel<D, 4, SPARSE>), grid, dim3(64 * few_waves(64)), 0, stream, a, p); break;
-    case kManyRows: hipLaunchKernelGGL((attn_many_kernel<D, SPARSE>), grid, dim3(64 * kManyWaves), 0, stream, a, p); break;
+    case 16: hipLaunchKernelGGL((attn_few_kernel<D, 1, SPARSE>), grid, block, 0, stream, a, p); break;
+    case 32: hipLaunchKernelGGL((attn_few_kernel<D, 2, SPARSE>), grid, block, 0, stream, a, p); break;
+    case 64: hipLaunchKernelGGL((attn_few_kernel<D, 4, SPARSE>), grid, block, 0, stream, a, p); break;
+    case kManyRows: hipLaunchKernelGGL((attn_many_kernel<D, SPARSE>), grid, block, 0, stream, a, p); break;
     default: return hipErrorInvalidValue;
     }
     return hipGetLastError();

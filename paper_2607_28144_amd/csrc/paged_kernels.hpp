@@ -54,6 +54,8 @@ struct AttnPlan {
     int64_t groups, ws_bytes;
 };
 AttnPlan attn_plan(const AttnShape &s, int n_cu);
+// Threads of a workgroup with a tile of 16, 32, 64 or 256 rows.
+constexpr int attn_threads(int tile_rows) { return tile_rows == 32 || tile_rows == 64 ? 256 : 512; }
 
 // selected null: every page.  o: bf16 or f32; lse: f32 [H, T] or null; ws: the partial results of key ranges.
 struct AttnArgs {

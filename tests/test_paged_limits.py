@@ -20,3 +20,30 @@ def test_attention_to_an_empty_list_of_pages(host):  # noqa: F811
         with pytest.raises(ValueError, match="selected"):
             paged.attn_pages_fwd(bf(3, 4, 64), c, selected=selected, q_block=2, **seqs)
     assert host.seen == []
+
+
+def plan(**kw):
+    """Status, tile rows and workgroups of the plan of a shape on 256 compute units."""
+    a = dict(dict(B=1, T=1, H=1, heads=1, D=128, page=64, q_block=1, count=0, max_rows=1, max_len=64, causal=1), **kw)
+    p, n = _lib.PagedAttnPlan(), ctypes.c_int64()
+    lib = _lib.load()
+    st = lib.regenvc_paged_attn_plan_query(ref(_lib.PagedAttnShape(*a.values())), 256, ref(p))
+    assert st == lib.regenvc_paged_attn_workspace(ref(_lib.PagedAttnShape(*a.values())), 256, ref(n))
+    return st, p.tile_rows, p.workgroups
+
+
+# Calls just within what one launch can have (fewer than 2^32 threads), and just beyond: tile rows, threads, shape, what changes
+LAUNCHES = [(16, 512, dict(H=8, heads=8, count=16), dict(T=(1 << 20) - 2), dict(T=(1 << 20) - 1)),
+            (16, 512, dict(B=1 << 20, T=1 << 20), dict(H=7, heads=7), dict(H=8, heads=8)),
+            (32, 256, dict(H=32, heads=2, q_block=2, count=16, max_rows=2), dict(T=(1 << 24) - 4), dict(T=(1 << 24) - 2)),
+            (64, 256, dict(B=1 << 20, T=64, q_block=64, count=16, max_rows=64), dict(H=15, heads=15), dict(H=16, heads=16)),
+            (256, 512, dict(B=1 << 20, T=300, q_block=300, count=16, max_rows=300), dict(H=3, heads=3), dict(H=4, heads=4))]
+
+
+@pytest.mark.parametrize("rows,threads,shape,within,beyond", LAUNCHES)
+def test_workgroups_of_one_launch(rows, threads, shape, within, beyond):
+    st, tile, groups = plan(**shape, **within)
+    assert st == _lib.OK and tile == rows and groups * threads < 1 << 32
+    st, _, _ = plan(**shape, **beyond)
+    assert st == _lib.ERR_UNSUPPORTED
+    assert "workgroups" in _lib.load().regenvc_last_error().decode()
