@@ -140,7 +140,8 @@ regenvc_status regenvc_paged_attn_plan_query(const regenvc_paged_attn_shape *sha
           first[b] / q_block + b + i; pages ascending, then -1; every entry is
           written, blocks without queries (with H = 0: all) with -1
    keep_first, keep_last >= 0, their sum at most count; count in [1, 16384],
-   columns at most 16384, q_block in [1, 2^20], T / q_block + B below 2^24. */
+   columns at most 16384, q_block in [1, 2^20], T / q_block + B below 2^24, H T at
+   most 2^29. */
 regenvc_status regenvc_paged_select(const regenvc_tensor *q, const regenvc_page_pool *pool,
                                     const regenvc_page_batch *batch, int32_t H, int32_t q_block, int32_t count,
                                     int32_t keep_first, int32_t keep_last, int32_t causal, int32_t *selected,

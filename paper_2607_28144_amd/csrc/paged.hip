@@ -391,7 +391,7 @@ __global__ __launch_bounds__(THREADS) void select_kernel(SelectArgs a)
     lookup(0, at);
     {
         double s[8] = {};
-        const int rows = k.rows * G;  // at most H T
+        const int rows = k.rows * G;  // at most H T, which is at most 2^29
         for (int r = r0; r < rows; r += 4 * RPP) {
             u32x4 y[4];
 #pragma unroll

@@ -25,7 +25,7 @@ constexpr int64_t kMaxPlaces = (int64_t)1 << 30;   // a tile past the last place
 constexpr int32_t kMaxBlock = 1 << 20, kMaxCount = 16384;
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;  // of a launch: its size has 32 bits
 constexpr int64_t kMaxBlocks = kMaxThreads / 256;        // of a choice of pages: so many threads to each of more than a few
-constexpr int64_t kMaxRows = (int64_t)1 << 29;
+constexpr int64_t kMaxRows = (int64_t)1 << 29;  // of query heads: the kernels count a tile's and a block's in 32 bits
 
 regenvc_status done()
 {
@@ -96,6 +96,13 @@ regenvc_status check_heads(const char *fn, int32_t H, int32_t heads)
     return REGENVC_OK;
 }
 
+regenvc_status check_rows(const char *fn, int32_t H, int32_t T)
+{
+    if ((int64_t)H * T > kMaxRows)
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: %lld rows, at most 2^29", fn, (long long)((int64_t)H * T));
+    return REGENVC_OK;
+}
+
 regenvc_status check_block(const char *fn, int32_t q_block, int32_t count)
 {
     if (q_block < 1 || q_block > kMaxBlock || count < 1 || count > kMaxCount)
@@ -162,9 +169,7 @@ regenvc_status check_shape(const char *fn, const regenvc_paged_attn_shape *s)
     if (s->max_rows > s->T)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: max_rows=%d of T=%d rows", fn, s->max_rows, s->T);
     if (s->count != 0 && (st = check_block(fn, s->q_block, s->count)) != REGENVC_OK) return st;
-    if ((int64_t)s->H * s->T > kMaxRows)
-        return failf(REGENVC_ERR_UNSUPPORTED, "%s: %lld rows, at most 2^29", fn, (long long)((int64_t)s->H * s->T));
-    return REGENVC_OK;
+    return check_rows(fn, s->H, s->T);
 }
 
 bool empty(const regenvc_paged_attn_shape &s)
@@ -271,6 +276,7 @@ regenvc_status regenvc_paged_select(const regenvc_tensor *q, const regenvc_page_
     regenvc_status st = check_pool(fn, pool, r.pool);
     if (st == REGENVC_OK) st = check_batch(fn, batch, pool->page, r.batch);
     if (st == REGENVC_OK) st = check_heads(fn, H, pool->heads);
+    if (st == REGENVC_OK) st = check_rows(fn, H, batch->T);
     if (st == REGENVC_OK) st = check_block(fn, q_block, count);
     if (st != REGENVC_OK) return st;
     if (keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > count)

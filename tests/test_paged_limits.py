@@ -47,3 +47,22 @@ def test_workgroups_of_one_launch(rows, threads, shape, within, beyond):
     st, _, _ = plan(**shape, **beyond)
     assert st == _lib.ERR_UNSUPPORTED
     assert "workgroups" in _lib.load().regenvc_last_error().decode()
+
+
+A = 0x10000000  # 256-byte aligned, never dereferenced
+K, V, M, Q, TAB, FIRST, LENS, SEL = (A + (i << 44) for i in range(8))
+
+
+def select(H, T, heads=1, q_block=1, pages=10, page=16, stride=0):
+    pool = _lib.PagePool(K, V, M, pages, page, heads, 64)
+    batch = _lib.PageBatch(TAB, FIRST, LENS, 5, 1, 5, T)
+    q = _lib.Tensor(Q, 0, stride, stride)
+    return _lib.load().regenvc_paged_select(ref(q), ref(pool), ref(batch), H, q_block, 2, 1, 1, 1, SEL, None)
+
+
+@pytest.mark.parametrize("H,T,q_block", [(2048, 1 << 20, 1 << 20), (4096, 1 << 19, 1 << 19), (1 << 20, 1 << 10, 1 << 10),
+                                         (513, 1 << 20, 1), (16, (1 << 26) - 1, 1 << 20)])
+def test_choice_of_more_rows_than_32_bits_count(H, T, q_block):
+    """A block's rows (queries times the heads that share a key head) are counted in 32 bits: H T is held to 2^29."""
+    assert select(H, T, q_block=q_block) == _lib.ERR_UNSUPPORTED
+    assert "rows, at most" in _lib.load().regenvc_last_error().decode()
