@@ -29,7 +29,7 @@ extern "C" {
 
 /* A pool of `pages` pages of `page` places for `heads` key heads, in caller
    memory, contiguous, 16-byte aligned.  D in {64, 128}; page a power of two, 16
-   to 1024; pages below 2^30; heads at most 65535. */
+   to 1024; pages below 2^30; heads at most 65535; k and v of at most 2^47 bytes each. */
 typedef struct {
     void *k, *v;  /* bf16 [pages, heads, page, D] */
     void *means;  /* bf16 [pages, heads, D]: each page's mean key; or NULL */

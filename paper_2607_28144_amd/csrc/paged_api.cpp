@@ -21,6 +21,7 @@ namespace paged = regenvc::paged;
 namespace {
 
 constexpr int32_t kMaxB = 1 << 20, kMaxT = 1 << 26, kMaxPages = 1 << 30;
+constexpr int64_t kMaxPoolBytes = (int64_t)1 << 47;  // all that a process can address
 constexpr int64_t kMaxPlaces = (int64_t)1 << 30;   // a tile past the last place stays within int32
 constexpr int32_t kMaxBlock = 1 << 20, kMaxCount = 16384;
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;  // of a launch: its size has 32 bits
@@ -59,7 +60,9 @@ regenvc_status check_pool(const char *fn, const regenvc_page_pool *p, Range (&r)
         return failf(REGENVC_ERR_INVALID_ARG, "%s: a NULL pool pointer", fn);
     if (!aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->means, 16))
         return failf(REGENVC_ERR_UNSUPPORTED, "%s: the pool must be 16-byte aligned", fn);
-    const int64_t rows = (int64_t)p->pages * p->heads;  // below 2^46, with 2^18 bytes each
+    const int64_t rows = (int64_t)p->pages * p->heads;  // below 2^46, with up to 2^18 bytes each
+    if (rows > kMaxPoolBytes / (p->page * p->D * 2))
+        return failf(REGENVC_ERR_UNSUPPORTED, "%s: keys of more than 2^47 bytes", fn);
     r[0] = range_of(p->k, rows * p->page * p->D * 2);
     r[1] = range_of(p->v, rows * p->page * p->D * 2);
     r[2] = range_of(p->means, p->means != nullptr ? rows * p->D * 2 : 0);

@@ -66,3 +66,11 @@ def test_choice_of_more_rows_than_32_bits_count(H, T, q_block):
     """A block's rows (queries times the heads that share a key head) are counted in 32 bits: H T is held to 2^29."""
     assert select(H, T, q_block=q_block) == _lib.ERR_UNSUPPORTED
     assert "rows, at most" in _lib.load().regenvc_last_error().decode()
+
+
+@pytest.mark.parametrize("pages,heads,page", [((1 << 30) - 1, 65535, 1024), ((1 << 30) - 1, 128, 16), (1 << 26, 65535, 64),
+                                              (1 << 20, 65535, 1024)])
+def test_pool_of_more_bytes_than_there_are_addresses(pages, heads, page):
+    """Its extent, which the checks of overlaps go by, would wrap."""
+    assert select(heads, 3, heads, pages=pages, page=page, stride=64) == _lib.ERR_UNSUPPORTED
+    assert "bytes" in _lib.load().regenvc_last_error().decode()
