@@ -19,6 +19,11 @@ __device__ __forceinline__ uint32_t pack(float a, float b)
     const bf16x2 v = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, v);
 }
+// Rounded once: through an f32 in between, a number next to the middle of two bf16 could go the wrong way.
+__device__ __forceinline__ uint16_t bf16_of(double x)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
 __device__ __forceinline__ u32x4 load16(const uint16_t *p)
 {
     return *reinterpret_cast<const u32x4 *>(p);
@@ -226,7 +231,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void a
             for (int e = 0; e < 8; ++e) sum[e] += part[pair][lane][e];
             u32x4 o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = pack((float)(sum[2 * e] / n), (float)(sum[2 * e + 1] / n));
+            for (int e = 0; e < 4; ++e) o[e] = bf16_of(sum[2 * e] / n) | (uint32_t)bf16_of(sum[2 * e + 1] / n) << 16;
             *reinterpret_cast<u32x4 *>(a.c.means + (page0 + hk) * D + d0) = o;
         }
         __syncthreads();
@@ -267,8 +272,7 @@ __global__ __launch_bounds__(256) void means_kernel(AppendArgs a)
     double sum = 0;
 #pragma unroll
     for (int r = 0; r < RPP; ++r) sum += part[r][threadIdx.x];
-    const __bf16 m = (__bf16)(float)(sum / rows);
-    a.c.means[((int64_t)page * a.c.heads + hk) * D + threadIdx.x] = __builtin_bit_cast(uint16_t, m);
+    a.c.means[((int64_t)page * a.c.heads + hk) * D + threadIdx.x] = bf16_of(sum / rows);
 }
 
 // ---------------------------------------------------------------- selection
