@@ -87,8 +87,10 @@ regenvc_status regenvc_paged_append(const regenvc_page_pool *pool, const regenvc
    softmax weight is rounded to bf16 before it multiplies a value, whatever
    o_dtype is; O is normalized by the sum of the rounded weights, LSE takes them
    unrounded.  What lies in places that a query does not see is of no account to
-   it, infinities and NaN included.  A query that sees no place gives O = 0, LSE
-   = -inf.
+   it, infinities and NaN included (in the values of a causal call's own tokens they
+   cost time: up to 256 queries before such a token are done again, key by key, 100
+   times as long as the call or more).  A query that sees no place gives O = 0, LSE =
+   -inf.
      o:   [T, H, D] in o_dtype; lse: f32 [H, T] or NULL
      selected: NULL, or int32 [T / q_block + B, heads, count] as from
           regenvc_paged_select: queries first[b] + i q_block .. + q_block - 1 of
