@@ -74,3 +74,17 @@ def test_pool_of_more_bytes_than_there_are_addresses(pages, heads, page):
     """Its extent, which the checks of overlaps go by, would wrap."""
     assert select(heads, 3, heads, pages=pages, page=page, stride=64) == _lib.ERR_UNSUPPORTED
     assert "bytes" in _lib.load().regenvc_last_error().decode()
+
+
+def test_keys_are_cut_up_to_256_sequences():
+    """Single tokens against up to 4096 places: cut into ranges for up to 256 sequences, beyond them not."""
+    def split(**kw):
+        a = dict(dict(B=1, T=1, H=1, heads=1, D=64, page=64, q_block=1, count=0, max_rows=1, max_len=4096, causal=1), **kw)
+        p = _lib.PagedAttnPlan()
+        assert _lib.load().regenvc_paged_attn_plan_query(ref(_lib.PagedAttnShape(*a.values())), 256, ref(p)) == _lib.OK
+        return p.split
+    assert split(B=256, T=256) == 1 and split(B=257, T=257) == 0
+    # of one sequence a short causal call has two rounds of workgroups: its tiles differ in their keys
+    shape = dict(H=4, heads=4, page=64, T=600, max_rows=600, max_len=2112)
+    assert plan(**shape, causal=1)[1:] == (256, 512) and plan(**shape, causal=0)[1:] == (256, 256)
+    assert split(**dict(shape, causal=1)) == split(**dict(shape, causal=0)) == 1
