@@ -75,7 +75,8 @@ typedef struct {
      k, v:  bf16 [T, heads, D];  q_out: bf16 [T, H, D], may be q itself
             (stride_b of these tensors is not looked at)
      w_q, w_k: bf16 [D], 16-byte aligned, or NULL
-   The pages written must not be shared by sequences of the call. */
+   The pages written must be neither shared by sequences of the call nor named twice
+   by one. */
 regenvc_status regenvc_paged_append(const regenvc_page_pool *pool, const regenvc_page_batch *batch,
                                     const regenvc_tensor *q, const regenvc_tensor *k, const regenvc_tensor *v,
                                     const void *w_q, const void *w_k, float eps, const regenvc_rotary *rotary,
@@ -137,7 +138,12 @@ regenvc_status regenvc_paged_attn_plan_query(const regenvc_paged_attn_shape *sha
      sum over the block's queries and the key head's query heads of q, dot the
      page's mean key (pool->means)
    (64-bit sums; NaN counts as -inf; ties go to the lower page), until `count` are
-   taken.
+   taken.  The last pages are counted from the block's last query: so that in a
+   causal call every query keeps the page that it stands in, keep_last has to be
+   (q_block - 1 + page - 1) / page + 1 (1 for single queries, 2 for blocks of up to
+   page + 1).  With less, the earlier queries of a block see their own page only if its
+   score wins (one that sees none of the block's pages gives O = 0), by a mean that
+   holds keys of later tokens.
      selected: int32 [T / q_block + B, heads, count]; block i of sequence b is
           first[b] / q_block + b + i; pages ascending, then -1; every entry is
           written, blocks without queries (with H = 0: all) with -1

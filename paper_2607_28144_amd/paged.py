@@ -69,7 +69,8 @@ class Rotary:
                "base"   theta factor^(dim / (dim - 2)) in theta's place
                "parts"  f_i where a pair turns `fast` times or more within
                         original_len, f_i / factor where it does so `slow` times or
-                        less, mixed linearly by that number between; queries and
+                        less, mixed linearly by that number of turns (not by the
+                        pair's index) between; the rotated channels of queries and
                         keys times 1 + ln(factor) / 10
     """
 
@@ -261,7 +262,9 @@ def select_pages(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, first:
     of the others those whose mean key has the largest product with the block's
     queries, `count` in all (regenvc_paged_select).  int32 [T // q_block + B, heads,
     count], ascending, -1 behind the last; block i of sequence b is first[b] //
-    q_block + b + i."""
+    q_block + b + i.  The last pages are counted from a block's last query: for each
+    query of a causal call to keep the page that it stands in, keep_last has to be
+    ceil((q_block - 1) / page) + 1, more than the default of 1 where q_block is."""
     idx = _index(cache)
     if q.dim() != 3:
         raise ValueError(f"q must be [T, H, D], got {tuple(q.shape)}")

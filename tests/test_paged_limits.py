@@ -88,3 +88,26 @@ def test_keys_are_cut_up_to_256_sequences():
     shape = dict(H=4, heads=4, page=64, T=600, max_rows=600, max_len=2112)
     assert plan(**shape, causal=1)[1:] == (256, 512) and plan(**shape, causal=0)[1:] == (256, 256)
     assert split(**dict(shape, causal=1)) == split(**dict(shape, causal=0)) == 1
+
+
+@pytest.mark.parametrize("q_block,page", [(1, 16), (2, 16), (16, 16), (17, 16), (18, 16), (64, 64), (64, 16), (20, 128)])
+def test_last_pages_that_keep_a_query_its_own(q_block, page):
+    """In the definition of the choice: with ceil((q_block - 1) / page) + 1 last pages, and no fewer, the page of every query
+    of a causal call is in its block's list, wherever the block begins."""
+    import numpy as np
+
+    from oracle import paged as opaged
+    need = -(-(q_block - 1) // page) + 1
+    pages = need + 4
+    rows = pages * page
+    # scores fall from page to page: none but the kept ones and the first few wins
+    means = -np.arange(pages, dtype=np.float64)[:, None, None] * np.ones((1, 1, 64))
+    q, table = np.ones((rows, 1, 64)), np.arange(pages)[None]
+
+    def kept(keep_last, start):
+        n = rows - start
+        got = opaged.select(q[:n], means, table, [0, n], [rows], page, need, q_block, 0, keep_last, True)
+        return all((start + t) // page in got[t // q_block, 0] for t in range(n))
+    starts = range(page)
+    assert all(kept(need, s) for s in starts)
+    assert need == 1 or not all(kept(need - 1, s) for s in starts)
