@@ -63,12 +63,12 @@ struct Work {
 // plan says so), every wave goes over the sequences, 64 at a time, adds up what there
 // is to do, and finds the one that workgroup `id` has a piece of.  Of one sequence
 // the tiles that fill whole rounds of slots stay whole, and the keys of the rest are
-// cut into as many ranges as the last round has room for: 300 tiles of 64 rows and 4096
-// selected places on 256 slots 82 us, all whole 109; 270 of 256 rows and 21840 places
-// (D = 64) 462 and 825.  Those of several are cut at 5/4 of what
-// a slot has on the average, those with the longest pieces first.  Seven chunks of 1
-// to 1365 tokens behind 0 to 10663 others, 20 heads on 4: 83 us so; cut at 1 or 1.5
-// of the average 87 and 91, in the order of the call 96, cut by a bound that the host
+// cut into as many ranges as the last round has room for: with the join, 264 tiles of 64
+// rows and 4096 selected places on 256 slots 85 us, all whole 110; 264 of 256 rows and
+// 21840 places (D = 64) 496 and 906.  Those of several are cut at 5/4 of what a slot has
+// on the average, those with the longest pieces first.  Seven chunks of 1 to 1365 tokens
+// behind 0 to 10663 others, 20 heads on 4: 80 us so; when it was chosen 83, cut at 1 or
+// 1.5 of the average 87 and 91, in the order of the call 96, cut by a bound that the host
 // has 133 (tiles of 256 rows: each workgroup's begin and end are worth six rounds of
 // keys, so that finer pieces cost more than they even out).
 struct Piece {
@@ -327,6 +327,12 @@ __device__ __forceinline__ bool finite4(f32x4 v)
     return fmaf(v[3], 0.f, fmaf(v[2], 0.f, fmaf(v[1], 0.f, v[0] * 0.f))) == 0.f;
 }
 
+// Places that row `row` of a causal tile sees.
+__device__ __forceinline__ int sees(const Work &w, int row, int G)
+{
+    return max(0, w.blk.pos + (w.row0 + row) / G + 1);
+}
+
 // One past the last place that some rows of a causal tile see and others do not (at least w.least, before w.see) and whose
 // value is not finite in some channel.  Without such a place, w.least or less.  Every lane of the wave takes part and gets
 // the answer.  A tile has no more such places than queries.
@@ -364,11 +370,6 @@ __device__ __forceinline__ int foul_end(const AttnArgs &a, const Work &w)
 // path of finite values, and slow: a row and 64 keys take about 9 us, a wave's rows one
 // after another.  10920 causal queries x 12 heads of 128 with a NaN in the first value 0.55
 // ms (all of their rows done again: 135), in the last one 48, in every value 57.
-// Places that row `row` of a causal tile sees.
-__device__ __forceinline__ int sees(const Work &w, int row, int G)
-{
-    return max(0, w.blk.pos + (w.row0 + row) / G + 1);
-}
 template <int D, bool SPARSE>
 __device__ __forceinline__ void redo_row(const AttnArgs &a, const AttnPlan &p, const Work &w, int row)
 {
@@ -451,11 +452,11 @@ __device__ __forceinline__ void redo_row(const AttnArgs &a, const AttnPlan &p, c
 // 16 rows: eight waves, so that few places need no second launch to join ranges
 // (1024 keys are four rounds); more rows take the registers of two waves each.
 // One query against 32760 places x 12 heads of 128 (201 MB): 39 us, 5.1 TB/s, and
-// 4.8 for the join of 21 ranges; queries of 16 sequences of 1 to 10920 places, 16
-// heads of 64 on 4 (75 MB): 16.4 + 3.9.  16 pages of 64 for one query: 10.9 + 3.9,
+// 4.9 for the join of 21 ranges; queries of 16 sequences of 1 to 10920 places, 16
+// heads of 64 on 4 (75 MB): 16.1 + 4.0.  16 pages of 64 for one query: 10.9 + 4.0,
 // of which a chain of eight dependent loads has most (sequence, list, table, keys).
 // 64 rows: 25 blocks of 64 queries x 12 heads with 64 pages of 64 each (629 MB from
-// the caches, 321 from HBM): 86 us and 5 for the join, 252 tiles whole and 48 in five
+// the caches, 321 from HBM): 85 us and 5 for the join, 252 tiles whole and 48 in five
 // ranges each, at the rate of what lies behind the L2; all whole it took 111.  The
 // next tile's scores beside a tile's weights (142 us instead of 135, with the
 // selection) or every tile's keys in three ranges (149) lose.
@@ -672,9 +673,9 @@ void attn_few_kernel(AttnArgs a, AttnPlan p)
 // 4-7, its V by M(u) of waves 4-7: a barrier before V(u) of the waves that load it.
 // Scores of places that a row does not see are set to -inf before one form of the
 // weights (with a form for either, 90 registers spilled: 409 us instead of 335).
-// 10920 causal queries x 12 heads of 128: 335-350 us, 1.05-1.09 PFLOP/s, matrix units
-// busy for 51 % of the cycles, no LDS conflicts; 1560 queries against 32760 places:
-// 293-301 us in three ranges and 8 for their join; both at the power limit.
+// 10920 causal queries x 12 heads of 128: 332-352 us from card to card, 1.04-1.10 PFLOP/s,
+// matrix units busy for 51 % of the cycles, no LDS conflicts; 1560 queries against 32760
+// places: 295-310 us in three ranges and 8 for their join; both at the power limit.
 constexpr int kManyWaves = 8, kManyRows = 32 * kManyWaves, kManyKeys = 64;
 static_assert(attn_threads(kManyRows) == 64 * kManyWaves, "what the plan counts on");
 
@@ -1146,8 +1147,9 @@ AttnPlan attn_plan(const AttnShape &s, int n_cu)
     const int64_t n = tiles / s.heads, full = s.B == 1 ? tiles / p.fill : 0, whole = full * p.fill / s.heads;
     const bool room = s.B == 1 ? n > whole && ((full + 1) * p.fill / s.heads - whole) / (n - whole) >= 2
                                : tiles < 4 * (int64_t)p.slots && s.B <= kMostCut;
-    // Behind whole rounds the join has to be worth a round's saving: 516 tiles of 64 rows 129 and 132 us at 1024 places to a
-    // tile, 272 and 251 at 4096; 324 of them 52 and 49 at 1024.  Up to four, as partial results of all are in the workspace.
+    // Behind whole rounds the join has to be worth a round's saving.  Blocks of 64 queries of 12 heads of 128 with 1024, 2048,
+    // 4096 places of a list each, all whole or cut: 324 tiles 54 or 56, 76 or 74, 113 or 100 us; 516 of them 79 or 78, 114 or
+    // 104, 169 or 144 (with 512 places 41 or 44, 61 or 64).  Up to four, as partial results of all are in the workspace.
     if (full == 0)
         p.split = room && keys >= (p.tile_rows == 16 && 8 * tiles > p.slots ? 6 : 2) * p.least;
     else
